@@ -460,6 +460,123 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
                                    const int64_t *d_labels, float *d_grad_logits, float *d_row_loss,
                                    void *stream);
 
+/* Losses over rows of logits and their gradients, beside gsplit_softmax_xent: for models that are
+ * trained from actions and advantages, or from pairs of which one is preferred.  d_logits: n_rows rows of
+ * n_classes values (dtype GSPLIT_F32 or GSPLIT_BF16), logits_stride elements apart; the rows a
+ * gsplit_sage_fwd or gsplit_gat_fwd wrote (row r belongs to local_cat[L][r]) or any other model's.
+ * d_grad_logits receives d loss / d logits in the same dtype, rows grad_stride elements apart: it may be
+ * d_logits itself with the same stride (each row is read before it is written), may not overlap it in
+ * another way, and NULL asks for the forward pass alone.  d_actions [n_rows] int64.  With
+ *     log p(r) = log softmax(logits of row r)[action of row r]
+ * a row takes no part in the loss if its action lies outside [0, n_classes), or if all its logits are
+ * -inf (no class is possible): its log p is reported as 0 and its gradient is 0.  Classes with a logit of
+ * -inf have the probability 0 and the gradient 0.  NaN, and logits of +inf, make their row's results NaN.
+ * Sums over a row are float, what is formed once a row is double.  Rows of the buffers' padding (columns
+ * n_classes .. stride) are neither read nor written.  Asynchronous; may be captured into a graph at any
+ * time.  The context lends its scratch memory: a replay of a captured call counts as a call on the
+ * context (one stream at a time). */
+
+/* Clipped policy loss with a KL term.  With rho = exp(log p - d_old_logp[r]), A = d_advantages[r] and
+ * delta = d_ref_logp[r] - log p:
+ *     loss(r) = w(r) * ( max(-A rho, -A clip(rho, 1 - clip_low, 1 + clip_high)) + kl_coef * kl(r) )
+ *     kl(r)   = exp(delta) - delta - 1      (estimates the KL divergence from the reference, >= 0)
+ * The loss is the sum of loss(r).  w = d_row_weight [n_rows], or 1 / n_rows if NULL; a row of weight 0
+ * takes no part (its logits are not read, all its outputs are 0).  Where both sides of the maximum
+ * are equal the gradient is that of the unclipped one.  d_ref_logp may be NULL if kl_coef is 0.  d_row_loss,
+ * d_row_logp (log p) and d_row_kl [n_rows] may be NULL; kl(r) is 0 without d_ref_logp.  EINVAL for NULL
+ * inputs, n_rows < 0, n_classes < 1, strides below n_classes, an unknown dtype, addresses that are no
+ * multiple of their type's size, clip_low outside [0, 1], clip_high or kl_coef negative or not finite. */
+typedef struct {
+    int32_t dtype;
+    float   clip_low, clip_high;
+    float   kl_coef;
+} gsplit_policy_config;
+
+GSPLIT_API int gsplit_policy_loss(gsplit_ctx *ctx, const gsplit_policy_config *config, const void *d_logits,
+                                  int64_t n_rows, int32_t n_classes, int64_t logits_stride,
+                                  const int64_t *d_actions, const float *d_old_logp, const float *d_ref_logp,
+                                  const float *d_advantages, const float *d_row_weight, void *d_grad_logits,
+                                  int64_t grad_stride, float *d_row_loss, float *d_row_logp, float *d_row_kl,
+                                  void *stream);
+
+/* Preference loss over pairs of sequences of rows (paired log ratios).  Sequence q holds the rows
+ * d_seq_ptr[q] .. d_seq_ptr[q + 1] - 1 (DEVICE [2 * n_pairs + 1] int64, ascending, values in
+ * [0, n_rows]; sequences may be empty); pair p prefers sequence 2 p to sequence 2 p + 1.  With
+ * S(q) = the sum of log p over the rows of q that take part, and R = d_ref_logp [2 * n_pairs] (the same
+ * sums under the reference; NULL: 0):
+ *     margin(p) = beta * ( (S(2p) - R(2p)) - (S(2p+1) - R(2p+1)) )
+ *     loss(p)   = w(p) * ( -(1 - e) log sigmoid(margin) - e log sigmoid(-margin) ),  e = label_smoothing
+ * The loss is the sum of loss(p).  w = d_pair_weight [n_pairs], or 1 / n_pairs if NULL; the gradient of the
+ * rows of a pair of weight 0 is 0.  Rows before d_seq_ptr[0] and from d_seq_ptr[2 * n_pairs] on are
+ * neither read nor written, in any buffer.  d_row_logp [n_rows], d_pair_loss and d_pair_margin
+ * [n_pairs] may be NULL.  d_row_work: 16-byte aligned working memory of 4 * n_rows floats.  Offsets
+ * that are not ascending or outside [0, n_rows] give wrong values, but no access outside the buffers.
+ * EINVAL as above, and for beta not finite, label_smoothing outside [0, 1], n_pairs < 0. */
+typedef struct {
+    int32_t dtype;
+    float   beta;
+    float   label_smoothing;
+} gsplit_preference_config;
+
+GSPLIT_API int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_config *config, const void *d_logits,
+                                      int64_t n_rows, int32_t n_classes, int64_t logits_stride,
+                                      const int64_t *d_actions, const int64_t *d_seq_ptr, int64_t n_pairs,
+                                      const float *d_ref_logp, const float *d_pair_weight, void *d_grad_logits,
+                                      int64_t grad_stride, float *d_row_logp, float *d_pair_loss,
+                                      float *d_pair_margin, float *d_row_work, void *stream);
+
+/* Behind the backward pass: the global norm of all gradients, clipping by it, and the update.
+ *     norm = sqrt( sum over all elements of all tensors of g^2 )   (double sums in a fixed order: the
+ *            same bits on every call; stored as float)
+ *     factor = norm > max_norm ? max_norm / norm : 1
+ * A norm that is not finite (an infinity or a NaN among the gradients) is reported, the factor is then
+ * 1 for gsplit_clip_grads, and gsplit_adamw_step leaves parameters and moments as they are.  Tensors are
+ * dense runs of n elements at any address that is a multiple of the element's size; n may be 0 (then the
+ * pointers may be NULL).  The HOST arrays are read during the call.  Asynchronous; may be captured at any
+ * time (the addresses are then fixed).  Scratch memory as for the losses above.
+ * EINVAL for NULL or misaligned pointers, negative counts, unknown dtypes, max_norm not above 0. */
+typedef struct {
+    const void *d_grad;
+    void       *d_out;           /* gsplit_clip_grads: receives factor * gradient; NULL or d_grad: in place */
+    int64_t     n;
+    int32_t     dtype;           /* of both: GSPLIT_F32 or GSPLIT_BF16 */
+} gsplit_grad_tensor;
+
+/* d_norm: DEVICE [1] float.  gsplit_clip_grads: may be NULL. */
+GSPLIT_API int gsplit_grad_norm(gsplit_ctx *ctx, const gsplit_grad_tensor *grads, int64_t n_tensors, float *d_norm,
+                                void *stream);
+GSPLIT_API int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *grads, int64_t n_tensors, double max_norm,
+                                 float *d_norm, void *stream);
+
+/* One AdamW step (decoupled weight decay) with the clipping above on the way: with g = factor * gradient
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     p = (1 - lr * weight_decay) p - lr * (m / (1 - beta1^t)) / ( sqrt(v / (1 - beta2^t)) + eps )
+ * all in float.  A bfloat16 parameter has a float copy, d_master, which is updated; the parameter is then
+ * its rounding (to nearest even).  Gradients may be of either type whatever the parameter's.
+ * max_norm 0: no norm is formed, the factor is 1, d_norm is not written.  t = *d_step if given (DEVICE, read
+ * when the kernels run, taken as 1 if lower), else step >= 1; the learning rate is *d_lr if given, else lr.
+ * EINVAL also for betas outside [0, 1), lr, eps or weight_decay negative or not finite, a missing d_master
+ * (or one that a float parameter has).  No two of a call's tensors may overlap. */
+typedef struct {
+    void       *d_param;
+    float      *d_master;        /* bfloat16 parameters: their float copy; NULL for float ones */
+    const void *d_grad;
+    float      *d_m, *d_v;
+    int64_t     n;
+    int32_t     param_dtype, grad_dtype;
+} gsplit_adamw_tensor;
+
+typedef struct {
+    double         lr, beta1, beta2, eps, weight_decay;
+    double         max_norm;
+    int64_t        step;
+    const int64_t *d_step;
+    const float   *d_lr;
+} gsplit_adamw_config;
+
+GSPLIT_API int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *config, const gsplit_adamw_tensor *tensors,
+                                 int64_t n_tensors, float *d_norm, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,6 +28,7 @@ EXPORTS = [
     "gsplit_input_counts_accumulate", "gsplit_cache_build", "gsplit_gather_features_cached",
     "gsplit_batch_shuffle", "gsplit_sage_activations", "gsplit_gat_score_terms", "gsplit_sample_split_noalloc",
     "gsplit_sample_split_multi", "gsplit_sage_step", "gsplit_gather_features_multi",
+    "gsplit_policy_loss", "gsplit_preference_loss", "gsplit_grad_norm", "gsplit_clip_grads", "gsplit_adamw_step",
 ]
 
 
@@ -86,6 +87,28 @@ class _GatParams(C.Structure):
                 ("d_a_dst", C.POINTER(C.c_void_p)), ("d_bias", C.POINTER(C.c_void_p))]
 
 
+class _PolicyConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_coef", C.c_float)]
+
+
+class _PreferenceConfig(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("beta", C.c_float), ("label_smoothing", C.c_float)]
+
+
+class _GradTensor(C.Structure):
+    _fields_ = [("d_grad", C.c_void_p), ("d_out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _AdamwTensor(C.Structure):
+    _fields_ = [("d_param", C.c_void_p), ("d_master", C.c_void_p), ("d_grad", C.c_void_p), ("d_m", C.c_void_p),
+                ("d_v", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32)]
+
+
+class _AdamwConfig(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")] + [
+        ("step", C.c_int64), ("d_step", C.c_void_p), ("d_lr", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -136,6 +159,13 @@ def load_library():
     L.gsplit_gat_fwd.argtypes = [vp, C.POINTER(_GatParams), vp, vp, vp]
     L.gsplit_gat_bwd.argtypes = [vp, C.POINTER(_GatParams), vp, vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(vp),
                                  C.POINTER(vp), vp]
+    L.gsplit_policy_loss.argtypes = [vp, C.POINTER(_PolicyConfig), vp, i64, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp,
+                                     vp, vp]
+    L.gsplit_preference_loss.argtypes = [vp, C.POINTER(_PreferenceConfig), vp, i64, i32, i64, vp, vp, i64, vp, vp, vp, i64,
+                                         vp, vp, vp, vp, vp]
+    L.gsplit_grad_norm.argtypes = [vp, C.POINTER(_GradTensor), i64, vp, vp]
+    L.gsplit_clip_grads.argtypes = [vp, C.POINTER(_GradTensor), i64, C.c_double, vp, vp]
+    L.gsplit_adamw_step.argtypes = [vp, C.POINTER(_AdamwConfig), C.POINTER(_AdamwTensor), i64, vp, vp]
     for name in EXPORTS:
         if name not in ("gsplit_last_error", "gsplit_max_rows", "gsplit_timing_read"):
             getattr(L, name).restype = C.c_int
@@ -302,6 +332,57 @@ class GatParams:
         self._heads = (C.c_int32 * L)(*heads)
         self._ptrs = [(C.c_void_p * L)(*[t.data_ptr() for t in lst]) for lst in self.tensors]
         self.c = _GatParams(GSPLIT_F32, self._dims, self._heads, *self._ptrs)
+
+
+_DTYPES = {torch.float32: GSPLIT_F32, torch.bfloat16: GSPLIT_BF16}
+
+
+def _same_device(ts):
+    assert all(t.is_cuda and t.device == ts[0].device for t in ts)
+    return ts[0].device if ts else None
+
+
+class GradTensors:
+    """Holds the marshalled gradient tensors of gsplit_grad_norm and gsplit_clip_grads (and keeps them
+    alive).  outs: where the clipped gradients go; None, or the gradients themselves: in place."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+        outs = grads if outs is None else outs
+        assert len(outs) == len(grads)
+        self.device = _same_device([*grads, *outs])
+        for g, o in zip(grads, outs):
+            assert g.dtype in _DTYPES and g.is_contiguous()
+            assert o.dtype == g.dtype and o.is_contiguous() and o.numel() == g.numel()
+        self.tensors = (list(grads), list(outs))
+        self.n = len(self.tensors[0])
+        self.c = (_GradTensor * max(1, self.n))(*[_GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), _DTYPES[g.dtype])
+                                                  for g, o in zip(grads, outs)])
+
+
+class AdamwTensors:
+    """Holds the marshalled tensors of gsplit_adamw_step (and keeps them alive).  masters: the float copies
+    of the bfloat16 parameters, None for the float ones (or None if there are none)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], m: Sequence[torch.Tensor],
+                 v: Sequence[torch.Tensor], masters: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        masters = [None] * len(params) if masters is None else masters
+        assert len(grads) == len(m) == len(v) == len(masters) == len(params)
+        self.device = _same_device([*params, *grads, *m, *v, *[t for t in masters if t is not None]])
+        for p, g, a, b, w in zip(params, grads, m, v, masters):
+            assert p.dtype in _DTYPES and g.dtype in _DTYPES and (w is not None) == (p.dtype == torch.bfloat16)
+            for t in (p, g, a, b, w):
+                assert t is None or (t.is_contiguous() and t.numel() == p.numel())
+            assert all(t is None or t.dtype == torch.float32 for t in (a, b, w))
+        self.tensors = (list(params), list(grads), list(m), list(v), list(masters))
+        self.n = len(self.tensors[0])
+        self.c = (_AdamwTensor * max(1, self.n))(*[
+            _AdamwTensor(p.data_ptr(), None if w is None else w.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
+                         p.numel(), _DTYPES[p.dtype], _DTYPES[g.dtype])
+            for p, g, a, b, w in zip(params, grads, m, v, masters)])
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 class Context:
@@ -491,6 +572,90 @@ class Context:
                                                  grad_logits.data_ptr(),
                                                  row_loss.data_ptr() if row_loss is not None else None,
                                                  _stream()))
+
+    # The calls below need no batch: tensors on the context's device, whichever device is current
+    def _own_stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _check_rows(self, logits, grad_logits, actions, per_row):
+        """(dtype, rows, classes, logits stride, gradient stride)"""
+        assert logits.dim() == 2 and logits.dtype in _DTYPES and logits.device == self.device
+        rows, classes = logits.shape
+        assert logits.stride(1) == 1 or classes == 1
+        assert actions.device == self.device and actions.dtype == torch.int64 and actions.is_contiguous()
+        assert actions.numel() == rows
+        for t in per_row:
+            assert t is None or (t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()
+                                 and t.numel() == rows)
+        if grad_logits is not None:
+            assert grad_logits.shape == logits.shape and grad_logits.dtype == logits.dtype
+            assert grad_logits.device == self.device and (grad_logits.stride(1) == 1 or classes == 1)
+        # (a single row may have any stride)
+        return (_DTYPES[logits.dtype], rows, classes, logits.stride(0) if rows > 1 else classes,
+                classes if grad_logits is None or rows <= 1 else grad_logits.stride(0))
+
+    def gsplit_policy_loss(self, logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor,
+                           advantages: torch.Tensor, grad_logits: Optional[torch.Tensor],
+                           ref_logp: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
+                           clip_low: float = 0.2, clip_high: float = 0.2, kl_coef: float = 0.0,
+                           row_loss: Optional[torch.Tensor] = None, row_logp: Optional[torch.Tensor] = None,
+                           row_kl: Optional[torch.Tensor] = None):
+        """Clipped policy loss with a KL term of every row of logits, and its gradient."""
+        assert old_logp is not None and advantages is not None
+        dt, rows, classes, ld, gld = self._check_rows(
+            logits, grad_logits, actions, (old_logp, advantages, ref_logp, row_weight, row_loss, row_logp, row_kl))
+        cfg = _PolicyConfig(dt, clip_low, clip_high, kl_coef)
+        self._check(self.lib.gsplit_policy_loss(
+            self.h, C.byref(cfg), logits.data_ptr(), rows, classes, ld, actions.data_ptr(), old_logp.data_ptr(),
+            _ptr(ref_logp), advantages.data_ptr(), _ptr(row_weight), _ptr(grad_logits), gld, _ptr(row_loss),
+            _ptr(row_logp), _ptr(row_kl), self._own_stream()))
+
+    def gsplit_preference_loss(self, logits: torch.Tensor, actions: torch.Tensor, seq_ptr: torch.Tensor,
+                               grad_logits: Optional[torch.Tensor], row_work: torch.Tensor,
+                               ref_logp: Optional[torch.Tensor] = None, pair_weight: Optional[torch.Tensor] = None,
+                               beta: float = 0.1, label_smoothing: float = 0.0,
+                               pair_loss: Optional[torch.Tensor] = None, pair_margin: Optional[torch.Tensor] = None,
+                               row_logp: Optional[torch.Tensor] = None):
+        """Preference loss of pairs of sequences of rows (2 p preferred to 2 p + 1), and its gradient.
+        row_work: float32, 4 values a row."""
+        dt, rows, classes, ld, gld = self._check_rows(logits, grad_logits, actions, (row_logp,))
+        assert seq_ptr.device == self.device and seq_ptr.dtype == torch.int64 and seq_ptr.is_contiguous()
+        assert seq_ptr.numel() % 2 == 1
+        pairs = seq_ptr.numel() // 2
+        for t, n in ((ref_logp, 2 * pairs), (pair_weight, pairs), (pair_loss, pairs), (pair_margin, pairs),
+                     (row_work, 4 * rows)):
+            assert t is None or (t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()
+                                 and t.numel() == n)
+        cfg = _PreferenceConfig(dt, beta, label_smoothing)
+        self._check(self.lib.gsplit_preference_loss(
+            self.h, C.byref(cfg), logits.data_ptr(), rows, classes, ld, actions.data_ptr(), seq_ptr.data_ptr(), pairs,
+            _ptr(ref_logp), _ptr(pair_weight), _ptr(grad_logits), gld, _ptr(row_logp), _ptr(pair_loss),
+            _ptr(pair_margin), _ptr(row_work), self._own_stream()))
+
+    def _check_table(self, table, norm):
+        assert table.device in (None, self.device)
+        assert norm is None or (norm.device == self.device and norm.dtype == torch.float32 and norm.numel() == 1)
+
+    def gsplit_grad_norm(self, grads: GradTensors, norm: torch.Tensor):
+        self._check_table(grads, norm)
+        self._check(self.lib.gsplit_grad_norm(self.h, grads.c, grads.n, _ptr(norm), self._own_stream()))
+
+    def gsplit_clip_grads(self, grads: GradTensors, max_norm: float, norm: Optional[torch.Tensor] = None):
+        """Gradients times min(1, max_norm / their global norm) into the table's outputs."""
+        self._check_table(grads, norm)
+        self._check(self.lib.gsplit_clip_grads(self.h, grads.c, grads.n, max_norm, _ptr(norm), self._own_stream()))
+
+    def gsplit_adamw_step(self, tensors: AdamwTensors, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                          eps: float = 1e-8, weight_decay: float = 0.01, step: int = 0, max_norm: float = 0.0,
+                          norm: Optional[torch.Tensor] = None, step_dev: Optional[torch.Tensor] = None,
+                          lr_dev: Optional[torch.Tensor] = None):
+        """AdamW step number `step` (from 1), gradients clipped to max_norm (0: as they are).  step_dev (int64)
+        and lr_dev (float32): the step and the learning rate in device memory, for captured steps."""
+        self._check_table(tensors, norm)
+        assert step_dev is None or (step_dev.device == self.device and step_dev.dtype == torch.int64 and step_dev.numel() == 1)
+        assert lr_dev is None or (lr_dev.device == self.device and lr_dev.dtype == torch.float32 and lr_dev.numel() == 1)
+        cfg = _AdamwConfig(lr, beta1, beta2, eps, weight_decay, max_norm, int(step), _ptr(step_dev), _ptr(lr_dev))
+        self._check(self.lib.gsplit_adamw_step(self.h, C.byref(cfg), tensors.c, tensors.n, _ptr(norm), self._own_stream()))
 
     def gsplit_presample_accumulate(self, vertex_count: Optional[torch.Tensor], edge_count: Optional[torch.Tensor]):
         # torch has no unsigned 32-bit arithmetic: int32 tensors carry the uint32 counters

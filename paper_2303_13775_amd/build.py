@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgsplit.so")
-SOURCES = ["api.hip", "sample_split.hip", "gather.hip", "sage.hip", "presample.hip", "gat.hip", "stats.hip", "cache.hip"]
+SOURCES = ["api.hip", "sample_split.hip", "gather.hip", "sage.hip", "presample.hip", "gat.hip", "stats.hip", "cache.hip",
+           "row_losses.hip", "update.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

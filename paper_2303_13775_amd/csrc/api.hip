@@ -97,6 +97,7 @@ extern "C" int gsplit_create(gsplit_ctx **out, const gsplit_graph *g, const gspl
         delete ctx;
         return gs_fail(nullptr, GSPLIT_EHIP, "gsplit_create: no HIP device");
     }
+    ctx->device = dev;
     ctx->n_cu = prop.multiProcessorCount > 0 ? prop.multiProcessorCount : 256;
 
     // no-dedup upper bounds on the frontier sizes
@@ -178,6 +179,7 @@ extern "C" int gsplit_create(gsplit_ctx **out, const gsplit_graph *g, const gspl
         A((void **)&ctx->pos_pair, sizeof(int32_t) * 2 * max_items, "row pairs by position");
         A((void **)&ctx->mixed_pos, sizeof(int32_t) * max_items, "positions of mixed rows");
     }
+    A((void **)&ctx->norm_part, sizeof(double) * GS_NORM_SLOTS, "gradient norm");
     A((void **)&ctx->part_hist, sizeof(int32_t) * 1024 * 25, "partition histogram");
     A((void **)&ctx->part_base, sizeof(int32_t) * 1024 * 25, "partition bases");
     if (rc == GSPLIT_OK && hipMemset(ctx->d_meta, 0, sizeof(GsLevelMeta) * (L + 1)) != hipSuccess)

@@ -18,6 +18,7 @@
 // launches, which cuts the dependent random accesses per slot from three to one
 #define GS_WIDE_SLOTS (1ll << 20)
 #define GS_MAXL GSPLIT_MAX_LAYERS
+#define GS_NORM_SLOTS 2048
 
 // Device-resident bookkeeping of one level l (0..L) of the current batch.  Every kernel reads its
 // problem sizes from here, so a whole iteration is enqueued without a host round trip.
@@ -192,6 +193,7 @@ struct gsplit_ctx {
     int      rev_from = 1;             // lowest sampling layer with a reverse index (0 with gat_index)
     int64_t  ub_front[GS_MAXL + 1] = {0};   // upper bounds on |local_cat[l]|
     int      n_cu = 256;
+    int      device = 0;
 
     int32_t     *front[GS_MAXL + 1] = {nullptr};
     int32_t     *target_perm = nullptr;
@@ -222,6 +224,8 @@ struct gsplit_ctx {
     hipStream_t  last_stream = nullptr;
     std::shared_ptr<GsEvent> own_done;      // the event that this context's calls record (none: static arrays)
     std::shared_ptr<GsEvent> sample_done;   // the one that stands behind its current batch: its own, or that of a grouped call
+
+    double      *norm_part = nullptr;       // [GS_NORM_SLOTS] a workgroup's sum of squares each (gradient norm)
 
     GsSageBuf    sage;
     GsGatBuf     gat;
@@ -273,6 +277,33 @@ struct GsTimeScope {
         return e;
     }
 };
+
+// A call that needs no batch: makes the context's device the current one while it lasts, takes no timing of a stream
+// under capture (GsTimeScope goes by the batch), and lets no C++ exception out of the C entry.
+template <class F>
+static int gs_call(gsplit_ctx *ctx, hipStream_t st, F &&body) {
+    int before = ctx->device;
+    const bool timing = ctx->timer.enabled;
+    int rc = GSPLIT_EHIP;
+    try {
+        GS_HIP(ctx, hipGetDevice(&before));
+        if (before != ctx->device) GS_HIP(ctx, hipSetDevice(ctx->device));
+        if (timing) {
+            hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+            if (hipStreamIsCapturing(st, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) ctx->timer.enabled = false;
+        }
+        rc = body();
+        if (rc == GSPLIT_OK) {
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) rc = gs_fail(ctx, GSPLIT_EHIP, hipGetErrorString(e));
+        }
+    } catch (...) {
+        rc = GSPLIT_ENOMEM;
+    }
+    ctx->timer.enabled = timing;
+    if (before != ctx->device) (void)hipSetDevice(before);
+    return rc;
+}
 
 static inline int64_t gs_ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 

@@ -1,0 +1,292 @@
+"""The gradient norm, clipping and the AdamW step against their plain float64 forms: many tensors of both types at any address, empty
+ones, norms that are not finite, and the ways a caller may run them.
+
+Tolerances, with u = 2^-24: the norm is a double sum rounded once to float (u); the factor max_norm / norm rounds once more; a clipped
+value is one product (u, and half a step of its type).  The moments are two products and a sum (3 u of their terms).  The parameter's
+change is a square root, a sum, a product and a division of factors that are each rounded (10 u of the change, and for the error of
+the moments in it what the derivatives give: 3 u of the terms of m / root, 3 u / 2 of m / root), its own sum 2 u of its terms."""
+import numpy as np
+import pytest
+import torch
+
+import row_loss_check as K
+from oracle import training as T
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = K.U
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = K.context()
+    yield c
+    c.close()
+
+
+def _cut(flat, sizes, gap):
+    """Views of these sizes into a flat buffer, `gap` values between them."""
+    out, at = [], gap
+    for n in sizes:
+        out.append(flat[at:at + n])
+        at += n + gap
+    return out
+
+
+def _room(sizes, gap):
+    return sum(sizes) + gap * (len(sizes) + 1)
+
+
+def _tensors(rng, sizes, dtypes, scale, gap=0, fill=7.0):
+    """Tensors of these sizes and types, of each type `gap` values apart in one buffer of that type: (tensors, buffers)."""
+    flats, out = {}, [None] * len(sizes)
+    for dt in set(dtypes):
+        which = [i for i, d in enumerate(dtypes) if d == dt]
+        flat = torch.full((_room([sizes[i] for i in which], gap),), fill, dtype=dt, device="cuda")
+        for i, v in zip(which, _cut(flat, [sizes[i] for i in which], gap)):
+            v.copy_(torch.from_numpy((rng.standard_normal(sizes[i]) * scale).astype(np.float32)))
+            out[i] = v
+        flats[dt] = flat
+    return out, flats
+
+
+def _gaps_kept(flats, sizes, dtypes, gap, fill=7.0):
+    for dt, flat in flats.items():
+        mask = torch.ones_like(flat, dtype=torch.bool)
+        for v in _cut(mask, [s for s, d in zip(sizes, dtypes) if d == dt], gap):
+            v.fill_(False)
+        if not bool((flat[mask] == fill).all()):
+            return False
+    return True
+
+
+def _np(ts):
+    return [t.double().cpu().numpy() for t in ts]
+
+
+SETS = [[1], [5], [255, 256, 257], [4095, 4096, 4097], [0, 3, 0, 7, 0], [100 * 256, 100 * 256, 256, 256 * 47, 256 * 47, 47], [20000, 1, 70001, 13, 8192],
+        [1] * 700, list(range(1, 300)), [1_000_003, 17, 2_500_000], [], [0], [33000], [65537], [300_000] * 9]
+
+
+def _types(kind, n):
+    return [F32] * n if kind == "f32" else [BF16] * n if kind == "bf16" else [(F32, BF16)[i % 2] for i in range(n)]
+
+
+@pytest.mark.parametrize("which", range(len(SETS)))
+@pytest.mark.parametrize("kind, gap", [("f32", 0), ("bf16", 0), ("mixed", 1), ("mixed", 3)])
+def test_norm_and_clipping(ctx, which, kind, gap):
+    from paper_2303_13775_amd import GradTensors
+    sizes = SETS[which]
+    dtypes = _types(kind, len(sizes))
+    rng = np.random.default_rng(which)
+    grads, flats = _tensors(rng, sizes, dtypes, 0.5, gap)
+    outs, oflats = _tensors(rng, sizes, dtypes, 0.5, gap)
+    kept = [g.clone() for g in grads]
+    want = T.grad_norm(_np(grads))
+    norm = torch.full((1,), 9.0, device="cuda")
+    ctx.gsplit_grad_norm(GradTensors(grads), norm)
+    assert abs(float(norm) - want) <= 1.5 * U * want
+    for bound in (0.37 * want + 1e-30, 3.0 * want + 1.0):
+        norm.fill_(9.0)
+        ctx.gsplit_clip_grads(GradTensors(grads, outs), bound, norm)
+        torch.cuda.synchronize()
+        assert abs(float(norm) - want) <= 1.5 * U * want
+        f = T.clip_factor(want, bound)
+        for g, o, k in zip(_np(kept), outs, kept):
+            K.check("clipped", o, f * g, 4 * U * np.abs(f * g), o.dtype)
+        assert all(torch.equal(a, b) for a, b in zip(grads, kept))
+        assert _gaps_kept(flats, sizes, dtypes, gap) and _gaps_kept(oflats, sizes, dtypes, gap)
+    ctx.gsplit_clip_grads(GradTensors(grads), 0.37 * want + 1e-30)        # in place, norm not asked for
+    ctx.gsplit_clip_grads(GradTensors(kept, outs), 0.37 * want + 1e-30)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs)) and _gaps_kept(flats, sizes, dtypes, gap)
+    ctx.gsplit_clip_grads(GradTensors(grads), 10.0 * want + 1.0, norm)
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs))             # below the bound: the same bits
+
+
+@pytest.mark.parametrize("sizes", [[40], [100, 30000], [400_000, 17]])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_norm_that_is_not_finite(ctx, sizes, bad):
+    from paper_2303_13775_amd import AdamwTensors, GradTensors
+    rng = np.random.default_rng(1)
+    grads, _ = _tensors(rng, sizes, [F32] * len(sizes), 1.0)
+    grads[-1][7] = float(bad)
+    kept, norm = [g.clone() for g in grads], torch.zeros(1, device="cuda")
+    outs = [torch.zeros_like(g) for g in grads]
+    ctx.gsplit_clip_grads(GradTensors(grads, outs), 0.1, norm)
+    ctx.gsplit_clip_grads(GradTensors(grads), 0.1)
+    same = lambda x, y: bool(((x == y) | (x.isnan() & y.isnan())).all())
+    assert not np.isfinite(float(norm)) and np.isnan(float(norm)) == np.isnan(bad)
+    assert all(same(a, b) and same(a, c) for a, b, c in zip(kept, outs, grads))
+    state = [[torch.rand_like(g) for g in grads] for _ in range(3)]
+    before = [[t.clone() for t in ts] for ts in state]
+    norm.zero_()
+    ctx.gsplit_adamw_step(AdamwTensors(state[0], grads, state[1], state[2]), step=3, max_norm=1.0, norm=norm)
+    assert not np.isfinite(float(norm))
+    assert all(torch.equal(a, b) for x, y in zip(state, before) for a, b in zip(x, y))
+    ctx.gsplit_adamw_step(AdamwTensors(state[0], grads, state[1], state[2]), step=3)      # no norm: the bad value goes where it is
+    assert not np.isfinite(float(state[1][-1][7])) and np.isfinite(float(state[1][-1][8]))
+
+
+def test_norm_of_values_whose_squares_leave_the_floats(ctx):
+    from paper_2303_13775_amd import GradTensors
+    norm = torch.zeros(1, device="cuda")
+    for x in (1e30, 1e-30):
+        for n in (50, 100_000):
+            g = torch.full((n,), x, device="cuda")
+            want = float(g[0].double()) * np.sqrt(n)
+            ctx.gsplit_clip_grads(GradTensors([g]), x, norm)
+            assert abs(float(norm) - want) < 2 * U * want
+            assert abs(float(g[3]) * np.sqrt(n) / x - 1) < 8 * U
+
+
+def _adamw_case(ctx, sizes, ptypes, gtypes, *, gap=0, max_norm=0.0, step=3, seed=0, lr=1e-2, b1=0.9, b2=0.99, eps=1e-8, wd=0.05, dev=False, fresh=False):
+    from paper_2303_13775_amd import AdamwTensors
+    rng = np.random.default_rng(seed)
+    n = len(sizes)
+    params, pf = _tensors(rng, sizes, ptypes, 0.3, gap)
+    grads, gf = _tensors(rng, sizes, gtypes, 0.1, gap)
+    m, mf = _tensors(rng, sizes, [F32] * n, 0.0 if fresh else 0.05, gap)
+    v, vf = _tensors(rng, sizes, [F32] * n, 0.0 if fresh else 0.05, gap)
+    for t in v:
+        t.square_()
+    full, ff = _tensors(rng, sizes, [F32] * n, 0.3, gap)
+    masters = [w if p.dtype == BF16 else None for p, w in zip(params, full)]
+    old = [_np(x) for x in ([w if w is not None else p for p, w in zip(params, masters)], grads, m, v)]
+    table = AdamwTensors(params, grads, m, v, masters)
+    norm = torch.full((1,), 9.0, device="cuda")
+    kw = dict(step_dev=torch.tensor([step], device="cuda"), lr_dev=torch.tensor([lr], device="cuda")) if dev else dict(step=step, lr=lr)
+    ctx.gsplit_adamw_step(table, beta1=b1, beta2=b2, eps=eps, weight_decay=wd, max_norm=max_norm, norm=norm, **kw)
+    torch.cuda.synchronize()
+    want_norm = T.grad_norm(old[1])
+    if max_norm:
+        assert abs(float(norm) - want_norm) <= 1.5 * U * want_norm
+    else:
+        assert float(norm) == 9.0
+    f = T.clip_factor(want_norm, max_norm) if max_norm else 1.0
+    if dev:
+        lr = float(np.float32(lr))
+    for i in range(n):
+        p0, g0, m0, v0 = (old[k][i] for k in range(4))
+        p1, m1, v1 = T.adamw(p0, g0, m0, v0, lr=lr, beta1=b1, beta2=b2, eps=eps, weight_decay=wd, step=step, factor=f)
+        mt = np.abs(b1 * m0) + np.abs((1 - b1) * f * g0)
+        K.check("m", m[i], m1, 5 * U * mt)
+        K.check("v", v[i], v1, 7 * U * v1)
+        root = np.sqrt(v1 / (1 - b2 ** step)) + eps
+        rate = lr / (1 - b1 ** step)
+        tol = rate / root * (6 * U * mt + 14 * U * np.abs(m1)) + 2 * U * np.abs(p0)
+        got = masters[i] if masters[i] is not None else params[i]
+        K.check("p", got, p1, tol)
+        if masters[i] is not None:
+            assert torch.equal(params[i], masters[i].bfloat16())
+    for flats, types in ((pf, ptypes), (gf, gtypes), (mf, [F32] * n), (vf, [F32] * n)):
+        assert _gaps_kept(flats, sizes, types, gap)
+    assert all(torch.equal(a.double().cpu(), torch.from_numpy(b)) for a, b in zip(grads, old[1]))
+
+
+@pytest.mark.parametrize("which", range(len(SETS)))
+@pytest.mark.parametrize("pk, gk, gap", [("f32", "f32", 0), ("bf16", "bf16", 0), ("mixed", "f32", 1), ("f32", "bf16", 3)])
+@pytest.mark.parametrize("max_norm", [0.0, 0.01])
+def test_adamw(ctx, which, pk, gk, gap, max_norm):
+    sizes = SETS[which]
+    _adamw_case(ctx, sizes, _types(pk, len(sizes)), _types(gk, len(sizes)), gap=gap, max_norm=max_norm, seed=which)
+
+
+@pytest.mark.parametrize("kw", [dict(step=1, fresh=True), dict(step=1, fresh=True, eps=1e-3), dict(step=10 ** 6), dict(max_norm=1e9), dict(max_norm=float("inf")),
+                                dict(dev=True, step=7), dict(dev=True, step=1, max_norm=0.1, fresh=True), dict(wd=0.0, lr=0.0), dict(b1=0.0, b2=0.0),
+                                dict(step=2, b2=0.999)])
+def test_adamw_settings(ctx, kw):
+    _adamw_case(ctx, [100, 5000, 33], [F32, BF16, F32], [F32, F32, BF16], **kw)
+    _adamw_case(ctx, [100_000, 5], [F32, BF16], [F32, F32], **kw)
+
+
+def test_device_step_below_one_is_one(ctx):
+    from paper_2303_13775_amd import AdamwTensors
+    rng = np.random.default_rng(2)
+    res = []
+    for s in (1, 0, -4):
+        ts = [_tensors(np.random.default_rng(k), [500], [F32], 0.1)[0] for k in range(3)]
+        v = [t.square() for t in ts[2]]
+        ctx.gsplit_adamw_step(AdamwTensors(ts[0], ts[1], ts[2], v), step_dev=torch.tensor([s], device="cuda"))
+        res.append(ts[0][0])
+    assert torch.equal(res[0], res[1]) and torch.equal(res[0], res[2])
+
+
+@pytest.mark.parametrize("sizes", [[300, 17], [5000] * 40, [1_000_000, 3]])
+def test_captured_steps(ctx, sizes):
+    """Clipping and the update captured once, the step and the learning rate in device memory, replayed for several steps with new
+    gradients and eager work of the same context between the replays: the bits of eager steps."""
+    from paper_2303_13775_amd import AdamwTensors, GradTensors
+    rng = np.random.default_rng(3)
+    n = len(sizes)
+    types = [F32] * n
+
+    def state():
+        r = np.random.default_rng(4)
+        return [_tensors(r, sizes, types, s)[0] for s in (0.3, 0.0, 0.0)]
+
+    grads, _ = _tensors(rng, sizes, types, 0.2)
+    clipped = [torch.zeros_like(g) for g in grads]
+    (p, m, v), (pe, me, ve) = state(), state()
+    step, lr, norm, norm_e = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    table, eager, clip = AdamwTensors(p, grads, m, v), AdamwTensors(pe, grads, me, ve), GradTensors(grads, clipped)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.gsplit_clip_grads(clip, 0.5)
+        ctx.gsplit_adamw_step(table, step_dev=step, lr_dev=lr, max_norm=1.0, norm=norm)
+    other = GradTensors([torch.ones(100_000, device="cuda")])
+    for k in range(1, 6):
+        for g in grads:
+            g.copy_(torch.from_numpy((rng.standard_normal(g.numel()) * 0.2).astype(np.float32)))
+        step.fill_(k)
+        lr.fill_(0.01 / k)
+        ctx.gsplit_clip_grads(clip, 0.5)
+        ctx.gsplit_adamw_step(eager, step_dev=step, lr_dev=lr, max_norm=1.0, norm=norm_e)
+        want = [t.clone() for t in clipped]
+        for t in clipped:
+            t.zero_()
+        ctx.gsplit_grad_norm(other, norm)
+        graph.replay()
+        ctx.gsplit_clip_grads(other, 1.0)
+        if k % 2:
+            torch.cuda.synchronize()
+        assert torch.equal(norm, norm_e) and all(torch.equal(a, b) for a, b in zip(clipped, want)), k
+        assert all(torch.equal(a, b) for x, y in ((p, pe), (m, me), (v, ve)) for a, b in zip(x, y)), k
+
+
+def test_same_bits_every_time_and_on_another_stream(ctx):
+    from paper_2303_13775_amd import GradTensors
+    rng = np.random.default_rng(5)
+    for sizes in ([1000, 3], [3_000_000, 17, 90_000]):
+        grads, _ = _tensors(rng, sizes, _types("mixed", len(sizes)), 1.0)
+        norms = [torch.zeros(1, device="cuda") for _ in range(4)]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        for k, n in enumerate(norms):
+            with torch.cuda.stream(s if k % 2 else torch.cuda.current_stream()):
+                ctx.gsplit_grad_norm(GradTensors(grads), n)
+                torch.cuda.synchronize()
+        assert len({float(n) for n in norms}) == 1
+
+
+def test_refusals(ctx):
+    from paper_2303_13775_amd import AdamwTensors, GradTensors, GsplitError
+    g = torch.ones(8, device="cuda")
+    norm = torch.zeros(1, device="cuda")
+    for bad in (0.0, -1.0, float("nan")):
+        with pytest.raises(GsplitError) as e:
+            ctx.gsplit_clip_grads(GradTensors([g]), bad, norm)
+        assert e.value.code == -1 and "gsplit_clip_grads" in str(e.value)
+    with pytest.raises(GsplitError):
+        ctx.gsplit_grad_norm(GradTensors([g]), None)
+    table = AdamwTensors([g.clone()], [g], [g.clone()], [g.clone()])
+    for kw in (dict(step=0), dict(step=1, beta1=1.0), dict(step=1, lr=-1.0), dict(step=1, max_norm=-1.0), dict(step=1, eps=float("nan"))):
+        with pytest.raises(GsplitError) as e:
+            ctx.gsplit_adamw_step(table, **kw)
+        assert e.value.code == -1 and "gsplit_adamw_step" in str(e.value)
+    for bad in (lambda: GradTensors([g.half()]), lambda: GradTensors([g[::2]]), lambda: GradTensors([g], [g.bfloat16()]), lambda: GradTensors([g.cpu()]),
+                lambda: AdamwTensors([g.bfloat16()], [g], [g], [g]), lambda: AdamwTensors([g], [g], [g], [g], [g]), lambda: AdamwTensors([g], [g[:4]], [g], [g])):
+        with pytest.raises(AssertionError):
+            bad()
+    ctx.gsplit_grad_norm(GradTensors([g]), norm)
+    assert abs(float(norm) - np.sqrt(8)) < 1e-6
