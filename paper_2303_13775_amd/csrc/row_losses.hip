@@ -2,126 +2,110 @@
 // One row: m = max z, s = sum exp(z - m), log p = (z_a - m) - log s; the gradient is slope * (1[c = a] - exp(z_c - m) / s),
 // where the slope d loss / d log p is one number a row (a pair).
 #include <algorithm>
+#include <cmath>
 
 #include "op_checks.h"
 #include "gsplit_internal.h"
+#include "row_pieces.h"
+#include "row_rules.h"
 
 namespace {
-
-typedef __bf16 bf16;
 
 struct Rows {
     const void *logits; int64_t ld;
     void *grad; int64_t gld;
     const int64_t *actions;
     int64_t n; int C;
+    int64_t first = 0;          // row of the launch's first team
 };
 
 struct Policy {
     const float *old_logp, *ref_logp, *advantage, *weight;
     float *loss, *logp, *kl;
+    double log_lo, log_hi;      // logarithms of the clip's borders: a ratio's side is decided in double
     float lo, hi, kl_coef, even_weight;
 };
 
-constexpr int RT = 256;
-
-// maximum and sum over a workgroup of RT threads
-__device__ __forceinline__ float wg_max(float x, float *lds) {
-    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < RT / 64; ++w) x = fmaxf(x, lds[w]);
-    __syncthreads();
-    return x;
-}
-template <class T>
-__device__ __forceinline__ T wg_sum(T x, T *lds) {
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < RT / 64; ++w) x += lds[w];
-    __syncthreads();
-    return x;
-}
-
-// (base, sum of exp(z - base)) of a row: base is its maximum, 0 for a row of -inf alone, whose sum is then 0: a row that has no
-// distribution.  fmaxf drops a NaN, the sum shows it.
-template <class T>
-__device__ __forceinline__ float2 row_stats(const T *z, int C, float *lds) {
-    float m = -INFINITY;
-    for (int c = threadIdx.x; c < C; c += RT) m = fmaxf(m, (float)z[c]);
-    m = wg_max(m, lds);
-    if (m == -INFINITY) m = 0.f;
-    float s = 0.f;
-    for (int c = threadIdx.x; c < C; c += RT) s += __expf((float)z[c] - m);
-    return {m, wg_sum(s, lds)};
-}
 // log p of a row from its statistics and its action's logit, in double: a KL term is a difference of nearly equal numbers
-__device__ __forceinline__ double row_logp(float2 st, float za) { return ((double)za - (double)st.x) - log((double)st.y); }
+__device__ __forceinline__ double row_logp(RowStats st, float za) { return ((double)za - (double)base_of(st.m)) - log((double)st.s); }
 
-// (slope 0 where a row takes no part, or its loss does not move: no class moves it either)
-template <class T>
-__device__ __forceinline__ void row_gradient(const T *z, T *g, int C, float2 st, float slope, int64_t a) {
-    if (slope == 0.f) {
-        for (int c = threadIdx.x; c < C; c += RT) g[c] = (T)0.f;
-        return;
-    }
-    const float scale = slope / st.y;
-    for (int c = threadIdx.x; c < C; c += RT) {
-        const float p = __expf((float)z[c] - st.x) * scale;
-        g[c] = (T)((c == a ? slope : 0.f) - p);
-    }
+// e^x - 1 - x without the cancellation near 0: its series up to |x| = 1 (the first term left out is 4e-9 of the value)
+__device__ __forceinline__ float exp_above_tangent(float x) {
+    if (fabsf(x) > 1.f) return (expf(x) - 1.f) - x;
+    float y = 1.f / 39916800.f;
+    const float c[] = {1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f, 1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 0.5f};
+    for (float k : c) y = fmaf(y, x, k);
+    return x * x * y;
 }
 
-// writes loss, log p and KL term of a row, returns its slope
-__device__ __forceinline__ float policy_row(const Policy &P, int64_t r, double logp, float w) {
-    const double adv = P.advantage[r], ratio = exp(logp - (double)P.old_logp[r]);
-    const double free_ = -adv * ratio;
-    const double held = -adv * fmin(fmax(ratio, 1.0 - (double)P.lo), 1.0 + (double)P.hi);
-    double loss = held, slope = 0.0, kl = 0.0;
-    if (!(free_ < held)) loss = slope = free_;      // (a NaN too)
+// Slope, and through *loss and *kl the loss and the KL term, of one row.  Differences of log-probabilities are formed in double and
+// rounded once; what follows from them is float.
+__device__ __forceinline__ float policy_row(const Policy &P, double logp, float old_logp, float ref_logp, float adv, float w, float *loss, float *kl) {
+    const double d = logp - (double)old_logp;
+    // an advantage above 0 gains nothing from a ratio over the upper border, one below 0 nothing from one under the lower
+    const bool held = adv >= 0.f ? d > P.log_hi : d < P.log_lo;
+    const float ratio = adv == 0.f ? (float)d : expf((float)d);     // (no advantage: 0 times any ratio, NaN stays)
+    float l = -adv * (held ? (adv >= 0.f ? P.hi : P.lo) : ratio), slope = held ? 0.f : l;
+    *kl = 0.f;
     if (P.ref_logp) {
-        const double d = (double)P.ref_logp[r] - logp, e = expm1(d);
-        kl = e - d;
-        if (P.kl_coef > 0.f) { loss += (double)P.kl_coef * kl; slope -= (double)P.kl_coef * e; }
+        const float x = (float)((double)ref_logp - logp);
+        *kl = exp_above_tangent(x);
+        if (P.kl_coef > 0.f) { l += P.kl_coef * *kl; slope -= P.kl_coef * (*kl + x); }
     }
-    if (P.loss) P.loss[r] = (float)((double)w * loss);
-    if (P.logp) P.logp[r] = (float)logp;
-    if (P.kl) P.kl[r] = (float)kl;
-    return (float)((double)w * slope);
-}
-__device__ __forceinline__ void policy_left_out(const Policy &P, int64_t r) {
-    if (P.loss) P.loss[r] = 0.f;
-    if (P.logp) P.logp[r] = 0.f;
-    if (P.kl) P.kl[r] = 0.f;
+    *loss = w * l;
+    return w * slope;
 }
 
-template <class T>
-__global__ __launch_bounds__(RT) void k_policy_rows(Rows R, Policy P) {
-    __shared__ float lds[RT / 64];
+// Lanes LANES of a team take a row each time.  LANES <= 64: several teams a wave, all lanes form the row's numbers alike; else the
+// team is the workgroup, and its first wave does.
+template <class T, int THREADS, int LANES, int E>
+__global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
+    constexpr bool WG = LANES > 64;
+    constexpr bool HELD = E > 0;
+    __shared__ RowStats lds[WG ? THREADS / 64 : 1];
     __shared__ float lds_slope;
-    for (int64_t r = blockIdx.x; r < R.n; r += gridDim.x) {
+    const int lane = WG ? threadIdx.x : threadIdx.x % LANES;
+    constexpr int TEAMS = THREADS / LANES;
+    // (no loop over rows: the compiler keeps what a loop needs in registers that the row is to have)
+    const int64_t r = R.first + (int64_t)blockIdx.x * TEAMS + (WG ? 0 : threadIdx.x / LANES);
+    if (r < R.n) {
         const T *z = (const T *)R.logits + r * R.ld;
+        T *g = R.grad ? (T *)R.grad + r * R.gld : nullptr;
         const float w = P.weight ? P.weight[r] : P.even_weight;
         const int64_t a = R.actions[r];
-        bool used = w != 0.f && a >= 0 && a < R.C;
-        float2 st{0.f, 0.f};
-        float za = 0.f;
-        if (used) {
+        RowStats st{-INFINITY, 0.f};
+        float za = 0.f, slope = 0.f;
+        HeldRow<T, LANES, HELD ? E : PIECE<T>> row;
+        if (w != 0.f && a >= 0 && a < R.C) {
             za = (float)z[a];
-            st = row_stats(z, R.C, lds);
-            used = st.y != 0.f;
+            if constexpr (HELD) { row.load(z, R.C, lane); st = row.stats(); }
+            else st = StreamedRow<T, LANES, -E>::stats(z, R.C, lane);
+            if constexpr (WG) st = join_waves<LANES>(st, lds);
+            else st = join_lanes<LANES>(st);
         }
-        if (threadIdx.x == 0) {
-            lds_slope = 0.f;
-            if (used) lds_slope = policy_row(P, r, row_logp(st, za), w);
-            else policy_left_out(P, r);
+        if (!WG || threadIdx.x < 64) {
+            float loss = 0.f, kl = 0.f, logp = 0.f;
+            if (st.s != 0.f) {      // 0: the row is left out
+                const double lp = row_logp(st, za);
+                logp = (float)lp;
+                slope = policy_row(P, lp, P.old_logp[r], P.ref_logp ? P.ref_logp[r] : 0.f, P.advantage[r], w, &loss, &kl);
+            }
+            if (lane == 0) {
+                if (P.loss) P.loss[r] = loss;
+                if (P.logp) P.logp[r] = logp;
+                if (P.kl) P.kl[r] = kl;
+            }
         }
-        __syncthreads();
-        if (R.grad) row_gradient(z, (T *)R.grad + r * R.gld, R.C, st, lds_slope, a);
-        __syncthreads();
+        if constexpr (WG) {
+            if (threadIdx.x == 0) lds_slope = slope;
+            __syncthreads();
+            slope = lds_slope;
+        }
+        if (g) {
+            if (slope == 0.f) store_zeros<T, LANES>(g, R.C, lane);      // nothing moves it
+            else if constexpr (HELD) row.store(g, R.C, lane, st, slope, (int)a, za);
+            else StreamedRow<T, LANES, -E>::store(z, g, R.C, lane, st, slope, (int)a, za);
+        }
     }
 }
 
@@ -129,7 +113,7 @@ struct Pairs {
     const int64_t *seq_ptr; int64_t n;
     const float *ref_logp, *weight;
     float *row_logp, *loss, *margin;
-    float4 *work;               // a row: base, sum, log p (double); the pairs put the row's slope in its place
+    float4 *work;               // a row: maximum, sum, log p (double); the pairs put the row's slope in its place
     float beta, smoothing, even_weight;
 };
 
@@ -138,36 +122,53 @@ __device__ __forceinline__ int64_t seq_at(const Pairs &Q, int64_t q, int64_t n_r
     return min(max(Q.seq_ptr[q], (int64_t)0), n_rows);
 }
 
-template <class T>
-__global__ __launch_bounds__(RT) void k_preference_rows(Rows R, Pairs Q) {
-    __shared__ float lds[RT / 64];
+template <class T, int THREADS, int LANES, int E>
+__global__ __launch_bounds__(THREADS) void k_preference_rows(Rows R, Pairs Q) {
+    constexpr bool WG = LANES > 64;
+    __shared__ RowStats lds[WG ? THREADS / 64 : 1];
+    const int lane = WG ? threadIdx.x : threadIdx.x % LANES;
+    constexpr int TEAMS = THREADS / LANES;
     const int64_t first = seq_at(Q, 0, R.n), last = seq_at(Q, 2 * Q.n, R.n);
-    for (int64_t r = first + blockIdx.x; r < last; r += gridDim.x) {
+    for (int64_t r = first + (int64_t)blockIdx.x * TEAMS + (WG ? 0 : threadIdx.x / LANES); r < last; r += (int64_t)gridDim.x * TEAMS) {
         const T *z = (const T *)R.logits + r * R.ld;
         const int64_t a = R.actions[r];
-        float2 st{0.f, 0.f};
-        double logp = 0.0;
+        RowStats st{-INFINITY, 0.f};
+        float za = 0.f;
         if (a >= 0 && a < R.C) {
-            const float za = (float)z[a];
-            st = row_stats(z, R.C, lds);
-            if (st.y != 0.f) logp = row_logp(st, za);
+            za = (float)z[a];
+            st = StreamedRow<T, LANES, E>::stats(z, R.C, lane);
+            if constexpr (WG) { st = join_waves<LANES>(st, lds); __syncthreads(); }
+            else st = join_lanes<LANES>(st);
         }
-        if (threadIdx.x == 0) {
+        if (lane == 0) {
+            const double logp = st.s != 0.f ? row_logp(st, za) : 0.0;
             const float2 bits = __builtin_bit_cast(float2, logp);
-            Q.work[r] = {st.x, st.y, bits.x, bits.y};
+            Q.work[r] = {st.m, st.s, bits.x, bits.y};
             if (Q.row_logp) Q.row_logp[r] = (float)logp;
         }
     }
 }
 
-__global__ __launch_bounds__(RT) void k_preference_pairs(Rows R, Pairs Q) {
-    __shared__ double lds[RT / 64];
+constexpr int PT = 256;
+
+__device__ __forceinline__ double wg_sum(double x, double *lds) {
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+    for (int w = 1; w < PT / 64; ++w) x += lds[w];
+    __syncthreads();
+    return x;
+}
+
+__global__ __launch_bounds__(PT) void k_preference_pairs(Rows R, Pairs Q) {
+    __shared__ double lds[PT / 64];
     for (int64_t p = blockIdx.x; p < Q.n; p += gridDim.x) {
         double sum[2];
         for (int k = 0; k < 2; ++k) {
             double x = 0.0;
             const int64_t end = seq_at(Q, 2 * p + k + 1, R.n);
-            for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += RT)
+            for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += PT)
                 x += __builtin_bit_cast(double, make_float2(Q.work[r].z, Q.work[r].w));
             sum[k] = wg_sum(x, lds) - (Q.ref_logp ? (double)Q.ref_logp[2 * p + k] : 0.0);
         }
@@ -183,22 +184,73 @@ __global__ __launch_bounds__(RT) void k_preference_pairs(Rows R, Pairs Q) {
         if (R.grad)
             for (int k = 0; k < 2; ++k) {
                 const int64_t end = seq_at(Q, 2 * p + k + 1, R.n);
-                for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += RT)
+                for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += PT)
                     Q.work[r].z = Q.work[r].y == 0.f ? 0.f : k ? -slope : slope;
             }
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(RT) void k_preference_grad(Rows R, Pairs Q) {
+template <class T, int THREADS, int LANES, int E>
+__global__ __launch_bounds__(THREADS) void k_preference_grad(Rows R, Pairs Q) {
+    constexpr int TEAMS = THREADS / LANES;
+    const int lane = LANES > 64 ? threadIdx.x : threadIdx.x % LANES;
     const int64_t first = seq_at(Q, 0, R.n), last = seq_at(Q, 2 * Q.n, R.n);
-    for (int64_t r = first + blockIdx.x; r < last; r += gridDim.x) {
+    // the last rows first: they are the ones that the pass before has left in the caches
+    for (int64_t r = last - 1 - (int64_t)blockIdx.x * TEAMS - (LANES > 64 ? 0 : threadIdx.x / LANES); r >= first; r -= (int64_t)gridDim.x * TEAMS) {
         const float4 k = Q.work[r];
-        row_gradient((const T *)R.logits + r * R.ld, (T *)R.grad + r * R.gld, R.C, {k.x, k.y}, k.z, R.actions[r]);
+        const T *z = (const T *)R.logits + r * R.ld;
+        T *g = (T *)R.grad + r * R.gld;
+        if (k.z == 0.f) store_zeros<T, LANES>(g, R.C, lane);
+        else {
+            const int64_t a = R.actions[r];
+            StreamedRow<T, LANES, E>::store(z, g, R.C, lane, {k.x, k.y}, k.z, (int)a, (float)z[a]);
+        }
     }
 }
 
-unsigned row_grid(const gsplit_ctx *ctx, int64_t n) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)ctx->n_cu * 8, n)); }
+unsigned row_grid(int64_t n, int teams, int64_t most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, gs_ceil_div(n, teams))); }
+
+template <int N> struct Int { static constexpr int value = N; };
+
+// calls f(threads, lanes, elements a lane) with the constants of the form; -elements: streamed
+template <class F>
+void with_form(int form, F f) {
+    switch (form) {
+        case ROW_16x8: f(Int<256>{}, Int<16>{}, Int<8>{}); break;
+        case ROW_16x16: f(Int<256>{}, Int<16>{}, Int<16>{}); break;
+        case ROW_64x8: f(Int<256>{}, Int<64>{}, Int<8>{}); break;
+        case ROW_64x16: f(Int<256>{}, Int<64>{}, Int<16>{}); break;
+        case ROW_256x8: f(Int<256>{}, Int<256>{}, Int<8>{}); break;
+        case ROW_256x16: f(Int<256>{}, Int<256>{}, Int<16>{}); break;
+        case ROW_256x32: f(Int<256>{}, Int<256>{}, Int<32>{}); break;
+        case ROW_512x32: f(Int<512>{}, Int<512>{}, Int<32>{}); break;
+        case ROW_512x64: f(Int<512>{}, Int<512>{}, Int<64>{}); break;
+        case ROW_1024x64: f(Int<1024>{}, Int<1024>{}, Int<64>{}); break;
+        default: f(Int<1024>{}, Int<1024>{}, Int<-32>{}); break;
+    }
+}
+
+// the same for kernels that stream rows: 16, 64 or 256 lanes a row
+template <class F>
+void with_part(int dtype, int lanes, F f) {
+    const auto typed = [&](auto type) {
+        if (lanes == 16) f(type, Int<256>{}, Int<16>{}, Int<16>{});
+        else if (lanes == 64) f(type, Int<256>{}, Int<64>{}, Int<16>{});
+        else f(type, Int<256>{}, Int<256>{}, Int<32>{});
+    };
+    if (dtype == GSPLIT_F32) typed(float{});
+    else typed(bf16{});
+}
+
+template <class T>
+void launch_policy(Rows R, const Policy &P, hipStream_t st) {
+    with_form(row_form(R.C, PIECE<T>), [&](auto threads, auto lanes, auto e) {
+        constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
+        constexpr int64_t MOST = 1 << 21;       // workgroups of a launch: it has less than 2^32 threads
+        for (; R.first < R.n; R.first += MOST * (TH / LA))
+            hipLaunchKernelGGL((k_policy_rows<T, TH, LA, E>), dim3(row_grid(R.n - R.first, TH / LA, MOST)), dim3(TH), 0, st, R, P);
+    });
+}
 
 }  // namespace
 
@@ -216,10 +268,11 @@ extern "C" int gsplit_policy_loss(gsplit_ctx *ctx, const gsplit_policy_config *c
         if (n_rows == 0) return GSPLIT_OK;
         const Rows R{d_logits, logits_stride, d_grad_logits, grad_stride, d_actions, n_rows, n_classes};
         const Policy P{d_old_logp, d_ref_logp, d_advantages, d_row_weight, d_row_loss, d_row_logp, d_row_kl,
-                       c->clip_low, c->clip_high, c->kl_coef, (float)(1.0 / (double)n_rows)};
+                       std::log(1.0 - (double)c->clip_low), std::log1p((double)c->clip_high), (float)(1.0 - (double)c->clip_low),
+                       (float)(1.0 + (double)c->clip_high), c->kl_coef, (float)(1.0 / (double)n_rows)};
         GsTimeScope ts(ctx, "policy_loss", -1, st);
-        if (c->dtype == GSPLIT_F32) hipLaunchKernelGGL(k_policy_rows<float>, dim3(row_grid(ctx, n_rows)), dim3(RT), 0, st, R, P);
-        else hipLaunchKernelGGL(k_policy_rows<bf16>, dim3(row_grid(ctx, n_rows)), dim3(RT), 0, st, R, P);
+        if (c->dtype == GSPLIT_F32) launch_policy<float>(R, P, st);
+        else launch_policy<bf16>(R, P, st);
         return GSPLIT_OK;
     });
 }
@@ -240,21 +293,26 @@ extern "C" int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
         const Rows R{d_logits, logits_stride, d_grad_logits, grad_stride, d_actions, n_rows, n_classes};
         const Pairs Q{d_seq_ptr, n_pairs, d_ref_logp, d_pair_weight, d_row_logp, d_pair_loss, d_pair_margin,
                       (float4 *)d_row_work, c->beta, c->label_smoothing, (float)(1.0 / (double)n_pairs)};
-        const dim3 rows(row_grid(ctx, n_rows)), block(RT);
-        const bool f32 = c->dtype == GSPLIT_F32;
+        const int64_t most = (int64_t)ctx->n_cu * 32;
         if (n_rows > 0) {
             GsTimeScope ts(ctx, "preference_rows", -1, st);
-            if (f32) hipLaunchKernelGGL(k_preference_rows<float>, rows, block, 0, st, R, Q);
-            else hipLaunchKernelGGL(k_preference_rows<bf16>, rows, block, 0, st, R, Q);
+            with_part(c->dtype, row_part(n_classes), [&](auto type, auto threads, auto lanes, auto e) {
+                using T = decltype(type);
+                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
+                hipLaunchKernelGGL((k_preference_rows<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);
+            });
         }
         {
             GsTimeScope ts(ctx, "preference_pairs", -1, st);
-            hipLaunchKernelGGL(k_preference_pairs, dim3(row_grid(ctx, n_pairs)), block, 0, st, R, Q);
+            hipLaunchKernelGGL(k_preference_pairs, dim3(row_grid(n_pairs, 1, most)), dim3(PT), 0, st, R, Q);
         }
         if (n_rows > 0 && d_grad_logits) {
             GsTimeScope ts(ctx, "preference_grad", -1, st);
-            if (f32) hipLaunchKernelGGL(k_preference_grad<float>, rows, block, 0, st, R, Q);
-            else hipLaunchKernelGGL(k_preference_grad<bf16>, rows, block, 0, st, R, Q);
+            with_part(c->dtype, row_part(n_classes), [&](auto type, auto threads, auto lanes, auto e) {
+                using T = decltype(type);
+                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
+                hipLaunchKernelGGL((k_preference_grad<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);
+            });
         }
         return GSPLIT_OK;
     });
