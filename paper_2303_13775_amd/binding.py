@@ -575,24 +575,25 @@ class Context:
 
     # The calls below need no batch: tensors on the context's device, whichever device is current
     def _own_stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+        # (the raw handle: torch.cuda.current_stream() builds a Stream object, 2 us of a call that takes 7)
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def _check_rows(self, logits, grad_logits, actions, per_row):
         """(dtype, rows, classes, logits stride, gradient stride)"""
-        assert logits.dim() == 2 and logits.dtype in _DTYPES and logits.device == self.device
+        assert logits.dim() == 2 and logits.dtype in _DTYPES
+        dev, dt = self.device, _DTYPES[logits.dtype]
         rows, classes = logits.shape
-        assert logits.stride(1) == 1 or classes == 1
-        assert actions.device == self.device and actions.dtype == torch.int64 and actions.is_contiguous()
-        assert actions.numel() == rows
+        ld, step = logits.stride()
+        assert logits.device == dev and (step == 1 or classes == 1)
+        assert actions.dtype is torch.int64 and actions.device == dev and actions.is_contiguous() and actions.numel() == rows
         for t in per_row:
-            assert t is None or (t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()
-                                 and t.numel() == rows)
+            assert t is None or (t.dtype is torch.float32 and t.device == dev and t.is_contiguous() and t.numel() == rows)
+        gld = classes
         if grad_logits is not None:
-            assert grad_logits.shape == logits.shape and grad_logits.dtype == logits.dtype
-            assert grad_logits.device == self.device and (grad_logits.stride(1) == 1 or classes == 1)
-        # (a single row may have any stride)
-        return (_DTYPES[logits.dtype], rows, classes, logits.stride(0) if rows > 1 else classes,
-                classes if grad_logits is None or rows <= 1 else grad_logits.stride(0))
+            gld, step = grad_logits.stride()
+            assert grad_logits.shape == logits.shape and grad_logits.dtype is logits.dtype
+            assert grad_logits.device == dev and (step == 1 or classes == 1)
+        return (dt, rows, classes, ld, gld) if rows > 1 else (dt, rows, classes, classes, classes)  # (one row: any stride)
 
     def gsplit_policy_loss(self, logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor,
                            advantages: torch.Tensor, grad_logits: Optional[torch.Tensor],

@@ -1,27 +1,26 @@
 // Behind the backward pass: the global gradient norm over many tensors, clipping by it, and the AdamW update.
 #include <algorithm>
+#include <cmath>
 
 #include "op_checks.h"
 #include "gsplit_internal.h"
+#include "row_pieces.h"
+#include "update_rules.h"
 
 namespace {
 
-typedef __bf16 bf16;
-
-constexpr int UT = 256;
-// The tensors of a launch travel in its arguments (up to 4 KB), so a captured call needs no table in device memory; more of them
+// The tensors of a launch travel in its arguments (up to 4 KB), so a captured call needs no table in device memory; more tensors
 // take more launches.
-constexpr int NORM_TENSORS = 128;
-constexpr int ADAMW_TENSORS = 56;
+constexpr int NORM_TENSORS = 224, CLIP_TENSORS = 144, ADAMW_TENSORS = 72;
 
-// How a launch's elements are dealt to workgroups: every tensor in chunks of `chunk` elements, numbered through
+// How the elements of a launch's tensors (none of them empty) are dealt: in chunks of `chunk` elements, numbered through
 template <int N>
 struct Chunks {
     int32_t first[N + 1];       // first chunk of a tensor
-    int32_t n;
-    int64_t chunk;
-    int64_t len[N];
-    __device__ __forceinline__ int tensor_of(int c) const {     // the last tensor with first <= c: tensors may be empty
+    int32_t tail[N];            // elements of its last chunk
+    int32_t n, chunk;
+    __device__ __forceinline__ int count() const { return first[n]; }
+    __device__ __forceinline__ int tensor_of(int c) const {
         int lo = 0, hi = n;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -29,68 +28,110 @@ struct Chunks {
         }
         return lo;
     }
+    __device__ __forceinline__ int64_t start(int c, int t) const { return (int64_t)(c - first[t]) * chunk; }
+    __device__ __forceinline__ int len(int c, int t) const { return c + 1 == first[t + 1] ? tail[t] : chunk; }
 };
-struct Grads {
-    Chunks<NORM_TENSORS> at;
+template <int N> struct Bits {
+    uint32_t w[(N + 31) / 32];
+    __device__ __forceinline__ bool operator[](int i) const { return w[i >> 5] >> (i & 31) & 1; }
+    void set(int i) { w[i >> 5] |= 1u << (i & 31); }
+};
+struct Norm {
     const void *g[NORM_TENSORS];
-    void *out[NORM_TENSORS];
-    uint32_t half[NORM_TENSORS / 32];
+    Chunks<NORM_TENSORS> at;
+    Bits<NORM_TENSORS> half;
+};
+struct Clip {
+    const void *g[CLIP_TENSORS];
+    void *out[CLIP_TENSORS];
+    Chunks<CLIP_TENSORS> at;
+    Bits<CLIP_TENSORS> half;
 };
 struct Adamw {
-    Chunks<ADAMW_TENSORS> at;
     void *p[ADAMW_TENSORS];
     float *master[ADAMW_TENSORS];
     const void *g[ADAMW_TENSORS];
     float *m[ADAMW_TENSORS], *v[ADAMW_TENSORS];
-    uint32_t half_p[2], half_g[2];
+    Chunks<ADAMW_TENSORS> at;
+    Bits<ADAMW_TENSORS> half_p, half_g;
 };
-static_assert(sizeof(Grads) <= 4096 - 256 && sizeof(Adamw) <= 4096 - 256, "kernel arguments");
+static_assert(sizeof(Norm) <= 4096 - 128 && sizeof(Clip) <= 4096 - 128 && sizeof(Adamw) <= 4096 - 256, "kernel arguments");
 
-struct Hyper {
-    double lr, beta1, beta2, weight_decay;
-    float eps, max_norm;
-    int64_t step;
-    const int64_t *d_step;
-    const float *d_lr;
-};
+// -- the norm ---------------------------------------------------------------------------------
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+// read again by the pass that uses the norm: not past the caches
+__device__ __forceinline__ u32x4 load_kept(const void *p) { return *(const u32x4_any *)p; }
+
+// Squares are formed and summed in double, which holds those of every float: neither 1e30 nor 1e-30 leaves its range, and the norm
+// is the float next to the exact one.  (A conversion and a double multiply-add an element: a fifth of what the chip could do in
+// the time the elements take to come.)
 template <class T>
-__device__ __forceinline__ double sum_of_squares(const T *g, int64_t n) {
+__device__ __forceinline__ double squares(u32x4 q, double s) {
+    float x[PIECE<T>];
+    unpack<T>(q, x);
+#pragma unroll
+    for (int k = 0; k < PIECE<T>; ++k) s = fma((double)x[k], (double)x[k], s);
+    return s;
+}
+template <class T, int THREADS>
+__device__ __forceinline__ double sum_of_squares(const T *g, int n) {
+    constexpr int V = PIECE<T>, DEEP = 4;       // pieces a thread has in flight
+    const int nv = n / V;
     double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += UT) { const double x = (float)g[i]; s += x * x; }
+    int j = threadIdx.x;
+    for (; j + (DEEP - 1) * THREADS < nv; j += DEEP * THREADS) {
+        u32x4 q[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) q[i] = load_kept(g + (j + i * THREADS) * V);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) s = squares<T>(q[i], s);
+    }
+    for (; j < nv; j += THREADS) s = squares<T>(load_kept(g + j * V), s);
+    if ((int)threadIdx.x < n - nv * V) { const double x = (float)g[nv * V + threadIdx.x]; s = fma(x, x, s); }
     return s;
 }
 
+template <int THREADS>
 __device__ __forceinline__ double wg_sum(double x, double *lds) {
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
     x = lds[0];
-    for (int w = 1; w < UT / 64; ++w) x += lds[w];
-    __syncthreads();
+    for (int w = 1; w < THREADS / 64; ++w) x += lds[w];
     return x;
 }
 
-__device__ __forceinline__ bool bit_of(const uint32_t *w, int i) { return w[i >> 5] >> (i & 31) & 1; }
+// this workgroup's share of all squares, as one of `of` workgroups
+template <int THREADS, class Table, class Half>
+__device__ __forceinline__ double share_of_squares(const Table &G, const Half &half, int which, int of) {
+    double s = 0.0;
+    for (int c = which; c < G.at.count(); c += of) {
+        const int t = G.at.tensor_of(c);
+        const int64_t at = G.at.start(c, t);
+        s += half[t] ? sum_of_squares<bf16, THREADS>((const bf16 *)G.g[t] + at, G.at.len(c, t))
+                     : sum_of_squares<float, THREADS>((const float *)G.g[t] + at, G.at.len(c, t));
+    }
+    return s;
+}
+
+constexpr int UT = 256;
 
 // slot b = workgroup b's sum; the launches of one call (`add` in all but the first) have the same grid
-__global__ __launch_bounds__(UT) void k_grad_norm(Grads G, double *__restrict__ slots, bool add) {
+__global__ __launch_bounds__(UT) void k_grad_norm(Norm G, double *__restrict__ slots, bool add) {
     __shared__ double lds[UT / 64];
-    double s = 0.0;
-    for (int c = blockIdx.x; c < G.at.first[G.at.n]; c += gridDim.x) {
-        const int t = G.at.tensor_of(c);
-        const int64_t at = (int64_t)(c - G.at.first[t]) * G.at.chunk, n = min(G.at.chunk, G.at.len[t] - at);
-        s += bit_of(G.half, t) ? sum_of_squares((const bf16 *)G.g[t] + at, n) : sum_of_squares((const float *)G.g[t] + at, n);
-    }
-    s = wg_sum(s, lds);
+    const double s = wg_sum<UT>(share_of_squares<UT>(G, G.half, blockIdx.x, gridDim.x), lds);
     if (threadIdx.x == 0) slots[blockIdx.x] = add ? slots[blockIdx.x] + s : s;
 }
 
 // the norm, from the slots of the kernel above
+template <int THREADS>
 __device__ __forceinline__ float norm_of(const double *__restrict__ slots, int n_slots, double *lds) {
     double s = 0.0;
-    for (int i = threadIdx.x; i < n_slots; i += UT) s += slots[i];
-    return (float)sqrt(wg_sum(s, lds));
+    for (int i = threadIdx.x; i < n_slots; i += THREADS) s += slots[i];
+    return (float)sqrt(wg_sum<THREADS>(s, lds));
 }
 __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
 __device__ __forceinline__ float factor_of(float norm, float max_norm) {
@@ -99,127 +140,239 @@ __device__ __forceinline__ float factor_of(float norm, float max_norm) {
 
 __global__ __launch_bounds__(UT) void k_norm_of(const double *__restrict__ slots, int n_slots, float *__restrict__ norm) {
     __shared__ double lds[UT / 64];
-    const float x = norm_of(slots, n_slots, lds);
+    const float x = norm_of<UT>(slots, n_slots, lds);
     if (threadIdx.x == 0) *norm = x;
 }
 
+// -- clipping ---------------------------------------------------------------------------------
+
 template <class T>
-__device__ __forceinline__ void scale_run(const T *g, T *out, int64_t n, float f) {
-    for (int64_t i = threadIdx.x; i < n; i += UT) out[i] = (T)((float)g[i] * f);
+__device__ __forceinline__ u32x4 scaled(u32x4 q, float f) {
+    float x[PIECE<T>];
+    unpack<T>(q, x);
+#pragma unroll
+    for (int k = 0; k < PIECE<T>; ++k) x[k] *= f;
+    return pack<T>(x);
+}
+template <class T, int THREADS>
+__device__ __forceinline__ void scale_run(const T *g, T *out, int n, float f) {
+    constexpr int V = PIECE<T>, DEEP = 4;
+    const int nv = n / V;
+    int j = threadIdx.x;
+    for (; j + (DEEP - 1) * THREADS < nv; j += DEEP * THREADS) {
+        u32x4 q[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) q[i] = load_piece(g + (j + i * THREADS) * V);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) store_piece(out + (j + i * THREADS) * V, scaled<T>(q[i], f));
+    }
+    for (; j < nv; j += THREADS) store_piece(out + j * V, scaled<T>(load_piece(g + j * V), f));
+    if ((int)threadIdx.x < n - nv * V) out[nv * V + threadIdx.x] = (T)((float)g[nv * V + threadIdx.x] * f);
 }
 
-__global__ __launch_bounds__(UT) void k_clip(Grads G, const double *__restrict__ slots, int n_slots, float max_norm,
-                                             float *__restrict__ norm_out) {
-    __shared__ double lds[UT / 64];
-    const float norm = norm_of(slots, n_slots, lds), f = factor_of(norm, max_norm);
-    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-    for (int c = blockIdx.x; c < G.at.first[G.at.n]; c += gridDim.x) {
+template <int THREADS>
+__device__ __forceinline__ void scale_chunks(const Clip &G, float f, int which, int of) {
+    // the last chunks first: the norm's pass has left them in the caches
+    for (int c = G.at.count() - 1 - which; c >= 0; c -= of) {
         const int t = G.at.tensor_of(c);
         if (f == 1.f && G.out[t] == G.g[t]) continue;
-        const int64_t at = (int64_t)(c - G.at.first[t]) * G.at.chunk, n = min(G.at.chunk, G.at.len[t] - at);
-        if (bit_of(G.half, t)) scale_run((const bf16 *)G.g[t] + at, (bf16 *)G.out[t] + at, n, f);
-        else scale_run((const float *)G.g[t] + at, (float *)G.out[t] + at, n, f);
+        const int64_t at = G.at.start(c, t);
+        if (G.half[t]) scale_run<bf16, THREADS>((const bf16 *)G.g[t] + at, (bf16 *)G.out[t] + at, G.at.len(c, t), f);
+        else scale_run<float, THREADS>((const float *)G.g[t] + at, (float *)G.out[t] + at, G.at.len(c, t), f);
     }
 }
 
-struct Steps { float f, keep, rate, b1, a1, b2, a2, root, eps; };      // of one launch's update
+__global__ __launch_bounds__(UT) void k_clip(Clip G, const double *__restrict__ slots, int n_slots, float max_norm,
+                                             float *__restrict__ norm_out) {
+    __shared__ double lds[UT / 64];
+    const float norm = norm_of<UT>(slots, n_slots, lds);
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+    scale_chunks<UT>(G, factor_of(norm, max_norm), blockIdx.x, gridDim.x);
+}
 
+// Norm and clipping of few elements by one workgroup (several could not clip in place: one would scale what another still adds up)
+constexpr int ST = 1024;
+__global__ __launch_bounds__(ST) void k_clip_small(Clip G, float max_norm, float *__restrict__ norm_out) {
+    __shared__ double lds[ST / 64];
+    const float norm = (float)sqrt(wg_sum<ST>(share_of_squares<ST>(G, G.half, 0, 1), lds));
+    if (norm_out && threadIdx.x == 0) *norm_out = norm;
+    scale_chunks<ST>(G, factor_of(norm, max_norm), 0, 1);
+}
+
+// -- the update -------------------------------------------------------------------------------
+
+struct Hyper {
+    double lr, beta1, beta2, weight_decay;
+    int64_t step;
+    const int64_t *d_step;
+    const float *d_lr;
+    float eps, max_norm;
+};
+struct Steps { float f, keep, rate, b1, a1, b2, a2, root, eps; };      // the numbers of a launch's update
+
+__host__ __device__ inline Steps steps_of(const Hyper &H, double lr, double t) {
+    return {1.f, (float)(1.0 - lr * H.weight_decay), (float)(lr / (1.0 - pow(H.beta1, t))), (float)H.beta1, (float)(1.0 - H.beta1),
+            (float)H.beta2, (float)(1.0 - H.beta2), (float)(1.0 / (1.0 - pow(H.beta2, t))), H.eps};
+}
+
+// four elements; the gradient of either type
 template <class T>
-__device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, float *m, float *v, int64_t n, const Steps &S) {
-    for (int64_t i = threadIdx.x; i < n; i += UT) {
-        const float x = (float)g[i] * S.f;
-        const float mi = S.b1 * m[i] + S.a1 * x, vi = S.b2 * v[i] + S.a2 * (x * x);
-        const float pi = S.keep * p[i] - S.rate * mi / (sqrtf(vi * S.root) + S.eps);
-        m[i] = mi; v[i] = vi; p[i] = pi;
-        if (half) half[i] = (bf16)pi;
+__device__ __forceinline__ void load4(const T *g, float *x) {
+    if constexpr (sizeof(T) == 4) {
+        unpack<float>(load_piece(g), x);
+    } else {
+        const u32x2 q = __builtin_nontemporal_load((const u32x2_any *)g);
+        for (int k = 0; k < 2; ++k) { x[2 * k] = __uint_as_float(q[k] << 16); x[2 * k + 1] = __uint_as_float(q[k] & 0xffff0000u); }
+    }
+}
+__device__ __forceinline__ void update1(float &p, float &m, float &v, float g, const Steps &S) {
+    g *= S.f;
+    m = S.b1 * m + S.a1 * g;
+    v = S.b2 * v + S.a2 * (g * g);
+    p = S.keep * p - S.rate * m / (sqrtf(v * S.root) + S.eps);
+}
+template <class T, bool HALF>
+__device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, float *m, float *v, int n, const Steps &S) {
+    constexpr int DEEP = 2;
+    const int nv = n / 4;
+    const auto step = [&](int j, auto deep) {
+        constexpr int D = decltype(deep)::value;
+        float pp[D][4], mm[D][4], vv[D][4], gg[D][4];
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int e = (j + i * UT) * 4;
+            load4(p + e, pp[i]); load4(m + e, mm[i]); load4(v + e, vv[i]); load4(g + e, gg[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int e = (j + i * UT) * 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) update1(pp[i][k], mm[i][k], vv[i][k], gg[i][k], S);
+            store_piece(p + e, pack<float>(pp[i])); store_piece(m + e, pack<float>(mm[i])); store_piece(v + e, pack<float>(vv[i]));
+            if constexpr (HALF)
+                __builtin_nontemporal_store((u32x2{bf16_pair(pp[i][0], pp[i][1]), bf16_pair(pp[i][2], pp[i][3])}), (u32x2_any *)(half + e));
+        }
+    };
+    int j = threadIdx.x;
+    for (; j + (DEEP - 1) * UT < nv; j += DEEP * UT) step(j, std::integral_constant<int, DEEP>{});
+    for (; j < nv; j += UT) step(j, std::integral_constant<int, 1>{});
+    if ((int)threadIdx.x < n - nv * 4) {
+        const int e = nv * 4 + threadIdx.x;
+        float pi = p[e], mi = m[e], vi = v[e];
+        update1(pi, mi, vi, (float)g[e], S);
+        p[e] = pi; m[e] = mi; v[e] = vi;
+        if constexpr (HALF) half[e] = (bf16)pi;
     }
 }
 
-__global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, const double *__restrict__ slots, int n_slots,
+// How the norm reaches the update: not at all, from the slots, or formed by every workgroup anew (few elements)
+enum : int { NORM_NONE, NORM_SLOTS, NORM_HERE };
+
+template <int WHENCE>
+__global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, Steps S, const double *__restrict__ slots, int n_slots,
                                               float *__restrict__ norm_out) {
     __shared__ double lds[UT / 64];
-    Steps S;
-    S.f = 1.f;
-    if (n_slots) {
-        const float norm = norm_of(slots, n_slots, lds);
+    if (H.d_step || H.d_lr) {
+        __shared__ Steps shared;
+        if (threadIdx.x == 0)
+            shared = steps_of(H, H.d_lr ? (double)*H.d_lr : H.lr, (double)(H.d_step ? max(*H.d_step, (int64_t)1) : H.step));
+        __syncthreads();
+        S = shared;
+    }
+    if constexpr (WHENCE != NORM_NONE) {
+        float norm;
+        if constexpr (WHENCE == NORM_SLOTS) norm = norm_of<UT>(slots, n_slots, lds);
+        else norm = (float)sqrt(wg_sum<UT>(share_of_squares<UT>(A, A.half_g, 0, 1), lds));
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
         if (!is_finite(norm)) return;
         S.f = factor_of(norm, H.max_norm);
     }
-    const double lr = H.d_lr ? (double)*H.d_lr : H.lr;
-    const double t = (double)(H.d_step ? max(*H.d_step, (int64_t)1) : H.step);
-    S.keep = (float)(1.0 - lr * H.weight_decay);
-    S.rate = (float)(lr / (1.0 - pow(H.beta1, t)));
-    S.root = (float)(1.0 / (1.0 - pow(H.beta2, t)));
-    S.b1 = (float)H.beta1; S.a1 = (float)(1.0 - H.beta1);
-    S.b2 = (float)H.beta2; S.a2 = (float)(1.0 - H.beta2);
-    S.eps = H.eps;
-    for (int c = blockIdx.x; c < A.at.first[A.at.n]; c += gridDim.x) {
-        const int k = A.at.tensor_of(c);
-        const int64_t at = (int64_t)(c - A.at.first[k]) * A.at.chunk, n = min(A.at.chunk, A.at.len[k] - at);
-        float *p = bit_of(A.half_p, k) ? A.master[k] + at : (float *)A.p[k] + at;
-        bf16 *half = bit_of(A.half_p, k) ? (bf16 *)A.p[k] + at : nullptr;
-        if (bit_of(A.half_g, k)) update_run(p, half, (const bf16 *)A.g[k] + at, A.m[k] + at, A.v[k] + at, n, S);
-        else update_run(p, half, (const float *)A.g[k] + at, A.m[k] + at, A.v[k] + at, n, S);
+    for (int c = A.at.count() - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+        const int t = A.at.tensor_of(c), n = A.at.len(c, t);
+        const int64_t at = A.at.start(c, t);
+        float *m = A.m[t] + at, *v = A.v[t] + at;
+        const float *g = (const float *)A.g[t] + at;
+        const bf16 *gh = (const bf16 *)A.g[t] + at;
+        if (A.half_p[t]) {
+            float *p = A.master[t] + at;
+            bf16 *half = (bf16 *)A.p[t] + at;
+            if (A.half_g[t]) update_run<bf16, true>(p, half, gh, m, v, n, S);
+            else update_run<float, true>(p, half, g, m, v, n, S);
+        } else {
+            float *p = (float *)A.p[t] + at;
+            if (A.half_g[t]) update_run<bf16, false>(p, nullptr, gh, m, v, n, S);
+            else update_run<float, false>(p, nullptr, g, m, v, n, S);
+        }
     }
 }
 
-int64_t chunk_of(int64_t total) {
-    int64_t chunk = 4096;
-    while (chunk < total / (4 * GS_NORM_SLOTS)) chunk *= 2;
-    return chunk;
-}
+// -- launches ---------------------------------------------------------------------------------
 
-// Calls launch(group) for the tensors in groups of N, chunks laid out; fill(group, k, i): tensor i is the group's k-th
+// Calls launch(group, first) for the tensors that are not empty, in groups of N (one empty group if there are none), the last
+// ones first if `back`; fill(group, k, i): tensor i is the group's k-th.
 template <int N, class Group, class Len, class Fill, class Launch>
-void in_groups(int64_t n_tensors, int64_t chunk, Len len, Fill fill, Launch launch) {
-    for (int64_t from = 0; from < n_tensors || from == 0; from += N) {
+void in_groups(int64_t n_tensors, int chunk, bool back, Len len, Fill fill, Launch launch) {
+    bool first = true;
+    int64_t i = back ? n_tensors - 1 : 0;
+    const int64_t by = back ? -1 : 1;
+    do {
+        int64_t from = i, to = i;           // a group's tensors: their own order in either direction
+        int found = 0;
+        for (; to >= 0 && to < n_tensors && found < N; to += by) found += len(to) > 0;
+        if (back) { const int64_t t = from; from = to + 1; to = t + 1; i = from - 1; }
+        else i = to;
         Group G{};
         G.at.chunk = chunk;
         int64_t chunks = 0;
-        for (int64_t i = from; i < std::min<int64_t>(n_tensors, from + N); ++i) {
+        for (int64_t x = from; x < to; ++x) {
+            const int64_t n = len(x);
+            if (n == 0) continue;
             const int k = G.at.n++;
             G.at.first[k] = (int32_t)chunks;
-            G.at.len[k] = len(i);
-            chunks += gs_ceil_div(len(i), chunk);
-            fill(G, k, i);
+            chunks += gs_ceil_div(n, chunk);
+            G.at.tail[k] = (int32_t)(n - (gs_ceil_div(n, chunk) - 1) * chunk);
+            fill(G, k, x);
         }
         G.at.first[G.at.n] = (int32_t)chunks;
-        launch(G, from == 0);
-    }
+        launch(G, first);
+        first = false;
+    } while (i >= 0 && i < n_tensors);
 }
 
-struct NormPlan { int64_t chunk; int slots; };
+struct Plan { int chunk; int grid; int64_t total, used; };      // grid: of every launch of a call
 
 template <class Len>
-NormPlan plan(int64_t n_tensors, Len len, int per_group) {
-    int64_t total = 0, most = 0;
-    for (int64_t i = 0; i < n_tensors; ++i) total += len(i);
-    NormPlan p{chunk_of(total), 1};
-    int64_t group = 0;
+Plan plan(const gsplit_ctx *ctx, int64_t n_tensors, int per_group, Len len) {
+    Plan p{0, 1, 0, 0};
+    for (int64_t i = 0; i < n_tensors; ++i) { p.total += len(i); p.used += len(i) > 0; }
+    p.chunk = update_chunk(p.total, ctx->n_cu);
+    int64_t most = 1, group = 0, k = 0;
     for (int64_t i = 0; i < n_tensors; ++i) {
-        if (i % per_group == 0) group = 0;
+        if (len(i) == 0) continue;
+        if (k++ % per_group == 0) group = 0;
         group += gs_ceil_div(len(i), p.chunk);
         most = std::max(most, group);
     }
-    p.slots = (int)std::max<int64_t>(1, std::min<int64_t>(GS_NORM_SLOTS, most));
+    p.grid = (int)std::min<int64_t>(std::min<int64_t>(GS_NORM_SLOTS, (int64_t)ctx->n_cu * 8), most);
     return p;
 }
 
+// slots of the squares of all gradients; returns how many
 template <class GradOf>
-void launch_norm(gsplit_ctx *ctx, int64_t n_tensors, const NormPlan &p, GradOf grad, hipStream_t st) {
-    in_groups<NORM_TENSORS, Grads>(
-        n_tensors, p.chunk, [&](int64_t i) { return grad(i).n; },
-        [&](Grads &G, int k, int64_t i) {
-            const gsplit_grad_tensor t = grad(i);
-            G.g[k] = t.d_grad;
-            G.out[k] = t.d_out ? t.d_out : (void *)t.d_grad;
-            if (t.dtype == GSPLIT_BF16) G.half[k >> 5] |= 1u << (k & 31);
+int launch_norm(gsplit_ctx *ctx, int64_t n_tensors, GradOf grad, hipStream_t st) {
+    const auto len = [&](int64_t i) { return grad(i).n; };
+    const Plan p = plan(ctx, n_tensors, NORM_TENSORS, len);
+    in_groups<NORM_TENSORS, Norm>(
+        n_tensors, p.chunk, false, len,
+        [&](Norm &G, int k, int64_t i) {
+            G.g[k] = grad(i).d_grad;
+            if (grad(i).dtype == GSPLIT_BF16) G.half.set(k);
         },
-        [&](const Grads &G, bool first) {
+        [&](const Norm &G, bool first) {
             GsTimeScope ts(ctx, "grad_norm", -1, st);
-            hipLaunchKernelGGL(k_grad_norm, dim3(p.slots), dim3(UT), 0, st, G, ctx->norm_part, !first);
+            hipLaunchKernelGGL(k_grad_norm, dim3(p.grid), dim3(UT), 0, st, G, ctx->norm_part, !first);
         });
+    return p.grid;
 }
 
 }  // namespace
@@ -231,10 +384,9 @@ extern "C" int gsplit_grad_norm(gsplit_ctx *ctx, const gsplit_grad_tensor *t, in
         const char *e = op_check_grads(t, n_tensors, 0.0, false);
         if (!e && (!d_norm || op_misaligned(d_norm, 4))) e = "bad d_norm";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grad_norm: ") + e);
-        const NormPlan p = plan(n_tensors, [&](int64_t i) { return t[i].n; }, NORM_TENSORS);
-        launch_norm(ctx, n_tensors, p, [&](int64_t i) { return t[i]; }, st);
+        const int slots = launch_norm(ctx, n_tensors, [&](int64_t i) { return t[i]; }, st);
         GsTimeScope ts(ctx, "norm_of", -1, st);
-        hipLaunchKernelGGL(k_norm_of, dim3(1), dim3(UT), 0, st, ctx->norm_part, p.slots, d_norm);
+        hipLaunchKernelGGL(k_norm_of, dim3(1), dim3(UT), 0, st, ctx->norm_part, slots, d_norm);
         return GSPLIT_OK;
     });
 }
@@ -247,19 +399,22 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
         const char *e = op_check_grads(t, n_tensors, max_norm, true);
         if (!e && op_misaligned(d_norm, 4)) e = "misaligned buffer";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_clip_grads: ") + e);
-        const NormPlan p = plan(n_tensors, [&](int64_t i) { return t[i].n; }, NORM_TENSORS);
-        launch_norm(ctx, n_tensors, p, [&](int64_t i) { return t[i]; }, st);
-        in_groups<NORM_TENSORS, Grads>(
-            n_tensors, p.chunk, [&](int64_t i) { return t[i].n; },
-            [&](Grads &G, int k, int64_t i) {
+        const auto len = [&](int64_t i) { return t[i].n; };
+        const Plan p = plan(ctx, n_tensors, CLIP_TENSORS, len);
+        const bool small = p.used <= CLIP_TENSORS && update_clip_small(p.total);
+        const int slots = small ? 0 : launch_norm(ctx, n_tensors, [&](int64_t i) { return t[i]; }, st);
+        in_groups<CLIP_TENSORS, Clip>(
+            n_tensors, small ? UPDATE_CLIP_SMALL : p.chunk, true, len,
+            [&](Clip &G, int k, int64_t i) {
                 G.g[k] = t[i].d_grad;
                 G.out[k] = t[i].d_out ? t[i].d_out : (void *)t[i].d_grad;
-                if (t[i].dtype == GSPLIT_BF16) G.half[k >> 5] |= 1u << (k & 31);
+                if (t[i].dtype == GSPLIT_BF16) G.half.set(k);
             },
-            [&](const Grads &G, bool first) {
+            [&](const Clip &G, bool first) {
                 GsTimeScope ts(ctx, "clip_grads", -1, st);
-                hipLaunchKernelGGL(k_clip, dim3(p.slots), dim3(UT), 0, st, G, ctx->norm_part, p.slots, (float)max_norm,
-                                   first ? d_norm : nullptr);
+                float *norm = first ? d_norm : nullptr;
+                if (small) hipLaunchKernelGGL(k_clip_small, dim3(1), dim3(ST), 0, st, G, (float)max_norm, norm);
+                else hipLaunchKernelGGL(k_clip, dim3(p.grid), dim3(UT), 0, st, G, ctx->norm_part, slots, (float)max_norm, norm);
             });
         return GSPLIT_OK;
     });
@@ -274,26 +429,26 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
         if (!e && op_misaligned(d_norm, 4)) e = "misaligned buffer";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_adamw_step: ") + e);
         const auto len = [&](int64_t i) { return t[i].n; };
+        const Plan p = plan(ctx, n_tensors, ADAMW_TENSORS, len);
+        const bool here = p.used <= ADAMW_TENSORS && update_norm_here(p.total);
         int slots = 0;
-        if (c->max_norm > 0.0) {
-            const NormPlan p = plan(n_tensors, len, NORM_TENSORS);
-            launch_norm(ctx, n_tensors, p, [&](int64_t i) {
+        if (c->max_norm > 0.0 && !here)
+            slots = launch_norm(ctx, n_tensors, [&](int64_t i) {
                 return gsplit_grad_tensor{t[i].d_grad, nullptr, t[i].n, t[i].grad_dtype};
             }, st);
-            slots = p.slots;
-        }
-        const NormPlan p = plan(n_tensors, len, ADAMW_TENSORS);
-        const Hyper H{c->lr, c->beta1, c->beta2, c->weight_decay, (float)c->eps, (float)c->max_norm, c->step, c->d_step, c->d_lr};
+        const Hyper H{c->lr, c->beta1, c->beta2, c->weight_decay, c->step, c->d_step, c->d_lr, (float)c->eps, (float)c->max_norm};
+        const Steps S = c->d_step || c->d_lr ? Steps{} : steps_of(H, H.lr, (double)H.step);
         in_groups<ADAMW_TENSORS, Adamw>(
-            n_tensors, p.chunk, len,
+            n_tensors, p.chunk, true, len,
             [&](Adamw &A, int k, int64_t i) {
                 A.p[k] = t[i].d_param; A.master[k] = t[i].d_master; A.g[k] = t[i].d_grad; A.m[k] = t[i].d_m; A.v[k] = t[i].d_v;
-                if (t[i].param_dtype == GSPLIT_BF16) A.half_p[k >> 5] |= 1u << (k & 31);
-                if (t[i].grad_dtype == GSPLIT_BF16) A.half_g[k >> 5] |= 1u << (k & 31);
+                if (t[i].param_dtype == GSPLIT_BF16) A.half_p.set(k);
+                if (t[i].grad_dtype == GSPLIT_BF16) A.half_g.set(k);
             },
             [&](const Adamw &A, bool first) {
                 GsTimeScope ts(ctx, "adamw", -1, st);
-                hipLaunchKernelGGL(k_adamw, dim3(p.slots), dim3(UT), 0, st, A, H, ctx->norm_part, slots, first ? d_norm : nullptr);
+                const auto kernel = c->max_norm == 0.0 ? k_adamw<NORM_NONE> : here ? k_adamw<NORM_HERE> : k_adamw<NORM_SLOTS>;
+                hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(UT), 0, st, A, H, S, ctx->norm_part, slots, first ? d_norm : nullptr);
             });
         return GSPLIT_OK;
     });
