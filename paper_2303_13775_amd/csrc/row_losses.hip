@@ -122,71 +122,132 @@ __device__ __forceinline__ int64_t seq_at(const Pairs &Q, int64_t q, int64_t n_r
     return min(max(Q.seq_ptr[q], (int64_t)0), n_rows);
 }
 
-template <class T, int THREADS, int LANES, int E>
-__global__ __launch_bounds__(THREADS) void k_preference_rows(Rows R, Pairs Q) {
-    constexpr bool WG = LANES > 64;
-    __shared__ RowStats lds[WG ? THREADS / 64 : 1];
-    const int lane = WG ? threadIdx.x : threadIdx.x % LANES;
-    constexpr int TEAMS = THREADS / LANES;
-    const int64_t first = seq_at(Q, 0, R.n), last = seq_at(Q, 2 * Q.n, R.n);
-    for (int64_t r = first + (int64_t)blockIdx.x * TEAMS + (WG ? 0 : threadIdx.x / LANES); r < last; r += (int64_t)gridDim.x * TEAMS) {
-        const T *z = (const T *)R.logits + r * R.ld;
+// Statistics and log p of row r into its place in the working memory, by a team of LANES lanes; returns log p (0: left out)
+template <class T, int LANES, int E>
+__device__ __forceinline__ double preference_row(const Rows &R, const Pairs &Q, int64_t r, int lane, RowStats *lds) {
+    const T *z = (const T *)R.logits + r * R.ld;
+    const int64_t a = R.actions[r];
+    RowStats st{-INFINITY, 0.f};
+    float za = 0.f;
+    if (a >= 0 && a < R.C) {
+        za = (float)z[a];
+        st = StreamedRow<T, LANES, E>::stats(z, R.C, lane);
+        if constexpr (LANES > 64) { st = join_waves<LANES>(st, lds); __syncthreads(); }
+        else st = join_lanes<LANES>(st);
+    }
+    const double logp = st.s != 0.f ? row_logp(st, za) : 0.0;
+    if (lane == 0) {
+        const float2 bits = __builtin_bit_cast(float2, logp);
+        Q.work[r] = {st.m, st.s, bits.x, bits.y};
+        if (Q.row_logp) Q.row_logp[r] = (float)logp;
+    }
+    return logp;
+}
+template <class T, int LANES, int E>
+__device__ __forceinline__ void preference_row_grad(const Rows &R, int64_t r, int lane, RowStats st, float slope) {
+    const T *z = (const T *)R.logits + r * R.ld;
+    T *g = (T *)R.grad + r * R.gld;
+    if (slope == 0.f) store_zeros<T, LANES>(g, R.C, lane);
+    else {
         const int64_t a = R.actions[r];
-        RowStats st{-INFINITY, 0.f};
-        float za = 0.f;
-        if (a >= 0 && a < R.C) {
-            za = (float)z[a];
-            st = StreamedRow<T, LANES, E>::stats(z, R.C, lane);
-            if constexpr (WG) { st = join_waves<LANES>(st, lds); __syncthreads(); }
-            else st = join_lanes<LANES>(st);
-        }
-        if (lane == 0) {
-            const double logp = st.s != 0.f ? row_logp(st, za) : 0.0;
-            const float2 bits = __builtin_bit_cast(float2, logp);
-            Q.work[r] = {st.m, st.s, bits.x, bits.y};
-            if (Q.row_logp) Q.row_logp[r] = (float)logp;
-        }
+        StreamedRow<T, LANES, E>::store(z, g, R.C, lane, st, slope, (int)a, (float)z[a]);
     }
 }
 
-constexpr int PT = 256;
+// Writes loss and margin of a pair from the difference of its log ratios (first thread), returns d loss / d log p of its chosen rows
+__device__ __forceinline__ float pair_row(const Pairs &Q, int64_t p, double ratio_gap) {
+    const double h = (double)Q.beta * ratio_gap, e = Q.smoothing;
+    const double w = Q.weight ? Q.weight[p] : Q.even_weight;
+    if (threadIdx.x == 0) {
+        const double soft = log1p(exp(-fabs(h)));
+        if (Q.margin) Q.margin[p] = (float)h;
+        if (Q.loss) Q.loss[p] = w == 0.0 ? 0.f : (float)(w * ((1.0 - e) * (soft + fmax(-h, 0.0)) + e * (soft + fmax(h, 0.0))));
+    }
+    // d loss / d margin = w (e - sigmoid(-margin))
+    return w == 0.0 ? 0.f : (float)((double)Q.beta * w * (e - 1.0 / (1.0 + exp(h))));
+}
+__device__ __forceinline__ double reference_gap(const Pairs &Q, int64_t p) {
+    return Q.ref_logp ? (double)Q.ref_logp[2 * p] - (double)Q.ref_logp[2 * p + 1] : 0.0;
+}
 
+// the rows of a pair, the chosen sequence's and then the rejected one's
+struct PairRows {
+    int64_t b0, n0, b1, n;
+    __device__ __forceinline__ PairRows(const Pairs &Q, int64_t p, int64_t n_rows) {
+        b0 = seq_at(Q, 2 * p, n_rows);
+        b1 = seq_at(Q, 2 * p + 1, n_rows);
+        n0 = max(b1 - b0, (int64_t)0);
+        n = n0 + max(seq_at(Q, 2 * p + 2, n_rows) - b1, (int64_t)0);
+    }
+    __device__ __forceinline__ int64_t row(int64_t i) const { return i < n0 ? b0 + i : b1 + (i - n0); }
+};
+
+template <int THREADS>
 __device__ __forceinline__ double wg_sum(double x, double *lds) {
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = lds[0];
-    for (int w = 1; w < PT / 64; ++w) x += lds[w];
-    __syncthreads();
+    if constexpr (THREADS > 64) {
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = lds[0];
+        for (int w = 1; w < THREADS / 64; ++w) x += lds[w];
+        __syncthreads();
+    }
     return x;
 }
 
+// A pair from its rows' statistics to their gradient by one workgroup, THREADS / LANES rows at a time; the second reading of the
+// rows comes from the caches.
+template <class T, int THREADS, int LANES, int E>
+__global__ __launch_bounds__(THREADS) void k_preference_whole(Rows R, Pairs Q) {
+    __shared__ RowStats lds[LANES > 64 ? THREADS / 64 : 1];
+    __shared__ double lds_sum[THREADS / 64];
+    constexpr int TEAMS = THREADS / LANES;
+    const int lane = LANES > 64 ? threadIdx.x : threadIdx.x % LANES, team = LANES > 64 ? 0 : threadIdx.x / LANES;
+    const PairRows P(Q, blockIdx.x, R.n);
+    double gap = 0.0;
+    for (int64_t i = team; i < P.n; i += TEAMS) {
+        const double logp = preference_row<T, LANES, E>(R, Q, P.row(i), lane, lds);
+        if (lane == 0) gap += i < P.n0 ? logp : -logp;
+    }
+    gap = wg_sum<THREADS>(gap, lds_sum) - reference_gap(Q, blockIdx.x);
+    const float slope = pair_row(Q, blockIdx.x, gap);
+    if (!R.grad) return;
+    __syncthreads();        // (the working memory of a row is written by its team's first lane)
+    for (int64_t i = team; i < P.n; i += TEAMS) {
+        const int64_t r = P.row(i);
+        const float4 k = Q.work[r];
+        preference_row_grad<T, LANES, E>(R, r, lane, {k.x, k.y}, k.y == 0.f ? 0.f : i < P.n0 ? slope : -slope);
+    }
+}
+
+// The same as three launches, for pairs too few or too long for a workgroup each: all rows, all pairs, all rows again
+template <class T, int THREADS, int LANES, int E>
+__global__ __launch_bounds__(THREADS) void k_preference_rows(Rows R, Pairs Q) {
+    __shared__ RowStats lds[LANES > 64 ? THREADS / 64 : 1];
+    constexpr int TEAMS = THREADS / LANES;
+    const int64_t first = seq_at(Q, 0, R.n), last = seq_at(Q, 2 * Q.n, R.n);
+    for (int64_t r = first + (int64_t)blockIdx.x * TEAMS + (LANES > 64 ? 0 : threadIdx.x / LANES); r < last; r += (int64_t)gridDim.x * TEAMS)
+        preference_row<T, LANES, E>(R, Q, r, threadIdx.x % LANES, lds);
+}
+
+constexpr int PT = 256;
 __global__ __launch_bounds__(PT) void k_preference_pairs(Rows R, Pairs Q) {
     __shared__ double lds[PT / 64];
     for (int64_t p = blockIdx.x; p < Q.n; p += gridDim.x) {
-        double sum[2];
-        for (int k = 0; k < 2; ++k) {
-            double x = 0.0;
-            const int64_t end = seq_at(Q, 2 * p + k + 1, R.n);
-            for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += PT)
-                x += __builtin_bit_cast(double, make_float2(Q.work[r].z, Q.work[r].w));
-            sum[k] = wg_sum(x, lds) - (Q.ref_logp ? (double)Q.ref_logp[2 * p + k] : 0.0);
+        const PairRows P(Q, p, R.n);
+        double gap = 0.0;
+        for (int64_t i = threadIdx.x; i < P.n; i += PT) {
+            const float4 k = Q.work[P.row(i)];
+            const double logp = __builtin_bit_cast(double, make_float2(k.z, k.w));
+            gap += i < P.n0 ? logp : -logp;
         }
-        const double h = (double)Q.beta * (sum[0] - sum[1]), e = Q.smoothing;
-        const double w = Q.weight ? Q.weight[p] : Q.even_weight;
-        const double soft = log1p(exp(-fabs(h)));
-        if (threadIdx.x == 0) {
-            if (Q.margin) Q.margin[p] = (float)h;
-            if (Q.loss) Q.loss[p] = w == 0.0 ? 0.f : (float)(w * ((1.0 - e) * (soft + fmax(-h, 0.0)) + e * (soft + fmax(h, 0.0))));
+        gap = wg_sum<PT>(gap, lds) - reference_gap(Q, p);
+        const float slope = pair_row(Q, p, gap);
+        if (!R.grad) continue;
+        for (int64_t i = threadIdx.x; i < P.n; i += PT) {
+            float4 &k = Q.work[P.row(i)];
+            k.z = k.y == 0.f ? 0.f : i < P.n0 ? slope : -slope;
         }
-        // d loss / d margin = w (e - sigmoid(-margin))
-        const float slope = w == 0.0 ? 0.f : (float)((double)Q.beta * w * (e - 1.0 / (1.0 + exp(h))));
-        if (R.grad)
-            for (int k = 0; k < 2; ++k) {
-                const int64_t end = seq_at(Q, 2 * p + k + 1, R.n);
-                for (int64_t r = seq_at(Q, 2 * p + k, R.n) + threadIdx.x; r < end; r += PT)
-                    Q.work[r].z = Q.work[r].y == 0.f ? 0.f : k ? -slope : slope;
-            }
     }
 }
 
@@ -198,13 +259,7 @@ __global__ __launch_bounds__(THREADS) void k_preference_grad(Rows R, Pairs Q) {
     // the last rows first: they are the ones that the pass before has left in the caches
     for (int64_t r = last - 1 - (int64_t)blockIdx.x * TEAMS - (LANES > 64 ? 0 : threadIdx.x / LANES); r >= first; r -= (int64_t)gridDim.x * TEAMS) {
         const float4 k = Q.work[r];
-        const T *z = (const T *)R.logits + r * R.ld;
-        T *g = (T *)R.grad + r * R.gld;
-        if (k.z == 0.f) store_zeros<T, LANES>(g, R.C, lane);
-        else {
-            const int64_t a = R.actions[r];
-            StreamedRow<T, LANES, E>::store(z, g, R.C, lane, {k.x, k.y}, k.z, (int)a, (float)z[a]);
-        }
+        preference_row_grad<T, LANES, E>(R, r, lane, {k.x, k.y}, k.z);
     }
 }
 
@@ -230,11 +285,13 @@ void with_form(int form, F f) {
     }
 }
 
-// the same for kernels that stream rows: 16, 64 or 256 lanes a row
+// the same for kernels that stream rows: 16, 64 or 256 lanes a row, in workgroups of 64 or 256 threads
 template <class F>
-void with_part(int dtype, int lanes, F f) {
+void with_part(int dtype, int lanes, int threads, F f) {
     const auto typed = [&](auto type) {
-        if (lanes == 16) f(type, Int<256>{}, Int<16>{}, Int<16>{});
+        if (lanes == 16 && threads == 64) f(type, Int<64>{}, Int<16>{}, Int<16>{});
+        else if (lanes == 16) f(type, Int<256>{}, Int<16>{}, Int<16>{});
+        else if (lanes == 64 && threads == 64) f(type, Int<64>{}, Int<64>{}, Int<16>{});
         else if (lanes == 64) f(type, Int<256>{}, Int<64>{}, Int<16>{});
         else f(type, Int<256>{}, Int<256>{}, Int<32>{});
     };
@@ -294,9 +351,19 @@ extern "C" int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
         const Pairs Q{d_seq_ptr, n_pairs, d_ref_logp, d_pair_weight, d_row_logp, d_pair_loss, d_pair_margin,
                       (float4 *)d_row_work, c->beta, c->label_smoothing, (float)(1.0 / (double)n_pairs)};
         const int64_t most = (int64_t)ctx->n_cu * 32;
+        const int whole = n_rows > 0 ? preference_whole(n_rows, n_pairs, (int64_t)n_classes * op_elem_size(c->dtype), ctx->n_cu) : 0;
+        if (whole) {
+            GsTimeScope ts(ctx, "preference_loss", -1, st);
+            with_part(c->dtype, row_part(n_classes), whole, [&](auto type, auto threads, auto lanes, auto e) {
+                using T = decltype(type);
+                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
+                hipLaunchKernelGGL((k_preference_whole<T, TH, LA, E>), dim3((unsigned)n_pairs), dim3(TH), 0, st, R, Q);
+            });
+            return GSPLIT_OK;
+        }
         if (n_rows > 0) {
             GsTimeScope ts(ctx, "preference_rows", -1, st);
-            with_part(c->dtype, row_part(n_classes), [&](auto type, auto threads, auto lanes, auto e) {
+            with_part(c->dtype, row_part(n_classes), 256, [&](auto type, auto threads, auto lanes, auto e) {
                 using T = decltype(type);
                 constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
                 hipLaunchKernelGGL((k_preference_rows<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);
@@ -308,7 +375,7 @@ extern "C" int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
         }
         if (n_rows > 0 && d_grad_logits) {
             GsTimeScope ts(ctx, "preference_grad", -1, st);
-            with_part(c->dtype, row_part(n_classes), [&](auto type, auto threads, auto lanes, auto e) {
+            with_part(c->dtype, row_part(n_classes), 256, [&](auto type, auto threads, auto lanes, auto e) {
                 using T = decltype(type);
                 constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
                 hipLaunchKernelGGL((k_preference_grad<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);

@@ -62,9 +62,6 @@ static_assert(sizeof(Norm) <= 4096 - 128 && sizeof(Clip) <= 4096 - 128 && sizeof
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
-// read again by the pass that uses the norm: not past the caches
-__device__ __forceinline__ u32x4 load_kept(const void *p) { return *(const u32x4_any *)p; }
-
 // Squares are formed and summed in double, which holds those of every float: neither 1e30 nor 1e-30 leaves its range, and the norm
 // is the float next to the exact one.  (A conversion and a double multiply-add an element: a fifth of what the chip could do in
 // the time the elements take to come.)
@@ -76,21 +73,22 @@ __device__ __forceinline__ double squares(u32x4 q, double s) {
     for (int k = 0; k < PIECE<T>; ++k) s = fma((double)x[k], (double)x[k], s);
     return s;
 }
-template <class T, int THREADS>
-__device__ __forceinline__ double sum_of_squares(const T *g, int n) {
+// (a team of LANES lanes: a wave or the workgroup)
+template <class T, int LANES>
+__device__ __forceinline__ double sum_of_squares(const T *g, int n, int lane) {
     constexpr int V = PIECE<T>, DEEP = 4;       // pieces a thread has in flight
     const int nv = n / V;
     double s = 0.0;
-    int j = threadIdx.x;
-    for (; j + (DEEP - 1) * THREADS < nv; j += DEEP * THREADS) {
+    int j = lane;
+    for (; j + (DEEP - 1) * LANES < nv; j += DEEP * LANES) {
         u32x4 q[DEEP];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) q[i] = load_kept(g + (j + i * THREADS) * V);
+        for (int i = 0; i < DEEP; ++i) q[i] = load_kept(g + (j + i * LANES) * V);
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) s = squares<T>(q[i], s);
     }
-    for (; j < nv; j += THREADS) s = squares<T>(load_kept(g + j * V), s);
-    if ((int)threadIdx.x < n - nv * V) { const double x = (float)g[nv * V + threadIdx.x]; s = fma(x, x, s); }
+    for (; j < nv; j += LANES) s = squares<T>(load_kept(g + j * V), s);
+    if (lane < n - nv * V) { const double x = (float)g[nv * V + lane]; s = fma(x, x, s); }
     return s;
 }
 
@@ -104,18 +102,21 @@ __device__ __forceinline__ double wg_sum(double x, double *lds) {
     return x;
 }
 
-// this workgroup's share of all squares, as one of `of` workgroups
-template <int THREADS, class Table, class Half>
+// a team's share of all squares, as one of `of` teams
+template <int LANES, class Table, class Half>
 __device__ __forceinline__ double share_of_squares(const Table &G, const Half &half, int which, int of) {
+    const int lane = (int)threadIdx.x % LANES;
     double s = 0.0;
     for (int c = which; c < G.at.count(); c += of) {
         const int t = G.at.tensor_of(c);
         const int64_t at = G.at.start(c, t);
-        s += half[t] ? sum_of_squares<bf16, THREADS>((const bf16 *)G.g[t] + at, G.at.len(c, t))
-                     : sum_of_squares<float, THREADS>((const float *)G.g[t] + at, G.at.len(c, t));
+        s += half[t] ? sum_of_squares<bf16, LANES>((const bf16 *)G.g[t] + at, G.at.len(c, t), lane)
+                     : sum_of_squares<float, LANES>((const float *)G.g[t] + at, G.at.len(c, t), lane);
     }
     return s;
 }
+// the wave's number, the same in all its lanes as far as the compiler can see
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
 constexpr int UT = 256;
 
@@ -154,31 +155,32 @@ __device__ __forceinline__ u32x4 scaled(u32x4 q, float f) {
     for (int k = 0; k < PIECE<T>; ++k) x[k] *= f;
     return pack<T>(x);
 }
-template <class T, int THREADS>
-__device__ __forceinline__ void scale_run(const T *g, T *out, int n, float f) {
+template <class T, int LANES>
+__device__ __forceinline__ void scale_run(const T *g, T *out, int n, float f, int lane) {
     constexpr int V = PIECE<T>, DEEP = 4;
     const int nv = n / V;
-    int j = threadIdx.x;
-    for (; j + (DEEP - 1) * THREADS < nv; j += DEEP * THREADS) {
+    int j = lane;
+    for (; j + (DEEP - 1) * LANES < nv; j += DEEP * LANES) {
         u32x4 q[DEEP];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) q[i] = load_piece(g + (j + i * THREADS) * V);
+        for (int i = 0; i < DEEP; ++i) q[i] = load_piece(g + (j + i * LANES) * V);
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) store_piece(out + (j + i * THREADS) * V, scaled<T>(q[i], f));
+        for (int i = 0; i < DEEP; ++i) store_piece(out + (j + i * LANES) * V, scaled<T>(q[i], f));
     }
-    for (; j < nv; j += THREADS) store_piece(out + j * V, scaled<T>(load_piece(g + j * V), f));
-    if ((int)threadIdx.x < n - nv * V) out[nv * V + threadIdx.x] = (T)((float)g[nv * V + threadIdx.x] * f);
+    for (; j < nv; j += LANES) store_piece(out + j * V, scaled<T>(load_piece(g + j * V), f));
+    if (lane < n - nv * V) out[nv * V + lane] = (T)((float)g[nv * V + lane] * f);
 }
 
-template <int THREADS>
+template <int LANES>
 __device__ __forceinline__ void scale_chunks(const Clip &G, float f, int which, int of) {
+    const int lane = (int)threadIdx.x % LANES;
     // the last chunks first: the norm's pass has left them in the caches
     for (int c = G.at.count() - 1 - which; c >= 0; c -= of) {
         const int t = G.at.tensor_of(c);
         if (f == 1.f && G.out[t] == G.g[t]) continue;
         const int64_t at = G.at.start(c, t);
-        if (G.half[t]) scale_run<bf16, THREADS>((const bf16 *)G.g[t] + at, (bf16 *)G.out[t] + at, G.at.len(c, t), f);
-        else scale_run<float, THREADS>((const float *)G.g[t] + at, (float *)G.out[t] + at, G.at.len(c, t), f);
+        if (G.half[t]) scale_run<bf16, LANES>((const bf16 *)G.g[t] + at, (bf16 *)G.out[t] + at, G.at.len(c, t), f, lane);
+        else scale_run<float, LANES>((const float *)G.g[t] + at, (float *)G.out[t] + at, G.at.len(c, t), f, lane);
     }
 }
 
@@ -190,13 +192,15 @@ __global__ __launch_bounds__(UT) void k_clip(Clip G, const double *__restrict__ 
     scale_chunks<UT>(G, factor_of(norm, max_norm), blockIdx.x, gridDim.x);
 }
 
-// Norm and clipping of few elements by one workgroup (several could not clip in place: one would scale what another still adds up)
+// Norm and clipping of few elements by one workgroup (several could not clip in place: one would scale what another still adds up),
+// a chunk a wave: taken by the whole workgroup one after the other, the six tensors of 64-64-16 were twelve trips to memory in a
+// row, 10.9 us.
 constexpr int ST = 1024;
 __global__ __launch_bounds__(ST) void k_clip_small(Clip G, float max_norm, float *__restrict__ norm_out) {
     __shared__ double lds[ST / 64];
-    const float norm = (float)sqrt(wg_sum<ST>(share_of_squares<ST>(G, G.half, 0, 1), lds));
+    const float norm = (float)sqrt(wg_sum<ST>(share_of_squares<64>(G, G.half, wave_id(), ST / 64), lds));
     if (norm_out && threadIdx.x == 0) *norm_out = norm;
-    scale_chunks<ST>(G, factor_of(norm, max_norm), 0, 1);
+    scale_chunks<64>(G, factor_of(norm, max_norm), wave_id(), ST / 64);
 }
 
 // -- the update -------------------------------------------------------------------------------
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, Steps S, const d
     if constexpr (WHENCE != NORM_NONE) {
         float norm;
         if constexpr (WHENCE == NORM_SLOTS) norm = norm_of<UT>(slots, n_slots, lds);
-        else norm = (float)sqrt(wg_sum<UT>(share_of_squares<UT>(A, A.half_g, 0, 1), lds));
+        else norm = (float)sqrt(wg_sum<UT>(share_of_squares<64>(A, A.half_g, wave_id(), UT / 64), lds));
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
         if (!is_finite(norm)) return;
         S.f = factor_of(norm, H.max_norm);
@@ -404,7 +408,7 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
         const bool small = p.used <= CLIP_TENSORS && update_clip_small(p.total);
         const int slots = small ? 0 : launch_norm(ctx, n_tensors, [&](int64_t i) { return t[i]; }, st);
         in_groups<CLIP_TENSORS, Clip>(
-            n_tensors, small ? UPDATE_CLIP_SMALL : p.chunk, true, len,
+            n_tensors, p.chunk, true, len,
             [&](Clip &G, int k, int64_t i) {
                 G.g[k] = t[i].d_grad;
                 G.out[k] = t[i].d_out ? t[i].d_out : (void *)t[i].d_grad;
