@@ -18,7 +18,7 @@
 // launches, which cuts the dependent random accesses per slot from three to one
 #define GS_WIDE_SLOTS (1ll << 20)
 #define GS_MAXL GSPLIT_MAX_LAYERS
-#define GS_NORM_SLOTS 2048
+#define GS_NORM_SLOTS 1024
 
 // Device-resident bookkeeping of one level l (0..L) of the current batch.  Every kernel reads its
 // problem sizes from here, so a whole iteration is enqueued without a host round trip.
@@ -226,6 +226,7 @@ struct gsplit_ctx {
     std::shared_ptr<GsEvent> sample_done;   // the one that stands behind its current batch: its own, or that of a grouped call
 
     double      *norm_part = nullptr;       // [GS_NORM_SLOTS] a workgroup's sum of squares each (gradient norm)
+    void        *row_part = nullptr;        // statistics of parts of rows (losses over few wide rows)
 
     GsSageBuf    sage;
     GsGatBuf     gat;

@@ -11,6 +11,8 @@
 
 namespace {
 
+enum : int { HELD, RAW, STREAMED };
+
 struct Rows {
     const void *logits; int64_t ld;
     void *grad; int64_t gld;
@@ -27,7 +29,7 @@ struct Policy {
 };
 
 // log p of a row from its statistics and its action's logit, in double: a KL term is a difference of nearly equal numbers
-__device__ __forceinline__ double row_logp(RowStats st, float za) { return ((double)za - (double)base_of(st.m)) - log((double)st.s); }
+__device__ __forceinline__ double row_logp(RowStats st, float za) { return ((double)za - (double)base_of(st.m)) - log(st.s); }
 
 // e^x - 1 - x without the cancellation near 0: its series up to |x| = 1 (the first term left out is 4e-9 of the value)
 __device__ __forceinline__ float exp_above_tangent(float x) {
@@ -58,10 +60,11 @@ __device__ __forceinline__ float policy_row(const Policy &P, double logp, float 
 
 // Lanes LANES of a team take a row each time.  LANES <= 64: several teams a wave, all lanes form the row's numbers alike; else the
 // team is the workgroup, and its first wave does.
-template <class T, int THREADS, int LANES, int E>
+template <class T, int THREADS, int LANES, int E, int WAYS>
 __global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
     constexpr bool WG = LANES > 64;
-    constexpr bool HELD = E > 0;
+    constexpr bool IN_REGS = WAYS != STREAMED;
+    using Row = std::conditional_t<WAYS == RAW, RawRow<T, LANES, E>, HeldRow<T, LANES, E>>;
     __shared__ RowStats lds[WG ? THREADS / 64 : 1];
     __shared__ float lds_slope;
     const int lane = WG ? threadIdx.x : threadIdx.x % LANES;
@@ -73,19 +76,19 @@ __global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
         T *g = R.grad ? (T *)R.grad + r * R.gld : nullptr;
         const float w = P.weight ? P.weight[r] : P.even_weight;
         const int64_t a = R.actions[r];
-        RowStats st{-INFINITY, 0.f};
+        RowStats st{-INFINITY, 0.0};
         float za = 0.f, slope = 0.f;
-        HeldRow<T, LANES, HELD ? E : PIECE<T>> row;
+        Row row;
         if (w != 0.f && a >= 0 && a < R.C) {
             za = (float)z[a];
-            if constexpr (HELD) { row.load(z, R.C, lane); st = row.stats(); }
-            else st = StreamedRow<T, LANES, -E>::stats(z, R.C, lane);
+            if constexpr (IN_REGS) { row.load(z, R.C, lane); st = row.stats(); }
+            else st = StreamedRow<T, LANES, E>::stats(z, R.C, lane);
             if constexpr (WG) st = join_waves<LANES>(st, lds);
             else st = join_lanes<LANES>(st);
         }
         if (!WG || threadIdx.x < 64) {
             float loss = 0.f, kl = 0.f, logp = 0.f;
-            if (st.s != 0.f) {      // 0: the row is left out
+            if (st.s != 0.0) {      // 0: the row is left out
                 const double lp = row_logp(st, za);
                 logp = (float)lp;
                 slope = policy_row(P, lp, P.old_logp[r], P.ref_logp ? P.ref_logp[r] : 0.f, P.advantage[r], w, &loss, &kl);
@@ -103,10 +106,79 @@ __global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
         }
         if (g) {
             if (slope == 0.f) store_zeros<T, LANES>(g, R.C, lane);      // nothing moves it
-            else if constexpr (HELD) row.store(g, R.C, lane, st, slope, (int)a, za);
-            else StreamedRow<T, LANES, -E>::store(z, g, R.C, lane, st, slope, (int)a, za);
+            else if constexpr (IN_REGS) row.store(g, R.C, lane, st, slope, (int)a, za);
+            else StreamedRow<T, LANES, E>::store(z, g, R.C, lane, st, slope, (int)a, za);
         }
     }
+}
+
+// Few rows of many classes: every row in `chunks` parts (at most 64) of `len` elements, a workgroup each.  One launch leaves the parts'
+// statistics and the action's logit, which the next one might otherwise have overwritten when it reads it; the next joins them.
+struct Parts {
+    RowStats *st;       // [rows x chunks]
+    float *za;          // [rows]
+    int chunks, len;
+    __device__ __forceinline__ int from() const { return (int)blockIdx.x * len; }
+    __device__ __forceinline__ int size(int C) const { return min(len, C - from()); }
+    // the statistics of row y of the launch: in all lanes of a wave, or by one thread
+    __device__ __forceinline__ RowStats joined(int64_t y) const {
+        const int lane = threadIdx.x & 63;
+        return join_lanes<64>(lane < chunks ? st[y * chunks + lane] : RowStats{-INFINITY, 0.0});
+    }
+    __device__ __forceinline__ RowStats joined_alone(int64_t y) const {
+        const RowStats *p = st + y * chunks;
+        float m = -INFINITY;
+        double s = 0.0;
+        for (int k = 0; k < chunks; ++k) m = fmaxf(m, p[k].m);
+        for (int k = 0; k < chunks; ++k) s += p[k].s * (double)share(p[k].m, base_of(m));
+        return {m, s};
+    }
+};
+constexpr int CT = 256, CE = 32;
+
+template <class T>
+__device__ __forceinline__ void part_stats(const Rows &R, const Parts &S, int64_t r, RowStats *lds) {
+    const int64_t a = R.actions[r];
+    if (a < 0 || a >= R.C) return;
+    const T *z = (const T *)R.logits + r * R.ld;
+    const RowStats st = join_waves<CT>(StreamedRow<T, CT, CE>::stats(z + S.from(), S.size(R.C), threadIdx.x), lds);
+    if (threadIdx.x == 0) {
+        S.st[(int64_t)blockIdx.y * S.chunks + blockIdx.x] = st;
+        if (blockIdx.x == 0) S.za[blockIdx.y] = (float)z[a];
+    }
+}
+template <class T>
+__device__ __forceinline__ void part_gradient(const Rows &R, const Parts &S, int64_t r, RowStats st, float slope) {
+    const T *z = (const T *)R.logits + r * R.ld + S.from();
+    T *g = (T *)R.grad + r * R.gld + S.from();
+    if (slope == 0.f) store_zeros<T, CT>(g, S.size(R.C), threadIdx.x);
+    else StreamedRow<T, CT, CE>::store(z, g, S.size(R.C), threadIdx.x, st, slope, (int)R.actions[r] - S.from(), S.za[blockIdx.y]);
+}
+
+template <class T>
+__global__ __launch_bounds__(CT) void k_policy_part_stats(Rows R, Policy P, Parts S) {
+    __shared__ RowStats lds[CT / 64];
+    const int64_t r = blockIdx.y;
+    if ((P.weight ? P.weight[r] : P.even_weight) != 0.f) part_stats<T>(R, S, r, lds);
+}
+template <class T>
+__global__ __launch_bounds__(CT) void k_policy_parts(Rows R, Policy P, Parts S) {
+    const int64_t r = blockIdx.y, a = R.actions[r];
+    const float w = P.weight ? P.weight[r] : P.even_weight;
+    RowStats st{-INFINITY, 0.0};
+    float loss = 0.f, kl = 0.f, logp = 0.f, slope = 0.f;
+    if (w != 0.f && a >= 0 && a < R.C) st = S.joined(r);
+    if (st.s != 0.0) {
+        const double lp = row_logp(st, S.za[r]);
+        logp = (float)lp;
+        slope = policy_row(P, lp, P.old_logp[r], P.ref_logp ? P.ref_logp[r] : 0.f, P.advantage[r], w, &loss, &kl);
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (P.loss) P.loss[r] = loss;
+        if (P.logp) P.logp[r] = logp;
+        if (P.kl) P.kl[r] = kl;
+    }
+    if (R.grad) part_gradient<T>(R, S, r, st, slope);
 }
 
 struct Pairs {
@@ -127,7 +199,7 @@ template <class T, int LANES, int E>
 __device__ __forceinline__ double preference_row(const Rows &R, const Pairs &Q, int64_t r, int lane, RowStats *lds) {
     const T *z = (const T *)R.logits + r * R.ld;
     const int64_t a = R.actions[r];
-    RowStats st{-INFINITY, 0.f};
+    RowStats st{-INFINITY, 0.0};
     float za = 0.f;
     if (a >= 0 && a < R.C) {
         za = (float)z[a];
@@ -135,10 +207,10 @@ __device__ __forceinline__ double preference_row(const Rows &R, const Pairs &Q, 
         if constexpr (LANES > 64) { st = join_waves<LANES>(st, lds); __syncthreads(); }
         else st = join_lanes<LANES>(st);
     }
-    const double logp = st.s != 0.f ? row_logp(st, za) : 0.0;
+    const double logp = st.s != 0.0 ? row_logp(st, za) : 0.0;
     if (lane == 0) {
         const float2 bits = __builtin_bit_cast(float2, logp);
-        Q.work[r] = {st.m, st.s, bits.x, bits.y};
+        Q.work[r] = {st.m, (float)st.s, bits.x, bits.y};
         if (Q.row_logp) Q.row_logp[r] = (float)logp;
     }
     return logp;
@@ -231,14 +303,27 @@ __global__ __launch_bounds__(THREADS) void k_preference_rows(Rows R, Pairs Q) {
 }
 
 constexpr int PT = 256;
-__global__ __launch_bounds__(PT) void k_preference_pairs(Rows R, Pairs Q) {
+// (S.chunks > 0: the rows come in parts, a thread joins those of a row)
+__global__ __launch_bounds__(PT) void k_preference_pairs(Rows R, Pairs Q, Parts S) {
     __shared__ double lds[PT / 64];
+    const int64_t first = seq_at(Q, 0, R.n);
     for (int64_t p = blockIdx.x; p < Q.n; p += gridDim.x) {
         const PairRows P(Q, p, R.n);
         double gap = 0.0;
         for (int64_t i = threadIdx.x; i < P.n; i += PT) {
-            const float4 k = Q.work[P.row(i)];
-            const double logp = __builtin_bit_cast(double, make_float2(k.z, k.w));
+            const int64_t r = P.row(i);
+            double logp;
+            if (S.chunks) {
+                const int64_t a = R.actions[r], y = r - first;
+                RowStats st{-INFINITY, 0.0};
+                if (a >= 0 && a < R.C && y >= 0) st = S.joined_alone(y);
+                logp = st.s != 0.0 ? row_logp(st, S.za[y]) : 0.0;
+                Q.work[r] = {st.m, (float)st.s, 0.f, 0.f};
+                if (Q.row_logp) Q.row_logp[r] = (float)logp;
+            } else {
+                const float4 k = Q.work[r];
+                logp = __builtin_bit_cast(double, make_float2(k.z, k.w));
+            }
             gap += i < P.n0 ? logp : -logp;
         }
         gap = wg_sum<PT>(gap, lds) - reference_gap(Q, p);
@@ -263,49 +348,88 @@ __global__ __launch_bounds__(THREADS) void k_preference_grad(Rows R, Pairs Q) {
     }
 }
 
+template <class T>
+__global__ __launch_bounds__(CT) void k_preference_part_stats(Rows R, Pairs Q, Parts S) {
+    __shared__ RowStats lds[CT / 64];
+    const int64_t r = seq_at(Q, 0, R.n) + blockIdx.y;
+    if (r < seq_at(Q, 2 * Q.n, R.n)) part_stats<T>(R, S, r, lds);
+}
+template <class T>
+__global__ __launch_bounds__(CT) void k_preference_parts(Rows R, Pairs Q, Parts S) {
+    const int64_t r = seq_at(Q, 0, R.n) + blockIdx.y;
+    if (r >= seq_at(Q, 2 * Q.n, R.n)) return;
+    const float4 k = Q.work[r];
+    part_gradient<T>(R, S, r, {k.x, k.y}, k.z);
+}
+
 unsigned row_grid(int64_t n, int teams, int64_t most) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, gs_ceil_div(n, teams))); }
 
 template <int N> struct Int { static constexpr int value = N; };
 
-// calls f(threads, lanes, elements a lane) with the constants of the form; -elements: streamed
-template <class F>
+// calls f(threads, lanes, elements a lane, way) with the constants of the form
+template <class T, class F>
 void with_form(int form, F f) {
+    const auto go = [&](auto threads, auto lanes, auto e) { f(threads, lanes, e, Int<HELD>{}); };
     switch (form) {
-        case ROW_16x8: f(Int<256>{}, Int<16>{}, Int<8>{}); break;
-        case ROW_16x16: f(Int<256>{}, Int<16>{}, Int<16>{}); break;
-        case ROW_64x8: f(Int<256>{}, Int<64>{}, Int<8>{}); break;
-        case ROW_64x16: f(Int<256>{}, Int<64>{}, Int<16>{}); break;
-        case ROW_256x8: f(Int<256>{}, Int<256>{}, Int<8>{}); break;
-        case ROW_256x16: f(Int<256>{}, Int<256>{}, Int<16>{}); break;
-        case ROW_256x32: f(Int<256>{}, Int<256>{}, Int<32>{}); break;
-        case ROW_512x32: f(Int<512>{}, Int<512>{}, Int<32>{}); break;
-        case ROW_512x64: f(Int<512>{}, Int<512>{}, Int<64>{}); break;
-        case ROW_1024x64: f(Int<1024>{}, Int<1024>{}, Int<64>{}); break;
-        default: f(Int<1024>{}, Int<1024>{}, Int<-32>{}); break;
+        case ROW_16x8: go(Int<256>{}, Int<16>{}, Int<8>{}); break;
+        case ROW_16x16: go(Int<256>{}, Int<16>{}, Int<16>{}); break;
+        case ROW_16x32: go(Int<256>{}, Int<16>{}, Int<32>{}); break;
+        case ROW_64x16: go(Int<256>{}, Int<64>{}, Int<16>{}); break;
+        case ROW_256x32: go(Int<256>{}, Int<256>{}, Int<32>{}); break;
+        case ROW_256x64: go(Int<256>{}, Int<256>{}, Int<64>{}); break;
+        case ROW_512x64: go(Int<512>{}, Int<512>{}, Int<64>{}); break;
+        case ROW_STREAMED: f(Int<1024>{}, Int<1024>{}, Int<32>{}, Int<STREAMED>{}); break;
+        default:
+            if constexpr (sizeof(T) == 4) {
+                if (form == ROW_256x8) go(Int<256>{}, Int<256>{}, Int<8>{});
+                else go(Int<1024>{}, Int<1024>{}, Int<64>{});
+            } else {
+                if (form == ROW_64x32) go(Int<256>{}, Int<64>{}, Int<32>{});
+                else if (form == ROW_1024x64) go(Int<1024>{}, Int<1024>{}, Int<64>{});
+                else if (form == ROW_512x128_RAW) f(Int<512>{}, Int<512>{}, Int<128>{}, Int<RAW>{});
+                else f(Int<1024>{}, Int<1024>{}, Int<128>{}, Int<RAW>{});
+            }
     }
 }
 
-// the same for kernels that stream rows: 16, 64 or 256 lanes a row, in workgroups of 64 or 256 threads
+// the same for kernels that stream rows: lanes a row, elements a lane has in flight
 template <class F>
-void with_part(int dtype, int lanes, int threads, F f) {
+void with_part(int dtype, int lanes, F f) {
     const auto typed = [&](auto type) {
-        if (lanes == 16 && threads == 64) f(type, Int<64>{}, Int<16>{}, Int<16>{});
-        else if (lanes == 16) f(type, Int<256>{}, Int<16>{}, Int<16>{});
-        else if (lanes == 64 && threads == 64) f(type, Int<64>{}, Int<64>{}, Int<16>{});
-        else if (lanes == 64) f(type, Int<256>{}, Int<64>{}, Int<16>{});
-        else f(type, Int<256>{}, Int<256>{}, Int<32>{});
+        if (lanes == 16) f(type, Int<16>{}, Int<16>{});
+        else if (lanes == 64) f(type, Int<64>{}, Int<32>{});
+        else f(type, Int<256>{}, Int<32>{});
     };
     if (dtype == GSPLIT_F32) typed(float{});
     else typed(bf16{});
 }
 
+Parts parts_of(const gsplit_ctx *ctx, int64_t n_rows, int C) {
+    const int chunks = row_chunks(n_rows, C, ctx->n_cu);
+    const int len = (int)gs_ceil_div(gs_ceil_div(C, chunks), 8) * 8;
+    return {(RowStats *)ctx->row_part, (float *)((RowStats *)ctx->row_part + GS_ROW_PARTS), (int)gs_ceil_div(C, len), len};
+}
+
 template <class T>
-void launch_policy(Rows R, const Policy &P, hipStream_t st) {
-    with_form(row_form(R.C, PIECE<T>), [&](auto threads, auto lanes, auto e) {
+void launch_policy(gsplit_ctx *ctx, Rows R, const Policy &P, hipStream_t st) {
+    if (policy_in_parts(R.n, R.C, PIECE<T>, ctx->n_cu)) {
+        const Parts S = parts_of(ctx, R.n, R.C);
+        const dim3 grid(S.chunks, (unsigned)R.n);
+        {
+            GsTimeScope ts(ctx, "policy_part_stats", -1, st);
+            hipLaunchKernelGGL(k_policy_part_stats<T>, grid, dim3(CT), 0, st, R, P, S);
+        }
+        GsTimeScope ts(ctx, "policy_loss", -1, st);
+        hipLaunchKernelGGL(k_policy_parts<T>, grid, dim3(CT), 0, st, R, P, S);
+        return;
+    }
+    with_form<T>(row_form(R.n, R.C, PIECE<T>, ctx->n_cu), [&](auto threads, auto lanes, auto e, auto way) {
         constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
         constexpr int64_t MOST = 1 << 21;       // workgroups of a launch: it has less than 2^32 threads
-        for (; R.first < R.n; R.first += MOST * (TH / LA))
-            hipLaunchKernelGGL((k_policy_rows<T, TH, LA, E>), dim3(row_grid(R.n - R.first, TH / LA, MOST)), dim3(TH), 0, st, R, P);
+        for (; R.first < R.n; R.first += MOST * (TH / LA)) {
+            GsTimeScope ts(ctx, "policy_loss", -1, st);
+            hipLaunchKernelGGL((k_policy_rows<T, TH, LA, E, decltype(way)::value>), dim3(row_grid(R.n - R.first, TH / LA, MOST)), dim3(TH), 0, st, R, P);
+        }
     });
 }
 
@@ -327,9 +451,8 @@ extern "C" int gsplit_policy_loss(gsplit_ctx *ctx, const gsplit_policy_config *c
         const Policy P{d_old_logp, d_ref_logp, d_advantages, d_row_weight, d_row_loss, d_row_logp, d_row_kl,
                        std::log(1.0 - (double)c->clip_low), std::log1p((double)c->clip_high), (float)(1.0 - (double)c->clip_low),
                        (float)(1.0 + (double)c->clip_high), c->kl_coef, (float)(1.0 / (double)n_rows)};
-        GsTimeScope ts(ctx, "policy_loss", -1, st);
-        if (c->dtype == GSPLIT_F32) launch_policy<float>(R, P, st);
-        else launch_policy<bf16>(R, P, st);
+        if (c->dtype == GSPLIT_F32) launch_policy<float>(ctx, R, P, st);
+        else launch_policy<bf16>(ctx, R, P, st);
         return GSPLIT_OK;
     });
 }
@@ -351,34 +474,48 @@ extern "C" int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
         const Pairs Q{d_seq_ptr, n_pairs, d_ref_logp, d_pair_weight, d_row_logp, d_pair_loss, d_pair_margin,
                       (float4 *)d_row_work, c->beta, c->label_smoothing, (float)(1.0 / (double)n_pairs)};
         const int64_t most = (int64_t)ctx->n_cu * 32;
-        const int whole = n_rows > 0 ? preference_whole(n_rows, n_pairs, (int64_t)n_classes * op_elem_size(c->dtype), ctx->n_cu) : 0;
+        const int whole = n_rows > 0 ? preference_whole(n_rows, n_pairs, n_classes, ctx->n_cu) : 0;
         if (whole) {
             GsTimeScope ts(ctx, "preference_loss", -1, st);
-            with_part(c->dtype, row_part(n_classes), whole, [&](auto type, auto threads, auto lanes, auto e) {
+            with_part(c->dtype, row_part(n_classes), [&](auto type, auto lanes, auto e) {
                 using T = decltype(type);
-                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
-                hipLaunchKernelGGL((k_preference_whole<T, TH, LA, E>), dim3((unsigned)n_pairs), dim3(TH), 0, st, R, Q);
+                constexpr int LA = decltype(lanes)::value, E = decltype(e)::value;
+                const auto go = [&](auto threads) {
+                    constexpr int TH = decltype(threads)::value;
+                    hipLaunchKernelGGL((k_preference_whole<T, TH, LA, E>), dim3((unsigned)n_pairs), dim3(TH), 0, st, R, Q);
+                };
+                if constexpr (LA == 256) go(Int<256>{});
+                else if (whole == 64) go(Int<64>{});
+                else if (whole == 256) go(Int<256>{});
+                else go(Int<1024>{});
             });
             return GSPLIT_OK;
         }
+        const bool grad = n_rows > 0 && d_grad_logits, f32 = c->dtype == GSPLIT_F32;
+        const Parts S = n_rows > 0 && preference_in_parts(n_rows, n_classes, ctx->n_cu) ? parts_of(ctx, n_rows, n_classes) : Parts{};
+        const dim3 parts(S.chunks, (unsigned)n_rows);
         if (n_rows > 0) {
             GsTimeScope ts(ctx, "preference_rows", -1, st);
-            with_part(c->dtype, row_part(n_classes), 256, [&](auto type, auto threads, auto lanes, auto e) {
+            if (S.chunks && f32) hipLaunchKernelGGL(k_preference_part_stats<float>, parts, dim3(CT), 0, st, R, Q, S);
+            else if (S.chunks) hipLaunchKernelGGL(k_preference_part_stats<bf16>, parts, dim3(CT), 0, st, R, Q, S);
+            else with_part(c->dtype, row_part(n_classes), [&](auto type, auto lanes, auto e) {
                 using T = decltype(type);
-                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
-                hipLaunchKernelGGL((k_preference_rows<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);
+                constexpr int LA = decltype(lanes)::value, E = decltype(e)::value;
+                hipLaunchKernelGGL((k_preference_rows<T, PT, LA, E>), dim3(row_grid(n_rows, PT / LA, most)), dim3(PT), 0, st, R, Q);
             });
         }
         {
             GsTimeScope ts(ctx, "preference_pairs", -1, st);
-            hipLaunchKernelGGL(k_preference_pairs, dim3(row_grid(n_pairs, 1, most)), dim3(PT), 0, st, R, Q);
+            hipLaunchKernelGGL(k_preference_pairs, dim3(row_grid(n_pairs, 1, most)), dim3(PT), 0, st, R, Q, S);
         }
-        if (n_rows > 0 && d_grad_logits) {
+        if (grad) {
             GsTimeScope ts(ctx, "preference_grad", -1, st);
-            with_part(c->dtype, row_part(n_classes), 256, [&](auto type, auto threads, auto lanes, auto e) {
+            if (S.chunks && f32) hipLaunchKernelGGL(k_preference_parts<float>, parts, dim3(CT), 0, st, R, Q, S);
+            else if (S.chunks) hipLaunchKernelGGL(k_preference_parts<bf16>, parts, dim3(CT), 0, st, R, Q, S);
+            else with_part(c->dtype, row_part(n_classes), [&](auto type, auto lanes, auto e) {
                 using T = decltype(type);
-                constexpr int TH = decltype(threads)::value, LA = decltype(lanes)::value, E = decltype(e)::value;
-                hipLaunchKernelGGL((k_preference_grad<T, TH, LA, E>), dim3(row_grid(n_rows, TH / LA, most)), dim3(TH), 0, st, R, Q);
+                constexpr int LA = decltype(lanes)::value, E = decltype(e)::value;
+                hipLaunchKernelGGL((k_preference_grad<T, PT, LA, E>), dim3(row_grid(n_rows, PT / LA, most)), dim3(PT), 0, st, R, Q);
             });
         }
         return GSPLIT_OK;

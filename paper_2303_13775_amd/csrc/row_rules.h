@@ -3,25 +3,53 @@
 
 #include <cstdint>
 
-// lanes a row x elements a lane holds; then rows that are read twice
-enum : int { ROW_16x8, ROW_16x16, ROW_64x8, ROW_64x16, ROW_256x8, ROW_256x16, ROW_256x32, ROW_512x32, ROW_512x64, ROW_1024x64, ROW_STREAMED };
+// lanes a row x elements a lane holds
+enum : int {
+    ROW_16x8, ROW_16x16, ROW_16x32, ROW_64x16, ROW_64x32, ROW_256x8, ROW_256x32, ROW_256x64, ROW_512x64, ROW_1024x64, ROW_512x128_RAW,
+    ROW_1024x128_RAW, ROW_STREAMED
+};
 
-// the first form whose registers hold a row of C elements, `piece` elements in 16 bytes
-inline int row_form(int C, int piece) {
-    const int held[] = {16 * 8, 16 * 16, 64 * 8, 64 * 16, 256 * 8, 256 * 16, 256 * 32, 512 * 32, 512 * 64, 1024 * 64};
-    for (int f = 0; f < ROW_STREAMED; ++f)
-        if (C / piece * piece <= held[f]) return f;
-    return ROW_STREAMED;
+// The form of rows of C elements, `piece` of them in 16 bytes (4: float, 8: bfloat16).
+inline int row_form(int64_t n_rows, int C, int piece, int n_cu) {
+    const int n = C / piece * piece;        // (what is behind the last whole piece has registers of its own)
+    if (n <= 16 * 8) return ROW_16x8;
+    if (n <= 16 * 16) return ROW_16x16;
+    if (n <= 16 * 32) return ROW_16x32;
+    if (n <= 64 * 16) return ROW_64x16;
+    if (n <= 64 * 32) return piece == 4 ? ROW_256x8 : ROW_64x32;
+    if (n <= 256 * 32) return ROW_256x32;
+    if (n <= 256 * 64) return ROW_256x64;
+    if (n <= 512 * 64) return ROW_512x64;
+    if (n <= 1024 * 64) return piece == 4 || n_rows <= n_cu ? ROW_1024x64 : ROW_512x128_RAW;
+    return piece == 8 && n <= 1024 * 128 ? ROW_1024x128_RAW : ROW_STREAMED;
 }
 
 // lanes a row of the kernels that stream rows
-inline int row_part(int C) { return C <= 256 ? 16 : C <= 1024 ? 64 : 256; }
+inline int row_part(int C) { return C <= 256 ? 16 : C <= 4096 ? 64 : 256; }
 
-// Threads of the workgroup that takes a pair of the preference loss from its rows to their gradient (0: three launches over all
-// rows, all pairs and all rows)
-inline int preference_whole(int64_t n_rows, int64_t n_pairs, int64_t row_bytes, int n_cu) {
+// Threads of the workgroup that takes a pair of the preference loss from its rows to their gradient; 0: three launches, over all
+// rows, all pairs and all rows.  A row a team up to what fills the chip with all pairs (in us, 1024 / 256 threads: 512 pairs of
+// 2 x 32 rows of 172 17.4 / 20.9, 2048 of 2 x 16 40 / 26.6).  A workgroup pays where its teams go round a few times only (one
+// launch / three, float: 256 x 2 x 17 x 172 7.8 / 12.4, 256 x 2 x 16 x 2048 34 / 41, 1024 x 2 x 16 x 2048, eight rounds, 126 / 128,
+// 600 x 2 x 64 x 1000, 32 rounds, 209 / 156); a team that is the whole workgroup also needs pairs for the whole chip (512 x 2 x 1 x
+// 65536 123 / 135, 128 x 2 x 2 x 20000 43 / 32), or next to nothing to do.
+inline int preference_whole(int64_t n_rows, int64_t n_pairs, int C, int n_cu) {
     if (n_pairs >= (1 << 24)) return 0;         // (a launch has less than 2^32 threads)
-    const int64_t pair_bytes = n_rows * row_bytes / n_pairs;
-    if (pair_bytes > (64 << 10) && n_pairs < 2 * n_cu) return 0;
-    return n_rows <= 4 * n_pairs ? 64 : 256;
+    const int lanes = row_part(C);
+    const int64_t rows = (n_rows + n_pairs - 1) / n_pairs;      // of a pair, on average
+    if (lanes == 256) return (n_pairs >= 2 * n_cu && rows <= 8) || rows * ((C + 8191) / 8192) <= 2 ? 256 : 0;
+    const int64_t room = (int64_t)n_cu * 2048 / n_pairs, want = rows * lanes < room ? rows * lanes : room;
+    const int threads = want <= 64 ? 64 : want <= 256 || room < 1024 ? 256 : 1024;
+    return rows * lanes <= 8 * threads ? threads : 0;
 }
+
+// Parts of a row where there are few rows: two workgroups a compute unit, parts of at least 4096 elements, at most 64 of them
+constexpr int GS_ROW_PARTS = 8192;      // (row, part) pairs the context's scratch holds
+inline int row_chunks(int64_t n_rows, int C, int n_cu) {
+    int64_t chunks = (2 * n_cu + n_rows - 1) / n_rows;
+    if (chunks > C / 4096) chunks = C / 4096;
+    if (chunks > GS_ROW_PARTS / n_rows) chunks = GS_ROW_PARTS / n_rows;
+    return chunks < 1 ? 1 : chunks > 64 ? 64 : (int)chunks;
+}
+inline bool policy_in_parts(int64_t n_rows, int C, int piece, int n_cu) { return C / piece * piece > 1024 * 64 && n_rows < n_cu / 2; }
+inline bool preference_in_parts(int64_t n_rows, int C, int n_cu) { return C > 8192 && n_rows < n_cu; }
