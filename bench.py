@@ -5,7 +5,8 @@ One step = one whole iteration over a fresh synthetic mini-batch, all inputs res
 gsplit_sample_split -> gsplit_gather_features -> gsplit_sage_fwd -> gsplit_softmax_xent (loss
 gradient of the logits) -> gsplit_sage_bwd.  Prints ONE JSON line of a few kilobytes (the figures a
 reader wants first); `--report FILE` also writes everything measured.  `--model gat` runs the paper's
-second model (gsplit_gat_fwd / gsplit_gat_bwd) through the same steps.
+second model (gsplit_gat_fwd / gsplit_gat_bwd) through the same steps, `--update` ends every step with the
+clipped AdamW update (gsplit_adamw_step).
 
 The workload is the "medium" configuration (2.4M-vertex / ~124M-edge R-MAT graph, 100-d fp32
 features, 47 classes, range partition map, 4 logical splits, batch 1024, fanouts [15,10,5],
@@ -57,6 +58,9 @@ def parse():
                     help="replay the timed steps as captured HIP graphs instead of enqueueing every kernel from the "
                          "host (measured: no faster here, the steps are bound by the device-side kernel boundaries, "
                          "not by the host's launch rate)")
+    ap.add_argument("--update", action="store_true",
+                    help="end every step with the update: gradients clipped to a global norm of 1 and AdamW "
+                         "(gsplit_adamw_step); not with --graph")
     ap.add_argument("--presample", action="store_true",
                     help="measure the offline pre-sampling stage instead (sampling + counting of k_v, k_e)")
     ap.add_argument("--redundancy", action="store_true",
@@ -79,13 +83,17 @@ def parse():
     ap.add_argument("--report", default=None, metavar="FILE",
                     help="write the full report (per-kernel times and rooflines, launch order, schedules, every extra "
                          "configuration in the same detail) to FILE as JSON")
-    return ap.parse_args()
+    a = ap.parse_args()
+    if a.update and a.graph:
+        ap.error("--update changes the weights from step to step: the check of a replayed step against an eager one cannot run with it")
+    return a
 
 
 class Runner:
     """Holds the device-resident inputs, the context and the preallocated outputs of a step."""
 
     separate_calls = False      # set from --separate-calls
+    with_update = False         # set from --update
 
     def __init__(self, w, dev, model="sage", heads=4, sampler_blocks_per_cu=0):
         import torch
@@ -109,6 +117,19 @@ class Runner:
         self.logits = torch.empty((w.batch, w.dims[-1]), device=dev)
         self.glogits = torch.empty_like(self.logits)
         self.seed = 0xC0FFEE
+        if Runner.with_update:
+            from paper_2303_13775_amd import AdamwTensors
+            params = [t for lst in self.params.tensors for t in lst]
+            if not hasattr(w, "moments"):       # one optimiser state, whichever slot runs the step
+                w.moments = [[torch.zeros_like(t) for t in params] for _ in range(2)]
+                w.updates = 0
+            self.table = AdamwTensors(params, [t for lst in self.grads for t in lst], *w.moments)
+
+    def update(self):
+        """Clipped AdamW step of the weights, if asked for."""
+        if Runner.with_update:
+            self.w.updates += 1
+            self.ctx.gsplit_adamw_step(self.table, lr=1e-3, step=self.w.updates, max_norm=1.0)
 
     def enable_cache(self, host_table, cache_ids, n_cache):
         self.ctx.gsplit_cache_build(host_table, cache_ids, n_cache)
@@ -155,6 +176,7 @@ class Runner:
             self.forward()
             self.loss()
             self.backward()
+        self.update()
 
     def capture(self, stream, parts):
         """One graph per element of parts ('sample', 'train', or 'step' for both)."""
@@ -202,6 +224,7 @@ class Runner:
         self.loss()
         rec(4)
         self.backward()
+        self.update()
         rec(5)
 
 
@@ -1191,6 +1214,7 @@ def json_line(out):
 def main():
     a = parse()
     Runner.separate_calls = a.separate_calls
+    Runner.with_update = a.update
     if a.gpus != 1:
         print("bench.py: this build runs on ONE GPU (logical splits share it); --gpus must be 1",
               file=sys.stderr)
@@ -1262,7 +1286,8 @@ def main():
                 use_graph=a.graph)
     r = m.pop("_runner")
     out = {
-        "metric": f"mini-batches/sec (sample+split+gather+{'GAT' if a.model == 'gat' else 'SAGE'} fwd/bwd) at 1 GPU",
+        "metric": f"mini-batches/sec (sample+split+gather+{'GAT' if a.model == 'gat' else 'SAGE'} fwd/bwd"
+                  f"{'+clipped AdamW update' if a.update else ''}) at 1 GPU",
         "value": m.pop("value"), "unit": "mini-batches/s", "n_gpus": 1, "steps": a.steps,
         "warmup": a.warmup, "ms_per_step": m.pop("ms_per_step"), "higher_is_better": True, "scaling": "weak",
         "vs_baseline": None, "dtype": dtype, "data": "synthetic",
@@ -1305,7 +1330,7 @@ def main():
     r.ctx.close()
     if a.extra_configs is None:
         a.extra_configs = (a.workload == "medium" and a.model == "sage" and dtype == "f32" and cache_info is None
-                           and not a.graph and not a.no_pipeline)
+                           and not a.graph and not a.no_pipeline and not a.update)
     if a.extra_configs:
         del w, r
         torch.cuda.empty_cache()

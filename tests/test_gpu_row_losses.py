@@ -104,7 +104,11 @@ def test_policy_wide_rows(ctx, C, dtype, n):
     _policy(ctx, _logits(rng, n, C, dtype), _actions(rng, n, C), dtype=dtype, pad=(C + n) % 3)
 
 
-@pytest.mark.parametrize("n, C", [(300, 16385), (270, 33001), (600, 9000)])
+# (rows, classes) of the forms that need many rows, or that the widths above leave out
+POLICY_FORMS = [(260, 60001), (257, 65543), (130, 70001), (128, 131079), (130, 140001)]
+
+
+@pytest.mark.parametrize("n, C", [(300, 16385), (270, 33001), (600, 9000)] + POLICY_FORMS)
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_policy_many_wide_rows(ctx, n, C, dtype):
     rng = np.random.default_rng(C)
@@ -293,6 +297,23 @@ def test_preference_lengths(ctx, lengths, C):
     rng = np.random.default_rng(len(lengths))
     n = int(np.sum(lengths))
     _preference(ctx, _logits(rng, n, C, F32), _actions(rng, n, C), _ptr(lengths))
+
+
+# lengths and classes of every way a pair is taken: a workgroup of 64, 256 or 1024 threads or three launches, teams of 16, 64 and 256
+# lanes, and rows in parts
+PREFERENCE_FORMS = [([1, 1] * 20, 47), ([3, 5] * 30, 47), ([40, 30] * 5, 172), ([700, 400], 172), ([1, 0] * 10, 1000), ([2, 1] * 9, 3000),
+                    ([7, 6] * 3, 600), ([100, 150], 900), ([1, 1], 5000), ([150, 160], 5001), ([20, 10], 20000)]
+
+
+@pytest.mark.parametrize("lengths, C", PREFERENCE_FORMS)
+def test_preference_forms(ctx, lengths, C):
+    rng = np.random.default_rng(C)
+    n = int(np.sum(lengths)) + 2
+    a = _actions(rng, n, C)
+    a[rng.random(n) < 0.2] = -1
+    for dtype in (F32, BF16):
+        _preference(ctx, _logits(rng, n, C, dtype), a, _ptr(lengths, 1), dtype=dtype)
+        _preference(ctx, _logits(rng, n, C, dtype), a, _ptr(lengths, 1), dtype=dtype, pad=3, gpad=3, grad="in place")
 
 
 @pytest.mark.parametrize("lengths, C", [([1, 1], 65537), ([2, 1], 131072), ([1, 0], 140001), ([3, 4, 1, 0], 50001), ([150, 160], 9001)])
