@@ -462,11 +462,11 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
 
 /* Losses over rows of logits and their gradients, beside gsplit_softmax_xent: for models that are
  * trained from actions and advantages, or from pairs of which one is preferred.  d_logits: n_rows rows of
- * n_classes values (dtype GSPLIT_F32 or GSPLIT_BF16), logits_stride elements apart; the rows a
+ * n_classes (at most 2^30) values (dtype GSPLIT_F32 or GSPLIT_BF16), logits_stride elements apart; the rows a
  * gsplit_sage_fwd or gsplit_gat_fwd wrote (row r belongs to local_cat[L][r]) or any other model's.
  * d_grad_logits receives d loss / d logits in the same dtype, rows grad_stride elements apart: it may be
  * d_logits itself with the same stride (each row is read before it is written), may not overlap it in
- * another way, and NULL asks for the forward pass alone.  d_actions [n_rows] int64.  With
+ * another way, and NULL asks for the forward pass alone.  No other output may overlap anything.  d_actions [n_rows] int64.  With
  *     log p(r) = log softmax(logits of row r)[action of row r]
  * a row takes no part in the loss if its action lies outside [0, n_classes), or if all its logits are
  * -inf (no class is possible): its log p is reported as 0 and its gradient is 0.  Classes with a logit of
@@ -484,7 +484,7 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
  * takes no part (its logits are not read, all its outputs are 0).  Where both sides of the maximum
  * are equal the gradient is that of the unclipped one.  d_ref_logp may be NULL if kl_coef is 0.  d_row_loss,
  * d_row_logp (log p) and d_row_kl [n_rows] may be NULL; kl(r) is 0 without d_ref_logp.  EINVAL for NULL
- * inputs, n_rows < 0, n_classes < 1, strides below n_classes, an unknown dtype, addresses that are no
+ * inputs, n_rows < 0, n_classes out of range, strides below n_classes, an unknown dtype, addresses that are no
  * multiple of their type's size, clip_low outside [0, 1], clip_high or kl_coef negative or not finite. */
 typedef struct {
     int32_t dtype;
@@ -532,7 +532,8 @@ GSPLIT_API int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
  * A norm that is not finite (an infinity or a NaN among the gradients) is reported, the factor is then
  * 1 for gsplit_clip_grads, and gsplit_adamw_step leaves parameters and moments as they are.  Tensors are
  * dense runs of n elements at any address that is a multiple of the element's size; n may be 0 (then the
- * pointers may be NULL).  The HOST arrays are read during the call.  Asynchronous; may be captured at any
+ * pointers may be NULL).  What a call writes may overlap none of its other tensors (a tensor may not be
+ * listed twice), but for a gradient clipped in place.  The HOST arrays are read during the call.  Asynchronous; may be captured at any
  * time (the addresses are then fixed).  Scratch memory as for the losses above.
  * EINVAL for NULL or misaligned pointers, negative counts, unknown dtypes, max_norm not above 0. */
 typedef struct {
@@ -556,7 +557,7 @@ GSPLIT_API int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *grad
  * max_norm 0: no norm is formed, the factor is 1, d_norm is not written.  t = *d_step if given (DEVICE, read
  * when the kernels run, taken as 1 if lower), else step >= 1; the learning rate is *d_lr if given, else lr.
  * EINVAL also for betas outside [0, 1), lr, eps or weight_decay negative or not finite, a missing d_master
- * (or one that a float parameter has).  No two of a call's tensors may overlap. */
+ * (or one that a float parameter has). */
 typedef struct {
     void       *d_param;
     float      *d_master;        /* bfloat16 parameters: their float copy; NULL for float ones */

@@ -342,6 +342,17 @@ def _same_device(ts):
     return ts[0].device if ts else None
 
 
+def _assert_apart(written, read):
+    """No tensor that is written overlaps another one."""
+    runs = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w)
+                  for ts, w in ((written, True), (read, False)) for t in ts if t is not None and t.numel())
+    end = end_written = 0
+    for lo, hi, w in runs:
+        assert lo >= (end if w else end_written), "tensors of a call overlap"
+        end = max(end, hi)
+        end_written = max(end_written, hi if w else 0)
+
+
 class GradTensors:
     """Holds the marshalled gradient tensors of gsplit_grad_norm and gsplit_clip_grads (and keeps them
     alive).  outs: where the clipped gradients go; None, or the gradients themselves: in place."""
@@ -353,6 +364,7 @@ class GradTensors:
         for g, o in zip(grads, outs):
             assert g.dtype in _DTYPES and g.is_contiguous()
             assert o.dtype == g.dtype and o.is_contiguous() and o.numel() == g.numel()
+        _assert_apart(outs, [g for g, o in zip(grads, outs) if g.data_ptr() != o.data_ptr()])
         self.tensors = (list(grads), list(outs))
         self.n = len(self.tensors[0])
         self.c = (_GradTensor * max(1, self.n))(*[_GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), _DTYPES[g.dtype])
@@ -373,6 +385,7 @@ class AdamwTensors:
             for t in (p, g, a, b, w):
                 assert t is None or (t.is_contiguous() and t.numel() == p.numel())
             assert all(t is None or t.dtype == torch.float32 for t in (a, b, w))
+        _assert_apart([*params, *masters, *m, *v], grads)
         self.tensors = (list(params), list(grads), list(m), list(v), list(masters))
         self.n = len(self.tensors[0])
         self.c = (_AdamwTensor * max(1, self.n))(*[

@@ -18,7 +18,7 @@ inline const char *op_check_rows(int32_t dtype, const void *d_logits, int64_t n_
     const int size = op_elem_size(dtype);
     if (!size) return "unknown dtype";
     if (n_rows < 0 || n_rows > (int64_t)1 << 40) return "n_rows out of range";
-    if (n_classes < 1) return "n_classes below 1";
+    if (n_classes < 1 || n_classes > 1 << 30) return "n_classes out of range";
     const int64_t stride_max = (int64_t)1 << 40;
     if (logits_stride < n_classes || logits_stride > stride_max || (d_grad && (grad_stride < n_classes || grad_stride > stride_max)))
         return "stride below n_classes or out of range";

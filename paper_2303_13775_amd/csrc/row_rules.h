@@ -9,7 +9,16 @@ enum : int {
     ROW_1024x128_RAW, ROW_STREAMED
 };
 
-// The form of rows of C elements, `piece` of them in 16 bytes (4: float, 8: bfloat16).
+// The form of n_rows rows of C elements, `piece` of them in 16 bytes (4: float, 8: bfloat16): the fewest lanes whose registers hold
+// the row, as long as the lanes of a wave hide the memory's latency.  Policy loss, us (taken / the next form up or down):
+//   lanes: 32768 x 172 float 16 10.5 / 64 22.2, 32768 x 512 bf16 16 13.8 / 64 23.7 (a row's double arithmetic is a wave's, whatever
+//     number of rows the wave has); 32768 x 1024 float 64 43.6 / 256 59.8; 32768 x 2048 bf16 64 45.0 / 256 60.6, float 64 91 / 256 84.7
+//   elements a lane: 32768 x 128 float 8 8.1 / 16 8.6; 32768 x 256 16 11.9 / 32 13.7; 32768 x 1024 16 43.6 / 32 44.9; 32768 x 4096
+//     float, 256 lanes, 32 172 / 64 168 / 16 172, bf16 32 87.7 / 64 110 / 16 87.6; 8192 x 16384 float 256 x 64 183 / 512 x 32 195
+//   bfloat16 rows as they are, exponentials formed twice, in half the registers, where a compute unit then holds two rows instead
+//     of one: 2048 x 65536 94.6 / 100, 2048 x 50001 92.7 / 102; no more rows than compute units: 1 x 65536 9.2 / 7.4.  Narrower ones
+//     gain nothing: 4096 x 32768 95.1 / 91.9, 16384 x 8192 87.2 / 84.7
+//   bfloat16 rows of up to 131072 the same way against reading them twice: 1024 x 131072 107 / 118.
 inline int row_form(int64_t n_rows, int C, int piece, int n_cu) {
     const int n = C / piece * piece;        // (what is behind the last whole piece has registers of its own)
     if (n <= 16 * 8) return ROW_16x8;
@@ -24,7 +33,7 @@ inline int row_form(int64_t n_rows, int C, int piece, int n_cu) {
     return piece == 8 && n <= 1024 * 128 ? ROW_1024x128_RAW : ROW_STREAMED;
 }
 
-// lanes a row of the kernels that stream rows
+// Lanes a row of the preference loss, which streams rows.  16 x 500 x 2 rows of 2048 float, three launches: 64 lanes 69 us, 256 89.
 inline int row_part(int C) { return C <= 256 ? 16 : C <= 4096 ? 64 : 256; }
 
 // Threads of the workgroup that takes a pair of the preference loss from its rows to their gradient; 0: three launches, over all
@@ -43,7 +52,10 @@ inline int preference_whole(int64_t n_rows, int64_t n_pairs, int C, int n_cu) {
     return rows * lanes <= 8 * threads ? threads : 0;
 }
 
-// Parts of a row where there are few rows: two workgroups a compute unit, parts of at least 4096 elements, at most 64 of them
+// Parts of a row where there are few rows: two workgroups a compute unit, parts of at least 4096 elements, at most 64 of them.
+// Policy loss, parts / whole rows: 1 x 131072 float 9.3 / 21, bf16 9.7 / 16.6, 64 x 131072 float 16 / 22.7, bf16 11.3 / 17.1; from
+// half a row a compute unit on whole rows again (250 x 131072 67 / 60).  Preference loss: 1 pair of 65536 12.4 / 28, 120 pairs
+// 39 / 47.
 constexpr int GS_ROW_PARTS = 8192;      // (row, part) pairs the context's scratch holds
 inline int row_chunks(int64_t n_rows, int C, int n_cu) {
     int64_t chunks = (2 * n_cu + n_rows - 1) / n_rows;

@@ -1,4 +1,9 @@
 // Behind the backward pass: the global gradient norm over many tensors, clipping by it, and the AdamW update.
+//
+// Memory bounds all of it.  The factor needs every gradient before the first can be scaled, so gradients are read twice; the second
+// pass begins with the chunks that the first has left in the 256 MB cache.  400 M gradients of two types in 387 tensors 679 us, 3.6 GB
+// at 5.3 TB/s (a plain copy of that size 4.8); the update of 250 M 1630 us, 7.5 GB at 4.6 TB/s: eight streams of it, four read and
+// four written.  Of small calls the launches are all: 10 k gradients clipped 4.2 us on the device, the update of 206 k 3.4 + 5.3.
 #include <algorithm>
 #include <cmath>
 
@@ -238,7 +243,7 @@ __device__ __forceinline__ void update1(float &p, float &m, float &v, float g, c
     v = S.b2 * v + S.a2 * (g * g);
     p = S.keep * p - S.rate * m / (sqrtf(v * S.root) + S.eps);
 }
-template <class T, bool HALF>
+template <class T, bool HALF, int THREADS>
 __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, float *m, float *v, int n, const Steps &S) {
     constexpr int DEEP = 2;
     const int nv = n / 4;
@@ -247,12 +252,12 @@ __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, flo
         float pp[D][4], mm[D][4], vv[D][4], gg[D][4];
 #pragma unroll
         for (int i = 0; i < D; ++i) {
-            const int e = (j + i * UT) * 4;
+            const int e = (j + i * THREADS) * 4;
             unpack<float>(load_kept(p + e), pp[i]); unpack<float>(load_kept(m + e), mm[i]); unpack<float>(load_kept(v + e), vv[i]); load4(g + e, gg[i]);
         }
 #pragma unroll
         for (int i = 0; i < D; ++i) {
-            const int e = (j + i * UT) * 4;
+            const int e = (j + i * THREADS) * 4;
 #pragma unroll
             for (int k = 0; k < 4; ++k) update1(pp[i][k], mm[i][k], vv[i][k], gg[i][k], S);
             store_kept(p + e, pack<float>(pp[i])); store_kept(m + e, pack<float>(mm[i])); store_kept(v + e, pack<float>(vv[i]));
@@ -261,8 +266,8 @@ __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, flo
         }
     };
     int j = threadIdx.x;
-    for (; j + (DEEP - 1) * UT < nv; j += DEEP * UT) step(j, std::integral_constant<int, DEEP>{});
-    for (; j < nv; j += UT) step(j, std::integral_constant<int, 1>{});
+    for (; j + (DEEP - 1) * THREADS < nv; j += DEEP * THREADS) step(j, std::integral_constant<int, DEEP>{});
+    for (; j < nv; j += THREADS) step(j, std::integral_constant<int, 1>{});
     if ((int)threadIdx.x < n - nv * 4) {
         const int e = nv * 4 + threadIdx.x;
         float pi = p[e], mi = m[e], vi = v[e];
@@ -275,10 +280,10 @@ __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, flo
 // How the norm reaches the update: not at all, from the slots, or formed by every workgroup anew (few elements)
 enum : int { NORM_NONE, NORM_SLOTS, NORM_HERE };
 
-template <int WHENCE>
-__global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, Steps S, const double *__restrict__ slots, int n_slots,
+template <int WHENCE, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_adamw(Adamw A, Hyper H, Steps S, const double *__restrict__ slots, int n_slots,
                                               float *__restrict__ norm_out) {
-    __shared__ double lds[UT / 64];
+    __shared__ double lds[THREADS / 64];
     if (H.d_step || H.d_lr) {
         __shared__ Steps shared;
         if (threadIdx.x == 0)
@@ -288,8 +293,8 @@ __global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, Steps S, const d
     }
     if constexpr (WHENCE != NORM_NONE) {
         float norm;
-        if constexpr (WHENCE == NORM_SLOTS) norm = norm_of<UT>(slots, n_slots, lds);
-        else norm = (float)sqrt(wg_sum<UT>(share_of_squares<64>(A, A.half_g, wave_id(), UT / 64), lds));
+        if constexpr (WHENCE == NORM_SLOTS) norm = norm_of<THREADS>(slots, n_slots, lds);
+        else norm = (float)sqrt(wg_sum<THREADS>(share_of_squares<64>(A, A.half_g, wave_id(), THREADS / 64), lds));
         if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
         if (!is_finite(norm)) return;
         S.f = factor_of(norm, H.max_norm);
@@ -303,12 +308,12 @@ __global__ __launch_bounds__(UT) void k_adamw(Adamw A, Hyper H, Steps S, const d
         if (A.half_p[t]) {
             float *p = A.master[t] + at;
             bf16 *half = (bf16 *)A.p[t] + at;
-            if (A.half_g[t]) update_run<bf16, true>(p, half, gh, m, v, n, S);
-            else update_run<float, true>(p, half, g, m, v, n, S);
+            if (A.half_g[t]) update_run<bf16, true, THREADS>(p, half, gh, m, v, n, S);
+            else update_run<float, true, THREADS>(p, half, g, m, v, n, S);
         } else {
             float *p = (float *)A.p[t] + at;
-            if (A.half_g[t]) update_run<bf16, false>(p, nullptr, gh, m, v, n, S);
-            else update_run<float, false>(p, nullptr, g, m, v, n, S);
+            if (A.half_g[t]) update_run<bf16, false, THREADS>(p, nullptr, gh, m, v, n, S);
+            else update_run<float, false, THREADS>(p, nullptr, g, m, v, n, S);
         }
     }
 }
@@ -437,7 +442,7 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_adamw_step: ") + e);
         const auto len = [&](int64_t i) { return t[i].n; };
         const Plan p = plan(ctx, n_tensors, ADAMW_TENSORS, len);
-        const bool here = p.used <= ADAMW_TENSORS && update_norm_here(p.total);
+        const bool here = c->max_norm > 0.0 && p.used <= ADAMW_TENSORS && update_norm_here(p.total);
         int slots = 0;
         if (c->max_norm > 0.0 && !here)
             slots = launch_norm(ctx, n_tensors, [&](int64_t i) {
@@ -454,8 +459,8 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
             },
             [&](const Adamw &A, bool first) {
                 GsTimeScope ts(ctx, "adamw", -1, st);
-                const auto kernel = c->max_norm == 0.0 ? k_adamw<NORM_NONE> : here ? k_adamw<NORM_HERE> : k_adamw<NORM_SLOTS>;
-                hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(UT), 0, st, A, H, S, ctx->norm_part, slots, first ? d_norm : nullptr);
+                const auto kernel = here ? k_adamw<NORM_HERE, ST> : slots ? k_adamw<NORM_SLOTS, UT> : k_adamw<NORM_NONE, UT>;
+                hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(here ? ST : UT), 0, st, A, H, S, ctx->norm_part, slots, first ? d_norm : nullptr);
             });
         return GSPLIT_OK;
     });

@@ -288,5 +288,15 @@ def test_refusals(ctx):
                 lambda: AdamwTensors([g.bfloat16()], [g], [g], [g]), lambda: AdamwTensors([g], [g], [g], [g], [g]), lambda: AdamwTensors([g], [g[:4]], [g], [g])):
         with pytest.raises(AssertionError):
             bad()
+    x = torch.ones(100, device="cuda")
+    y = [torch.ones(50, device="cuda") for _ in range(2)]
+    for bad in (lambda: GradTensors([x, x]), lambda: GradTensors([x[:60], x[50:]]), lambda: GradTensors([x[:50], x[50:]], [x[50:], x[:50]]),
+                lambda: GradTensors([x[:50]], [x[1:51]]), lambda: GradTensors(y, [x[:50], x[49:99]]), lambda: AdamwTensors([x[:50]], [x[20:70]], *[[t] for t in y]),
+                lambda: AdamwTensors([x[:50]], [y[0]], [y[1]], [y[1]])):
+        with pytest.raises(AssertionError):
+            bad()
+    GradTensors([x[:50], x[50:]])
+    GradTensors([x, x[:50]], [torch.ones_like(x), y[0]])        # what is only read may be listed twice
+    GradTensors([x[:0], x, x[:0]])
     ctx.gsplit_grad_norm(GradTensors([g]), norm)
     assert abs(float(norm) - np.sqrt(8)) < 1e-6

@@ -63,7 +63,7 @@ def test_policy_takes(change):
 
 
 @pytest.mark.parametrize("change", [
-    dict(cfg=(2, 0.2, 0.2, 0.1)), dict(cfg=(-1, 0.2, 0.2, 0.1)), dict(n=-1), dict(classes=0), dict(ld=7), dict(gld=7), dict(z=None), dict(a=None),
+    dict(cfg=(2, 0.2, 0.2, 0.1)), dict(cfg=(-1, 0.2, 0.2, 0.1)), dict(n=-1), dict(classes=0), dict(classes=(1 << 30) + 1, ld=1 << 31, gld=1 << 31), dict(ld=7), dict(gld=7), dict(z=None), dict(a=None),
     dict(old=None), dict(adv=None), dict(ref=None), dict(z=P + 2), dict(a=P + 4), dict(g=P + 2), dict(cfg=(1, 0.2, 0.2, 0.1), z=P + 1),
     dict(old=P + 2), dict(kl=P + 1), dict(g=P, gld=9), dict(n=1 << 41), dict(ld=1 << 41)]
     + [dict(cfg=(0, x, 0.2, 0.1)) for x in (-0.1, 1.1, NAN, INF)] + [dict(cfg=(0, 0.2, x, 0.1)) for x in (-0.1, NAN, INF)]
