@@ -181,7 +181,7 @@ extern "C" int gsplit_create(gsplit_ctx **out, const gsplit_graph *g, const gspl
         A((void **)&ctx->mixed_pos, sizeof(int32_t) * max_items, "positions of mixed rows");
     }
     A(&ctx->row_part, GS_ROW_PARTS * (16 + sizeof(float)), "statistics of parts of rows");
-    A((void **)&ctx->norm_part, sizeof(double) * GS_NORM_SLOTS, "gradient norm");
+    A((void **)&ctx->norm_part, sizeof(double) * (GS_NORM_SLOTS + 1), "gradient norm");
     A((void **)&ctx->part_hist, sizeof(int32_t) * 1024 * 25, "partition histogram");
     A((void **)&ctx->part_base, sizeof(int32_t) * 1024 * 25, "partition bases");
     if (rc == GSPLIT_OK && hipMemset(ctx->d_meta, 0, sizeof(GsLevelMeta) * (L + 1)) != hipSuccess)

@@ -225,7 +225,7 @@ struct gsplit_ctx {
     std::shared_ptr<GsEvent> own_done;      // the event that this context's calls record (none: static arrays)
     std::shared_ptr<GsEvent> sample_done;   // the one that stands behind its current batch: its own, or that of a grouped call
 
-    double      *norm_part = nullptr;       // [GS_NORM_SLOTS] a workgroup's sum of squares each (gradient norm)
+    double      *norm_part = nullptr;       // [GS_NORM_SLOTS + 1] a workgroup's sum of squares each, and their sum (gradient norm)
     void        *row_part = nullptr;        // statistics of parts of rows (losses over few wide rows)
 
     GsSageBuf    sage;

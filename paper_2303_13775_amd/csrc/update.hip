@@ -1,8 +1,8 @@
 // Behind the backward pass: the global gradient norm over many tensors, clipping by it, and the AdamW update.
 //
 // Memory bounds all of it.  The factor needs every gradient before the first can be scaled, so gradients are read twice; the second
-// pass begins with the chunks that the first has left in the 256 MB cache.  400 M gradients of two types in 387 tensors 679 us, 3.6 GB
-// at 5.3 TB/s (a plain copy of that size 4.8); the update of 250 M 1630 us, 7.5 GB at 4.6 TB/s: eight streams of it, four read and
+// pass begins with the chunks that the first has left in the 256 MB cache.  400 M gradients of two types in 387 tensors 606 us, 3.6 GB
+// at 5.9 TB/s (a plain copy of that size 4.8); the update of 250 M 1476 us, 7.5 GB at 5.1 TB/s: eight streams of it, four read and
 // four written.  Of small calls the launches are all: 10 k gradients clipped 4.2 us on the device, the update of 206 k 3.4 + 5.3.
 #include <algorithm>
 #include <cmath>
@@ -24,7 +24,7 @@ struct Chunks {
     int32_t first[N + 1];       // first chunk of a tensor
     int32_t tail[N];            // elements of its last chunk
     int32_t n, chunk;
-    __device__ __forceinline__ int count() const { return first[n]; }
+    __host__ __device__ __forceinline__ int count() const { return first[n]; }
     __device__ __forceinline__ int tensor_of(int c) const {
         int lo = 0, hi = n;
         while (hi - lo > 1) {
@@ -144,6 +144,15 @@ __device__ __forceinline__ float factor_of(float norm, float max_norm) {
     return is_finite(norm) && norm > max_norm ? max_norm / norm : 1.f;
 }
 
+// their sum, in the slot behind them: for passes of many workgroups, which would each add up a thousand slots
+__global__ __launch_bounds__(UT) void k_sum_slots(double *__restrict__ slots, int n_slots) {
+    __shared__ double lds[UT / 64];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n_slots; i += UT) s += slots[i];
+    s = wg_sum<UT>(s, lds);
+    if (threadIdx.x == 0) slots[GS_NORM_SLOTS] = s;
+}
+
 __global__ __launch_bounds__(UT) void k_norm_of(const double *__restrict__ slots, int n_slots, float *__restrict__ norm) {
     __shared__ double lds[UT / 64];
     const float x = norm_of<UT>(slots, n_slots, lds);
@@ -225,7 +234,7 @@ __host__ __device__ inline Steps steps_of(const Hyper &H, double lr, double t) {
 }
 
 // Parameter and moments go through the caches like any other data: with the hint that they will not be read again 250 M elements
-// took 1711 us, without it 1630.  (Four pieces in flight, or twice the workgroups, came out the same; 1024 threads a workgroup 1790.)
+// took 1711 us instead of 1630, then.
 
 // four elements of the gradient of either type
 template <class T>
@@ -245,7 +254,7 @@ __device__ __forceinline__ void update1(float &p, float &m, float &v, float g, c
 }
 template <class T, bool HALF, int THREADS>
 __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, float *m, float *v, int n, const Steps &S) {
-    constexpr int DEEP = 2;
+    constexpr int DEEP = 4;
     const int nv = n / 4;
     const auto step = [&](int j, auto deep) {
         constexpr int D = decltype(deep)::value;
@@ -351,40 +360,39 @@ void in_groups(int64_t n_tensors, int chunk, bool back, Len len, Fill fill, Laun
     } while (i >= 0 && i < n_tensors);
 }
 
-struct Plan { int chunk; int grid; int64_t total, used; };      // grid: of every launch of a call
-
+struct Totals { int64_t elements = 0, tensors = 0; };       // tensors: those that are not empty
 template <class Len>
-Plan plan(const gsplit_ctx *ctx, int64_t n_tensors, int per_group, Len len) {
-    Plan p{0, 1, 0, 0};
-    for (int64_t i = 0; i < n_tensors; ++i) { p.total += len(i); p.used += len(i) > 0; }
-    p.chunk = update_chunk(p.total, ctx->n_cu);
-    int64_t most = 1, group = 0, k = 0;
-    for (int64_t i = 0; i < n_tensors; ++i) {
-        if (len(i) == 0) continue;
-        if (k++ % per_group == 0) group = 0;
-        group += gs_ceil_div(len(i), p.chunk);
-        most = std::max(most, group);
-    }
-    p.grid = (int)std::min<int64_t>(std::min<int64_t>(GS_NORM_SLOTS, (int64_t)ctx->n_cu * 4), most);
-    return p;
+Totals totals_of(int64_t n_tensors, Len len) {
+    Totals t;
+    for (int64_t i = 0; i < n_tensors; ++i) { t.elements += len(i); t.tensors += len(i) > 0; }
+    return t;
 }
 
-// slots of the squares of all gradients; returns how many
+// Where a pass finds the sum of all squares: at[0 .. n - 1]
+struct Slots { const double *at; int n; };
+
+// forms it; passes of `workgroups` workgroups will read it
 template <class GradOf>
-int launch_norm(gsplit_ctx *ctx, int64_t n_tensors, GradOf grad, hipStream_t st) {
+Slots launch_norm(gsplit_ctx *ctx, int64_t n_tensors, const Totals &total, int64_t workgroups, GradOf grad, hipStream_t st) {
     const auto len = [&](int64_t i) { return grad(i).n; };
-    const Plan p = plan(ctx, n_tensors, NORM_TENSORS, len);
+    const int chunk = norm_chunk(total.elements, ctx->n_cu);
+    // the grid of all launches: what the first one's chunks fill (a slot that a launch has nothing for keeps its sum)
+    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(GS_NORM_SLOTS, (int64_t)ctx->n_cu * 4),
+                                                                 total.elements / chunk + total.tensors));
     in_groups<NORM_TENSORS, Norm>(
-        n_tensors, p.chunk, false, len,
+        n_tensors, chunk, false, len,
         [&](Norm &G, int k, int64_t i) {
             G.g[k] = grad(i).d_grad;
             if (grad(i).dtype == GSPLIT_BF16) G.half.set(k);
         },
         [&](const Norm &G, bool first) {
             GsTimeScope ts(ctx, "grad_norm", -1, st);
-            hipLaunchKernelGGL(k_grad_norm, dim3(p.grid), dim3(UT), 0, st, G, ctx->norm_part, !first);
+            hipLaunchKernelGGL(k_grad_norm, dim3(grid), dim3(UT), 0, st, G, ctx->norm_part, !first);
         });
-    return p.grid;
+    if (!norm_in_one_slot(workgroups, ctx->n_cu)) return {ctx->norm_part, grid};
+    GsTimeScope ts(ctx, "sum_slots", -1, st);
+    hipLaunchKernelGGL(k_sum_slots, dim3(1), dim3(UT), 0, st, ctx->norm_part, grid);
+    return {ctx->norm_part + GS_NORM_SLOTS, 1};
 }
 
 }  // namespace
@@ -396,9 +404,10 @@ extern "C" int gsplit_grad_norm(gsplit_ctx *ctx, const gsplit_grad_tensor *t, in
         const char *e = op_check_grads(t, n_tensors, 0.0, false);
         if (!e && (!d_norm || op_misaligned(d_norm, 4))) e = "bad d_norm";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grad_norm: ") + e);
-        const int slots = launch_norm(ctx, n_tensors, [&](int64_t i) { return t[i]; }, st);
+        const Totals total = totals_of(n_tensors, [&](int64_t i) { return t[i].n; });
+        const Slots slots = launch_norm(ctx, n_tensors, total, 1, [&](int64_t i) { return t[i]; }, st);
         GsTimeScope ts(ctx, "norm_of", -1, st);
-        hipLaunchKernelGGL(k_norm_of, dim3(1), dim3(UT), 0, st, ctx->norm_part, slots, d_norm);
+        hipLaunchKernelGGL(k_norm_of, dim3(1), dim3(UT), 0, st, slots.at, slots.n, d_norm);
         return GSPLIT_OK;
     });
 }
@@ -412,11 +421,12 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
         if (!e && op_misaligned(d_norm, 4)) e = "misaligned buffer";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_clip_grads: ") + e);
         const auto len = [&](int64_t i) { return t[i].n; };
-        const Plan p = plan(ctx, n_tensors, CLIP_TENSORS, len);
-        const bool small = p.used <= CLIP_TENSORS && update_clip_small(p.total);
-        const int slots = small ? 0 : launch_norm(ctx, n_tensors, [&](int64_t i) { return t[i]; }, st);
+        const Totals total = totals_of(n_tensors, len);
+        const bool small = total.tensors <= CLIP_TENSORS && update_clip_small(total.elements);
+        const int chunk = update_chunk(total.elements, ctx->n_cu);
+        const Slots slots = small ? Slots{nullptr, 0} : launch_norm(ctx, n_tensors, total, total.elements / chunk, [&](int64_t i) { return t[i]; }, st);
         in_groups<CLIP_TENSORS, Clip>(
-            n_tensors, p.chunk, true, len,
+            n_tensors, chunk, true, len,
             [&](Clip &G, int k, int64_t i) {
                 G.g[k] = t[i].d_grad;
                 G.out[k] = t[i].d_out ? t[i].d_out : (void *)t[i].d_grad;
@@ -426,7 +436,7 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
                 GsTimeScope ts(ctx, "clip_grads", -1, st);
                 float *norm = first ? d_norm : nullptr;
                 if (small) hipLaunchKernelGGL(k_clip_small, dim3(1), dim3(ST), 0, st, G, (float)max_norm, norm);
-                else hipLaunchKernelGGL(k_clip, dim3(p.grid), dim3(UT), 0, st, G, ctx->norm_part, slots, (float)max_norm, norm);
+                else hipLaunchKernelGGL(k_clip, dim3(std::max(1, G.at.count())), dim3(UT), 0, st, G, slots.at, slots.n, (float)max_norm, norm);
             });
         return GSPLIT_OK;
     });
@@ -441,17 +451,18 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
         if (!e && op_misaligned(d_norm, 4)) e = "misaligned buffer";
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_adamw_step: ") + e);
         const auto len = [&](int64_t i) { return t[i].n; };
-        const Plan p = plan(ctx, n_tensors, ADAMW_TENSORS, len);
-        const bool here = c->max_norm > 0.0 && p.used <= ADAMW_TENSORS && update_norm_here(p.total);
-        int slots = 0;
-        if (c->max_norm > 0.0 && !here)
-            slots = launch_norm(ctx, n_tensors, [&](int64_t i) {
+        const Totals total = totals_of(n_tensors, len);
+        const bool clip = c->max_norm > 0.0, here = clip && total.tensors <= ADAMW_TENSORS && update_norm_here(total.elements);
+        const int chunk = update_chunk(total.elements, ctx->n_cu);
+        Slots slots{nullptr, 0};
+        if (clip && !here)
+            slots = launch_norm(ctx, n_tensors, total, total.elements / chunk, [&](int64_t i) {
                 return gsplit_grad_tensor{t[i].d_grad, nullptr, t[i].n, t[i].grad_dtype};
             }, st);
         const Hyper H{c->lr, c->beta1, c->beta2, c->weight_decay, c->step, c->d_step, c->d_lr, (float)c->eps, (float)c->max_norm};
         const Steps S = c->d_step || c->d_lr ? Steps{} : steps_of(H, H.lr, (double)H.step);
         in_groups<ADAMW_TENSORS, Adamw>(
-            n_tensors, p.chunk, true, len,
+            n_tensors, chunk, true, len,
             [&](Adamw &A, int k, int64_t i) {
                 A.p[k] = t[i].d_param; A.master[k] = t[i].d_master; A.g[k] = t[i].d_grad; A.m[k] = t[i].d_m; A.v[k] = t[i].d_v;
                 if (t[i].param_dtype == GSPLIT_BF16) A.half_p.set(k);
@@ -459,8 +470,9 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
             },
             [&](const Adamw &A, bool first) {
                 GsTimeScope ts(ctx, "adamw", -1, st);
-                const auto kernel = here ? k_adamw<NORM_HERE, ST> : slots ? k_adamw<NORM_SLOTS, UT> : k_adamw<NORM_NONE, UT>;
-                hipLaunchKernelGGL(kernel, dim3(p.grid), dim3(here ? ST : UT), 0, st, A, H, S, ctx->norm_part, slots, first ? d_norm : nullptr);
+                const auto kernel = here ? k_adamw<NORM_HERE, ST> : clip ? k_adamw<NORM_SLOTS, UT> : k_adamw<NORM_NONE, UT>;
+                hipLaunchKernelGGL(kernel, dim3(std::max(1, A.at.count())), dim3(here ? ST : UT), 0, st, A, H, S, slots.at, slots.n,
+                                   first ? d_norm : nullptr);
             });
         return GSPLIT_OK;
     });

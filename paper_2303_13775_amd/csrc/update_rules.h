@@ -3,15 +3,26 @@
 
 #include <cstdint>
 
-// Elements of a chunk, which a workgroup takes at a time: four workgroups of 256 threads a compute unit while that leaves each thread
-// at least four elements, then up to 16384 (250 M elements of the update 1735 us, with 4096 1715, with 65536 1782; 387 gradients of
-// 400 M elements clipped 680, 694, 720).
-inline int update_chunk(int64_t total, int n_cu) {
+// Elements of a chunk of the norm, which workgroups of 256 threads that stay, four a compute unit, take one after the other: from four
+// elements a thread up to 8192 a chunk.
+inline int norm_chunk(int64_t total, int n_cu) {
     int64_t chunk = 1024;
-    while (chunk < 16384 && chunk * 4 * n_cu < total) chunk *= 2;
+    while (chunk < 8192 && chunk * 4 * n_cu < total) chunk *= 2;
     while (total / chunk > (1 << 30)) chunk *= 2;
     return (int)chunk;
 }
+// Elements of a chunk of the passes that write, a workgroup of 256 threads each: as many as give a compute unit four, up to 4096, sixteen
+// a thread.  Workgroups that stay, four a compute unit, are slower (250 M elements of the update 1477 us, 1629; 400 M gradients
+// clipped 612, 679), and so are longer and shorter chunks (8192: 1538, 620; 2048: 1507, 654).
+inline int update_chunk(int64_t total, int n_cu) {
+    int64_t chunk = 1024;
+    while (chunk < 4096 && chunk * 4 * n_cu < total) chunk *= 2;
+    while (total / chunk > (1 << 23)) chunk *= 2;       // (a launch has less than 2^32 threads)
+    return (int)chunk;
+}
+// A pass of many workgroups reads the norm from one slot, which a launch of its own forms, instead of all of them (400 M gradients
+// clipped 612 us, 636).
+inline bool norm_in_one_slot(int64_t workgroups, int n_cu) { return workgroups > 8 * n_cu; }
 
 // Norm and clipping in one launch of one workgroup of 1024 threads, against two launches: 10 k elements 5.4 us / 8.6, 20 k 6.6 / 8.7,
 // 40 k 8.4 / 8.7, 65 k 11.4 / 8.7.
