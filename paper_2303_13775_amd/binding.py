@@ -334,6 +334,7 @@ class GatParams:
         self.c = _GatParams(GSPLIT_F32, self._dims, self._heads, *self._ptrs)
 
 
+_F32 = torch.float32
 _DTYPES = {torch.float32: GSPLIT_F32, torch.bfloat16: GSPLIT_BF16}
 
 
@@ -392,10 +393,6 @@ class AdamwTensors:
             _AdamwTensor(p.data_ptr(), None if w is None else w.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
                          p.numel(), _DTYPES[p.dtype], _DTYPES[g.dtype])
             for p, g, a, b, w in zip(params, grads, m, v, masters)])
-
-
-def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
 
 
 class Context:
@@ -591,22 +588,36 @@ class Context:
         # (the raw handle: torch.cuda.current_stream() builds a Stream object, 2 us of a call that takes 7)
         return torch._C._cuda_getCurrentRawStream(self.device.index)
 
-    def _check_rows(self, logits, grad_logits, actions, per_row):
-        """(dtype, rows, classes, logits stride, gradient stride)"""
-        assert logits.dim() == 2 and logits.dtype in _DTYPES
-        dev, dt = self.device, _DTYPES[logits.dtype]
+    # (a small call is the host's time: one pass over the tensors checks them and takes their addresses)
+    def _vectors(self, tensors, n):
+        """Addresses of float32 vectors of n values (None: absent)."""
+        dev, out = self.device.index, []
+        for t in tensors:
+            if t is None:
+                out.append(None)
+            else:
+                assert t.dtype is _F32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev
+                out.append(t.data_ptr())
+        return out
+
+    def _rows(self, logits, grad_logits, actions):
+        """(dtype, rows, classes, logits stride, address of the gradient, its stride)"""
+        dt = _DTYPES.get(logits.dtype)
+        assert dt is not None and logits.dim() == 2
+        dev = self.device.index
         rows, classes = logits.shape
         ld, step = logits.stride()
-        assert logits.device == dev and (step == 1 or classes == 1)
-        assert actions.dtype is torch.int64 and actions.device == dev and actions.is_contiguous() and actions.numel() == rows
-        for t in per_row:
-            assert t is None or (t.dtype is torch.float32 and t.device == dev and t.is_contiguous() and t.numel() == rows)
-        gld = classes
+        assert (step == 1 or classes == 1) and logits.get_device() == dev
+        assert actions.dtype is torch.int64 and actions.numel() == rows and actions.is_contiguous() and actions.get_device() == dev
+        grad, gld = None, classes
         if grad_logits is not None:
+            assert grad_logits.dtype is logits.dtype and grad_logits.shape == logits.shape and grad_logits.get_device() == dev
             gld, step = grad_logits.stride()
-            assert grad_logits.shape == logits.shape and grad_logits.dtype is logits.dtype
-            assert grad_logits.device == dev and (step == 1 or classes == 1)
-        return (dt, rows, classes, ld, gld) if rows > 1 else (dt, rows, classes, classes, classes)  # (one row: any stride)
+            assert step == 1 or classes == 1
+            grad = grad_logits.data_ptr()
+        if rows <= 1:
+            ld = gld = classes          # (one row: any stride)
+        return dt, rows, classes, ld, grad, gld
 
     def gsplit_policy_loss(self, logits: torch.Tensor, actions: torch.Tensor, old_logp: torch.Tensor,
                            advantages: torch.Tensor, grad_logits: Optional[torch.Tensor],
@@ -615,14 +626,12 @@ class Context:
                            row_loss: Optional[torch.Tensor] = None, row_logp: Optional[torch.Tensor] = None,
                            row_kl: Optional[torch.Tensor] = None):
         """Clipped policy loss with a KL term of every row of logits, and its gradient."""
-        assert old_logp is not None and advantages is not None
-        dt, rows, classes, ld, gld = self._check_rows(
-            logits, grad_logits, actions, (old_logp, advantages, ref_logp, row_weight, row_loss, row_logp, row_kl))
-        cfg = _PolicyConfig(dt, clip_low, clip_high, kl_coef)
-        self._check(self.lib.gsplit_policy_loss(
-            self.h, C.byref(cfg), logits.data_ptr(), rows, classes, ld, actions.data_ptr(), old_logp.data_ptr(),
-            _ptr(ref_logp), advantages.data_ptr(), _ptr(row_weight), _ptr(grad_logits), gld, _ptr(row_loss),
-            _ptr(row_logp), _ptr(row_kl), self._own_stream()))
+        dt, rows, classes, ld, grad, gld = self._rows(logits, grad_logits, actions)
+        old, adv, ref, w, loss, logp, kl = self._vectors((old_logp, advantages, ref_logp, row_weight, row_loss, row_logp, row_kl), rows)
+        rc = self.lib.gsplit_policy_loss(self.h, C.byref(_PolicyConfig(dt, clip_low, clip_high, kl_coef)), logits.data_ptr(), rows,
+                                         classes, ld, actions.data_ptr(), old, ref, adv, w, grad, gld, loss, logp, kl, self._own_stream())
+        if rc:
+            self._check(rc)
 
     def gsplit_preference_loss(self, logits: torch.Tensor, actions: torch.Tensor, seq_ptr: torch.Tensor,
                                grad_logits: Optional[torch.Tensor], row_work: torch.Tensor,
@@ -632,32 +641,30 @@ class Context:
                                row_logp: Optional[torch.Tensor] = None):
         """Preference loss of pairs of sequences of rows (2 p preferred to 2 p + 1), and its gradient.
         row_work: float32, 4 values a row."""
-        dt, rows, classes, ld, gld = self._check_rows(logits, grad_logits, actions, (row_logp,))
-        assert seq_ptr.device == self.device and seq_ptr.dtype == torch.int64 and seq_ptr.is_contiguous()
-        assert seq_ptr.numel() % 2 == 1
-        pairs = seq_ptr.numel() // 2
-        for t, n in ((ref_logp, 2 * pairs), (pair_weight, pairs), (pair_loss, pairs), (pair_margin, pairs),
-                     (row_work, 4 * rows)):
-            assert t is None or (t.device == self.device and t.dtype == torch.float32 and t.is_contiguous()
-                                 and t.numel() == n)
-        cfg = _PreferenceConfig(dt, beta, label_smoothing)
-        self._check(self.lib.gsplit_preference_loss(
-            self.h, C.byref(cfg), logits.data_ptr(), rows, classes, ld, actions.data_ptr(), seq_ptr.data_ptr(), pairs,
-            _ptr(ref_logp), _ptr(pair_weight), _ptr(grad_logits), gld, _ptr(row_logp), _ptr(pair_loss),
-            _ptr(pair_margin), _ptr(row_work), self._own_stream()))
+        dt, rows, classes, ld, grad, gld = self._rows(logits, grad_logits, actions)
+        n = seq_ptr.numel()
+        assert n % 2 == 1 and seq_ptr.dtype is torch.int64 and seq_ptr.is_contiguous() and seq_ptr.get_device() == self.device.index
+        w, loss, margin = self._vectors((pair_weight, pair_loss, pair_margin), n // 2)
+        ref, = self._vectors((ref_logp,), n - 1)
+        logp, = self._vectors((row_logp,), rows)
+        work, = self._vectors((row_work,), 4 * rows)
+        rc = self.lib.gsplit_preference_loss(self.h, C.byref(_PreferenceConfig(dt, beta, label_smoothing)), logits.data_ptr(), rows,
+                                             classes, ld, actions.data_ptr(), seq_ptr.data_ptr(), n // 2, ref, w, grad, gld, logp, loss,
+                                             margin, work, self._own_stream())
+        if rc:
+            self._check(rc)
 
-    def _check_table(self, table, norm):
-        assert table.device in (None, self.device)
-        assert norm is None or (norm.device == self.device and norm.dtype == torch.float32 and norm.numel() == 1)
+    def _table(self, table, norm):
+        """Address of the norm, for a table of this device."""
+        assert table.device is None or table.device == self.device
+        return self._vectors((norm,), 1)[0]
 
     def gsplit_grad_norm(self, grads: GradTensors, norm: torch.Tensor):
-        self._check_table(grads, norm)
-        self._check(self.lib.gsplit_grad_norm(self.h, grads.c, grads.n, _ptr(norm), self._own_stream()))
+        self._check(self.lib.gsplit_grad_norm(self.h, grads.c, grads.n, self._table(grads, norm), self._own_stream()))
 
     def gsplit_clip_grads(self, grads: GradTensors, max_norm: float, norm: Optional[torch.Tensor] = None):
         """Gradients times min(1, max_norm / their global norm) into the table's outputs."""
-        self._check_table(grads, norm)
-        self._check(self.lib.gsplit_clip_grads(self.h, grads.c, grads.n, max_norm, _ptr(norm), self._own_stream()))
+        self._check(self.lib.gsplit_clip_grads(self.h, grads.c, grads.n, max_norm, self._table(grads, norm), self._own_stream()))
 
     def gsplit_adamw_step(self, tensors: AdamwTensors, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
                           eps: float = 1e-8, weight_decay: float = 0.01, step: int = 0, max_norm: float = 0.0,
@@ -665,11 +672,12 @@ class Context:
                           lr_dev: Optional[torch.Tensor] = None):
         """AdamW step number `step` (from 1), gradients clipped to max_norm (0: as they are).  step_dev (int64)
         and lr_dev (float32): the step and the learning rate in device memory, for captured steps."""
-        self._check_table(tensors, norm)
-        assert step_dev is None or (step_dev.device == self.device and step_dev.dtype == torch.int64 and step_dev.numel() == 1)
-        assert lr_dev is None or (lr_dev.device == self.device and lr_dev.dtype == torch.float32 and lr_dev.numel() == 1)
-        cfg = _AdamwConfig(lr, beta1, beta2, eps, weight_decay, max_norm, int(step), _ptr(step_dev), _ptr(lr_dev))
-        self._check(self.lib.gsplit_adamw_step(self.h, C.byref(cfg), tensors.c, tensors.n, _ptr(norm), self._own_stream()))
+        norm = self._table(tensors, norm)
+        if step_dev is not None:
+            assert step_dev.dtype is torch.int64 and step_dev.numel() == 1 and step_dev.device == self.device
+        cfg = _AdamwConfig(lr, beta1, beta2, eps, weight_decay, max_norm, step, None if step_dev is None else step_dev.data_ptr(),
+                           self._vectors((lr_dev,), 1)[0])
+        self._check(self.lib.gsplit_adamw_step(self.h, C.byref(cfg), tensors.c, tensors.n, norm, self._own_stream()))
 
     def gsplit_presample_accumulate(self, vertex_count: Optional[torch.Tensor], edge_count: Optional[torch.Tensor]):
         # torch has no unsigned 32-bit arithmetic: int32 tensors carry the uint32 counters
