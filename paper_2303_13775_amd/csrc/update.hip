@@ -2,7 +2,7 @@
 //
 // Memory bounds all of it.  The factor needs every gradient before the first can be scaled, so gradients are read twice; the second
 // pass begins with the chunks that the first has left in the 256 MB cache.  400 M gradients of two types in 387 tensors 606 us, 3.6 GB
-// at 5.9 TB/s (a plain copy of that size 4.8); the update of 250 M 1476 us, 7.5 GB at 5.1 TB/s: eight streams of it, four read and
+// at 5.9 TB/s (a plain copy of that size 4.8); the update of 250 M 1355 us, 7.8 GB at 5.7 TB/s: eight streams of it, four read and
 // four written.  Of small calls the launches are all: 10 k gradients clipped 4.2 us on the device, the update of 206 k 3.4 + 5.3.
 #include <algorithm>
 #include <cmath>
@@ -233,9 +233,6 @@ __host__ __device__ inline Steps steps_of(const Hyper &H, double lr, double t) {
             (float)H.beta2, (float)(1.0 - H.beta2), (float)(1.0 / (1.0 - pow(H.beta2, t))), H.eps};
 }
 
-// Parameter and moments go through the caches like any other data: with the hint that they will not be read again 250 M elements
-// took 1711 us instead of 1630, then.
-
 // four elements of the gradient of either type
 template <class T>
 __device__ __forceinline__ void load4(const T *g, float *x) {
@@ -252,24 +249,27 @@ __device__ __forceinline__ void update1(float &p, float &m, float &v, float g, c
     v = S.b2 * v + S.a2 * (g * g);
     p = S.keep * p - S.rate * m / (sqrtf(v * S.root) + S.eps);
 }
-template <class T, bool HALF, int THREADS>
+// LARGE: what is read and written will not be found in the caches by the next step, and is said not to be read again.
+template <class T, bool HALF, int THREADS, bool LARGE>
 __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, float *m, float *v, int n, const Steps &S) {
-    constexpr int DEEP = 4;
+    constexpr int DEEP = 2;
     const int nv = n / 4;
+    const auto load = [](const float *from, float *x) { unpack<float>(LARGE ? load_piece(from) : load_kept(from), x); };
+    const auto store = [](float *to, const float *x) { LARGE ? store_piece(to, pack<float>(x)) : store_kept(to, pack<float>(x)); };
     const auto step = [&](int j, auto deep) {
         constexpr int D = decltype(deep)::value;
         float pp[D][4], mm[D][4], vv[D][4], gg[D][4];
 #pragma unroll
         for (int i = 0; i < D; ++i) {
             const int e = (j + i * THREADS) * 4;
-            unpack<float>(load_kept(p + e), pp[i]); unpack<float>(load_kept(m + e), mm[i]); unpack<float>(load_kept(v + e), vv[i]); load4(g + e, gg[i]);
+            load(p + e, pp[i]); load(m + e, mm[i]); load(v + e, vv[i]); load4(g + e, gg[i]);
         }
 #pragma unroll
         for (int i = 0; i < D; ++i) {
             const int e = (j + i * THREADS) * 4;
 #pragma unroll
             for (int k = 0; k < 4; ++k) update1(pp[i][k], mm[i][k], vv[i][k], gg[i][k], S);
-            store_kept(p + e, pack<float>(pp[i])); store_kept(m + e, pack<float>(mm[i])); store_kept(v + e, pack<float>(vv[i]));
+            store(p + e, pp[i]); store(m + e, mm[i]); store(v + e, vv[i]);
             if constexpr (HALF)
                 __builtin_nontemporal_store((u32x2{bf16_pair(pp[i][0], pp[i][1]), bf16_pair(pp[i][2], pp[i][3])}), (u32x2_any *)(half + e));
         }
@@ -289,7 +289,7 @@ __device__ __forceinline__ void update_run(float *p, bf16 *half, const T *g, flo
 // How the norm reaches the update: not at all, from the slots, or formed by every workgroup anew (few elements)
 enum : int { NORM_NONE, NORM_SLOTS, NORM_HERE };
 
-template <int WHENCE, int THREADS>
+template <int WHENCE, int THREADS, bool LARGE>
 __global__ __launch_bounds__(THREADS) void k_adamw(Adamw A, Hyper H, Steps S, const double *__restrict__ slots, int n_slots,
                                               float *__restrict__ norm_out) {
     __shared__ double lds[THREADS / 64];
@@ -317,12 +317,12 @@ __global__ __launch_bounds__(THREADS) void k_adamw(Adamw A, Hyper H, Steps S, co
         if (A.half_p[t]) {
             float *p = A.master[t] + at;
             bf16 *half = (bf16 *)A.p[t] + at;
-            if (A.half_g[t]) update_run<bf16, true, THREADS>(p, half, gh, m, v, n, S);
-            else update_run<float, true, THREADS>(p, half, g, m, v, n, S);
+            if (A.half_g[t]) update_run<bf16, true, THREADS, LARGE>(p, half, gh, m, v, n, S);
+            else update_run<float, true, THREADS, LARGE>(p, half, g, m, v, n, S);
         } else {
             float *p = (float *)A.p[t] + at;
-            if (A.half_g[t]) update_run<bf16, false, THREADS>(p, nullptr, gh, m, v, n, S);
-            else update_run<float, false, THREADS>(p, nullptr, g, m, v, n, S);
+            if (A.half_g[t]) update_run<bf16, false, THREADS, LARGE>(p, nullptr, gh, m, v, n, S);
+            else update_run<float, false, THREADS, LARGE>(p, nullptr, g, m, v, n, S);
         }
     }
 }
@@ -423,7 +423,7 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
         const auto len = [&](int64_t i) { return t[i].n; };
         const Totals total = totals_of(n_tensors, len);
         const bool small = total.tensors <= CLIP_TENSORS && update_clip_small(total.elements);
-        const int chunk = update_chunk(total.elements, ctx->n_cu);
+        const int chunk = update_chunk(total.elements, 4096, ctx->n_cu);
         const Slots slots = small ? Slots{nullptr, 0} : launch_norm(ctx, n_tensors, total, total.elements / chunk, [&](int64_t i) { return t[i]; }, st);
         in_groups<CLIP_TENSORS, Clip>(
             n_tensors, chunk, true, len,
@@ -453,7 +453,8 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
         const auto len = [&](int64_t i) { return t[i].n; };
         const Totals total = totals_of(n_tensors, len);
         const bool clip = c->max_norm > 0.0, here = clip && total.tensors <= ADAMW_TENSORS && update_norm_here(total.elements);
-        const int chunk = update_chunk(total.elements, ctx->n_cu);
+        const bool large = update_large(total.elements);
+        const int chunk = update_chunk(total.elements, 2048, ctx->n_cu);
         Slots slots{nullptr, 0};
         if (clip && !here)
             slots = launch_norm(ctx, n_tensors, total, total.elements / chunk, [&](int64_t i) {
@@ -470,8 +471,10 @@ extern "C" int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *c, 
             },
             [&](const Adamw &A, bool first) {
                 GsTimeScope ts(ctx, "adamw", -1, st);
-                const auto kernel = here ? k_adamw<NORM_HERE, ST> : clip ? k_adamw<NORM_SLOTS, UT> : k_adamw<NORM_NONE, UT>;
-                hipLaunchKernelGGL(kernel, dim3(std::max(1, A.at.count())), dim3(here ? ST : UT), 0, st, A, H, S, slots.at, slots.n,
+                const auto kernel = here ? k_adamw<NORM_HERE, ST, false>
+                                    : large ? clip ? k_adamw<NORM_SLOTS, UT, true> : k_adamw<NORM_NONE, UT, true>
+                                            : clip ? k_adamw<NORM_SLOTS, UT, false> : k_adamw<NORM_NONE, UT, false>;
+                hipLaunchKernelGGL(kernel, dim3(std::max(1, A.at.count())), dim3(here ? ST : UT), large ? UPDATE_LARGE_LDS : 0, st, A, H, S, slots.at, slots.n,
                                    first ? d_norm : nullptr);
             });
         return GSPLIT_OK;

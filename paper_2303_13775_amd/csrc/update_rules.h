@@ -11,15 +11,21 @@ inline int norm_chunk(int64_t total, int n_cu) {
     while (total / chunk > (1 << 30)) chunk *= 2;
     return (int)chunk;
 }
-// Elements of a chunk of the passes that write, a workgroup of 256 threads each: as many as give a compute unit four, up to 4096, sixteen
-// a thread.  Workgroups that stay, four a compute unit, are slower (250 M elements of the update 1477 us, 1629; 400 M gradients
-// clipped 612, 679), and so are longer and shorter chunks (8192: 1538, 620; 2048: 1507, 654).
-inline int update_chunk(int64_t total, int n_cu) {
+// Elements of a chunk of the passes that write, a workgroup of 256 threads each: as many as give a compute unit four, up to `most`: 4096
+// for clipping (400 M gradients 605 us; 2048 648, 8192 620), 2048 for the update (250 M elements 1355 us; 1024 1363, 4096 1445).
+// Workgroups that stay, four a compute unit, are slower (679; 1629).
+inline int update_chunk(int64_t total, int most, int n_cu) {
     int64_t chunk = 1024;
-    while (chunk < 4096 && chunk * 4 * n_cu < total) chunk *= 2;
+    while (chunk < most && chunk * 4 * n_cu < total) chunk *= 2;
     while (total / chunk > (1 << 23)) chunk *= 2;       // (a launch has less than 2^32 threads)
     return (int)chunk;
 }
+// An update whose parameters, moments and gradients (16 bytes an element) outgrow the 256 MB cache says that what it moves is not read
+// again (32 M elements 161 us, 195 without; 250 M 1441 and 1472; but 16 M 87 and 85), and its workgroups ask for LDS that they do not
+// use, so that three are on a compute unit and not eight: the memory does better with fewer places at once in each of the eight
+// streams (250 M 1355 us; eight workgroups 1410, five 1381, four 1380, two 1379).
+inline bool update_large(int64_t total) { return total > 16 << 20; }
+constexpr int UPDATE_LARGE_LDS = 52 << 10;
 // A pass of many workgroups reads the norm from one slot, which a launch of its own forms, instead of all of them (400 M gradients
 // clipped 612 us, 636).
 inline bool norm_in_one_slot(int64_t workgroups, int n_cu) { return workgroups > 8 * n_cu; }

@@ -21,7 +21,7 @@ extern "C" int chunks(I rows, int C, int n_cu) { return row_chunks(rows, C, n_cu
 extern "C" int policy_parts(I rows, int C, int piece, int n_cu) { return policy_in_parts(rows, C, piece, n_cu); }
 extern "C" int preference_parts(I rows, int C, int n_cu) { return preference_in_parts(rows, C, n_cu); }
 extern "C" int parts_held() { return GS_ROW_PARTS; }
-extern "C" int chunk(I total, int n_cu) { return update_chunk(total, n_cu); }
+extern "C" int chunk(I total, int most, int n_cu) { return update_chunk(total, most, n_cu); }
 extern "C" int chunk_norm(I total, int n_cu) { return norm_chunk(total, n_cu); }
 extern "C" int clip_small(I total) { return update_clip_small(total); }
 extern "C" int norm_here(I total) { return update_norm_here(total); }
@@ -38,7 +38,7 @@ def lib():
         L = C.CDLL(out)
     i, q = C.c_int, C.c_longlong
     for name, args in dict(form=[q, i, i, i], part=[i], whole=[q, q, i, i], chunks=[q, i, i], policy_parts=[q, i, i, i],
-                           preference_parts=[q, i, i], parts_held=[], chunk=[q, i], chunk_norm=[q, i], clip_small=[q], norm_here=[q]).items():
+                           preference_parts=[q, i, i], parts_held=[], chunk=[q, i, i], chunk_norm=[q, i], clip_small=[q], norm_here=[q]).items():
         getattr(L, name).argtypes = args
     return L
 

@@ -51,7 +51,7 @@ def test_workgroups_of_pairs():
 def test_chunks_of_the_update():
     L = R.lib()
     for total in (0, 1, 1000, 10 ** 6, 10 ** 9, 2 ** 46):
-        for c, most in ((L.chunk(total, R.N_CU), 2 ** 23), (L.chunk_norm(total, R.N_CU), 2 ** 30)):
+        for c, most in ((L.chunk(total, 4096, R.N_CU), 2 ** 23), (L.chunk(total, 2048, R.N_CU), 2 ** 23), (L.chunk_norm(total, R.N_CU), 2 ** 30)):
             assert c % 1024 == 0 and total / c <= most and c < 2 ** 31 // 16
         assert not L.clip_small(total) or total <= 32768
 
