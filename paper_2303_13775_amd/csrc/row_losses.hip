@@ -76,7 +76,7 @@ __global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
     constexpr bool IN_REGS = WAYS != STREAMED;
     using Row = std::conditional_t<WAYS == RAW, RawRow<T, LANES, E>, HeldRow<T, LANES, E>>;
     __shared__ RowStats lds[WG ? THREADS / 64 : 1];
-    __shared__ float lds_slope;
+    __shared__ float lds_row[3];        // a workgroup's row: maximum, sum, slope
     const int lane = WG ? threadIdx.x : threadIdx.x % LANES;
     constexpr int TEAMS = THREADS / LANES;
     // (no loop over rows: the compiler keeps what a loop needs in registers that the row is to have)
@@ -110,9 +110,10 @@ __global__ __launch_bounds__(THREADS) void k_policy_rows(Rows R, Policy P) {
             }
         }
         if constexpr (WG) {
-            if (threadIdx.x == 0) lds_slope = slope;
+            if (threadIdx.x == 0) { lds_row[0] = st.m; lds_row[1] = (float)st.s; lds_row[2] = slope; }
             __syncthreads();
-            slope = lds_slope;
+            st = {lds_row[0], lds_row[1]};
+            slope = lds_row[2];
         }
         if (g) {
             if (slope == 0.f) store_zeros<T, LANES>(g, R.C, lane);      // nothing moves it
