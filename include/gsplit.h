@@ -466,13 +466,14 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
  * gsplit_sage_fwd or gsplit_gat_fwd wrote (row r belongs to local_cat[L][r]) or any other model's.
  * d_grad_logits receives d loss / d logits in the same dtype, rows grad_stride elements apart: it may be
  * d_logits itself with the same stride (each row is read before it is written), may not overlap it in
- * another way, and NULL asks for the forward pass alone.  No other output may overlap anything.  d_actions [n_rows] int64.  With
+ * another way, and NULL asks for the forward pass alone.  No other output may overlap anything.
+ * d_actions [n_rows] int64.  With
  *     log p(r) = log softmax(logits of row r)[action of row r]
  * a row takes no part in the loss if its action lies outside [0, n_classes), or if all its logits are
  * -inf (no class is possible): its log p is reported as 0 and its gradient is 0.  Classes with a logit of
  * -inf have the probability 0 and the gradient 0.  NaN, and logits of +inf, make their row's results NaN.
- * Sums over a row are float, what is formed once a row is double.  Rows of the buffers' padding (columns
- * n_classes .. stride) are neither read nor written.  Asynchronous; may be captured into a graph at any
+ * A lane's part of a row's sum is float; the parts' sum, log p, its differences and the margins are double,
+ * losses and slopes float.  The buffers' padding (columns n_classes .. stride) is neither read nor written.  Asynchronous; may be captured into a graph at any
  * time.  The context lends its scratch memory: a replay of a captured call counts as a call on the
  * context (one stream at a time). */
 
@@ -482,7 +483,9 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
  *     kl(r)   = exp(delta) - delta - 1      (estimates the KL divergence from the reference, >= 0)
  * The loss is the sum of loss(r).  w = d_row_weight [n_rows], or 1 / n_rows if NULL; a row of weight 0
  * takes no part (its logits are not read, all its outputs are 0).  Where both sides of the maximum
- * are equal the gradient is that of the unclipped one.  d_ref_logp may be NULL if kl_coef is 0.  d_row_loss,
+ * are equal the gradient is that of the unclipped one.  An action with a logit of -inf has log p = -inf and
+ * rho = 0, and with a reference kl(r) = inf (with a kl_coef, loss and gradient of the row are then not finite).
+ * d_ref_logp may be NULL if kl_coef is 0.  d_row_loss,
  * d_row_logp (log p) and d_row_kl [n_rows] may be NULL; kl(r) is 0 without d_ref_logp.  EINVAL for NULL
  * inputs, n_rows < 0, n_classes out of range, strides below n_classes, an unknown dtype, addresses that are no
  * multiple of their type's size, clip_low outside [0, 1], clip_high or kl_coef negative or not finite. */
@@ -529,12 +532,12 @@ GSPLIT_API int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
  *     norm = sqrt( sum over all elements of all tensors of g^2 )   (double sums in a fixed order: the
  *            same bits on every call; stored as float)
  *     factor = norm > max_norm ? max_norm / norm : 1
- * A norm that is not finite (an infinity or a NaN among the gradients) is reported, the factor is then
- * 1 for gsplit_clip_grads, and gsplit_adamw_step leaves parameters and moments as they are.  Tensors are
+ * A norm that is not finite (an infinity or a NaN among the gradients, or more than the largest float) is
+ * reported, the factor is then 1 for gsplit_clip_grads, and gsplit_adamw_step leaves parameters and moments as they are.  Tensors are
  * dense runs of n elements at any address that is a multiple of the element's size; n may be 0 (then the
  * pointers may be NULL).  What a call writes may overlap none of its other tensors (a tensor may not be
- * listed twice), but for a gradient clipped in place.  The HOST arrays are read during the call.  Asynchronous; may be captured at any
- * time (the addresses are then fixed).  Scratch memory as for the losses above.
+ * listed twice), but for a gradient clipped in place.  The HOST arrays are read during the call.
+ * Asynchronous; may be captured at any time (the addresses are then fixed).  Scratch memory as for the losses above.
  * EINVAL for NULL or misaligned pointers, negative counts, unknown dtypes, max_norm not above 0. */
 typedef struct {
     const void *d_grad;

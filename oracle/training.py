@@ -41,7 +41,7 @@ def policy_loss(logits, actions, old_logp, advantages, *, ref_logp=None, weight=
             loss, slope = max(free, held), free if free >= held else 0.0
         if ref_logp is not None:
             d = float(ref_logp[r]) - lp
-            out["kl"][r] = np.expm1(d) - d
+            out["kl"][r] = np.inf if d == np.inf else np.expm1(d) - d
             if kl_coef:
                 loss += kl_coef * out["kl"][r]
                 slope -= kl_coef * np.expm1(d)

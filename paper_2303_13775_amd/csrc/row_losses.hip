@@ -43,6 +43,7 @@ __device__ __forceinline__ double row_logp(RowStats st, float za) { return ((dou
 
 // e^x - 1 - x without the cancellation near 0: its series up to |x| = 1 (the first term left out is 4e-9 of the value)
 __device__ __forceinline__ float exp_above_tangent(float x) {
+    if (x > 80.f) return expf(x);       // (what is missing is nothing beside it, and inf - inf is no number)
     if (fabsf(x) > 1.f) return (expf(x) - 1.f) - x;
     float y = 1.f / 39916800.f;
     const float c[] = {1.f / 3628800.f, 1.f / 362880.f, 1.f / 40320.f, 1.f / 5040.f, 1.f / 720.f, 1.f / 120.f, 1.f / 24.f, 1.f / 6.f, 0.5f};
@@ -56,7 +57,7 @@ __device__ __forceinline__ float policy_row(const Policy &P, double logp, float 
     const double d = logp - (double)old_logp;
     // an advantage above 0 gains nothing from a ratio over the upper border, one below 0 nothing from one under the lower
     const bool held = adv >= 0.f ? d > P.log_hi : d < P.log_lo;
-    const float ratio = adv == 0.f ? (float)d : expf((float)d);     // (no advantage: 0 times any ratio, NaN stays)
+    const float ratio = adv == 0.f && d > 80.0 ? 1.f : expf((float)d);      // (no advantage: 0 times a ratio that leaves the floats)
     float l = -adv * (held ? (adv >= 0.f ? P.hi : P.lo) : ratio), slope = held ? 0.f : l;
     *kl = 0.f;
     if (P.ref_logp) {

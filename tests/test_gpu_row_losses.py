@@ -175,19 +175,22 @@ def test_policy_left_out_rows_and_classes(ctx, dtype, n, C):
     assert not g0.any() and not any(t.any() for t in outs)
 
 
-@pytest.mark.parametrize("C", [47, 3000, 40000])
-def test_policy_impossible_action(ctx, C):
-    """An action whose logit is -inf: log p = -inf, ratio 0, the loss and gradient that the formula gives."""
+@pytest.mark.parametrize("n, C", [(6, 47), (6, 3000), (6, 40000), (6, 90001)])
+def test_policy_impossible_action(ctx, n, C):
+    """An action whose logit is -inf: log p = -inf, ratio 0, the loss and gradient that the formula gives; also without an advantage."""
     rng = np.random.default_rng(C)
-    z = _logits(rng, 4, C, F32)
-    a = _actions(rng, 4, C)
-    z[1, a[1]] = z[2, a[2]] = -np.inf
-    old, adv = np.full(4, -3.0, np.float32), np.array([1, 1, -1, -1], np.float32)
+    z = _logits(rng, n, C, F32)
+    a = _actions(rng, n, C)
+    for r in (1, 2, 3):
+        z[r, a[r]] = -np.inf
+    old, adv = np.full(n, -3.0, np.float32), np.array([1, 1, -1, 0, 0, -1], np.float32)
+    old[4] = -200.0             # a ratio of e^190 and no advantage
     want = T.policy_loss(z.double().numpy(), a, old, adv)
-    g, loss, logp = torch.zeros(4, C, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda")
-    ctx.gsplit_policy_loss(z.cuda(), _dev(a), _dev(old), _dev(adv), g, row_loss=loss, row_logp=logp)
-    assert logp[1].item() == logp[2].item() == -np.inf
-    assert np.allclose(loss.cpu().numpy(), want["loss"], rtol=1e-4) and not g[1].any() and not g[2].any()
+    g, loss, logp, kl = torch.zeros(n, C, device="cuda"), *(torch.zeros(n, device="cuda") for _ in range(3))
+    ctx.gsplit_policy_loss(z.cuda(), _dev(a), _dev(old), _dev(adv), g, row_loss=loss, row_logp=logp, ref_logp=_dev(old), row_kl=kl)
+    assert bool((logp[1:4] == -np.inf).all()) and bool((kl[1:4] == np.inf).all()) and bool(torch.isfinite(kl[[0, 5]]).all())
+    assert np.allclose(loss.cpu().numpy(), want["loss"], rtol=1e-4)
+    assert (g.any(1).cpu().numpy() == (want["slope"] != 0)).all() and not want["slope"][1:5].any()
 
 
 def test_policy_far_ratios(ctx):
@@ -506,6 +509,55 @@ def test_no_rows_and_refusals(ctx):
             bad()
     ctx.gsplit_policy_loss(z, a, f, f, z.clone())       # the context stays usable
     torch.cuda.synchronize()
+
+
+def test_rows_behind_32_bits_of_elements(ctx):
+    """Logits of more than 2^31 elements, whose last rows lie more than 4 GiB into the buffers: the bits of a call on those rows alone."""
+    n, C = 32800, 65537
+    z = torch.empty(n, C, dtype=BF16, device="cuda")
+    for i in range(0, n, 4100):
+        z[i:i + 4100].normal_(generator=torch.Generator(device="cuda").manual_seed(i))
+    g = torch.empty_like(z)
+    a = (torch.arange(n, device="cuda") * 7919) % C
+    old, adv = torch.full((n,), -11.0, device="cuda"), torch.ones(n, device="cuda")
+    w, logp = torch.full((n,), 0.25, device="cuda"), torch.zeros(n, device="cuda")
+    ctx.gsplit_policy_loss(z, a, old, adv, g, row_weight=w, row_logp=logp, clip_high=50.0)
+    ptr, work, plogp = torch.tensor([0, n - 300, n], device="cuda"), torch.zeros(n, 4, device="cuda"), torch.zeros(n, device="cuda")
+    for lo in (0, n - 300):         # (as many rows as take the same form)
+        few = slice(lo, lo + 300)
+        g1, logp1 = torch.zeros(300, C, dtype=BF16, device="cuda"), torch.zeros(300, device="cuda")
+        ctx.gsplit_policy_loss(z[few].clone(), a[few].clone(), old[few].clone(), adv[few].clone(), g1, row_weight=w[few].clone(), row_logp=logp1, clip_high=50.0)
+        assert torch.equal(g[few], g1) and torch.equal(logp[few], logp1) and bool(g1.any(1).all())
+    g.fill_(3.0)
+    ctx.gsplit_preference_loss(z, a, ptr, g, work, beta=1e-4, row_logp=plogp)
+    assert float((plogp - logp).abs().max()) < 1e-5
+    for r in (0, n - 301, n - 300, n - 1):
+        slope = float(work[r, 2])               # (where the call leaves it)
+        assert (slope < 0) == (r < n - 300)
+        p = torch.softmax(z[r].double(), 0)
+        p[a[r]] -= 1.0
+        assert slope and float((g[r].double() + slope * p).abs().max()) <= 2.0 ** -8 * abs(slope) + 1e-12, r
+
+
+def test_capture_with_timing_on(ctx):
+    """Calls under capture take no timing, whatever is enabled; eager ones around them do."""
+    run, outs, _ = _calls(ctx, 64, 47, F32, 2)
+    ctx.gsplit_timing_enable(True)
+    ctx.gsplit_timing_read()
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for t in outs:
+        t.fill_(9)
+    g.replay()
+    run()
+    torch.cuda.synchronize()
+    got = ctx.gsplit_timing_read()
+    ctx.gsplit_timing_enable(False)
+    assert got["policy_loss"][0] == 2 and all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
 def test_timing_labels(ctx):

@@ -138,6 +138,9 @@ def test_norm_of_values_whose_squares_leave_the_floats(ctx):
             ctx.gsplit_clip_grads(GradTensors([g]), x, norm)
             assert abs(float(norm) - want) < 2 * U * want
             assert abs(float(g[3]) * np.sqrt(n) / x - 1) < 8 * U
+    g = torch.full((100_000,), 3e38, device="cuda")         # a norm beyond the floats is not finite: nothing is scaled
+    ctx.gsplit_clip_grads(GradTensors([g]), 1.0, norm)
+    assert float(norm) == np.inf and bool((g == g[0]).all()) and float(g[0]) > 2e38
 
 
 def _adamw_case(ctx, sizes, ptypes, gtypes, *, gap=0, max_norm=0.0, step=3, seed=0, lr=1e-2, b1=0.9, b2=0.99, eps=1e-8, wd=0.05, dev=False, fresh=False):
@@ -252,6 +255,30 @@ def test_captured_steps(ctx, sizes):
             torch.cuda.synchronize()
         assert torch.equal(norm, norm_e) and all(torch.equal(a, b) for a, b in zip(clipped, want)), k
         assert all(torch.equal(a, b) for x, y in ((p, pe), (m, me), (v, ve)) for a, b in zip(x, y)), k
+
+
+def test_more_than_32_bits_of_elements(ctx):
+    """Tensors of more than 2^31 and 2^32 elements: values set near their ends are found, scaled and updated."""
+    from paper_2303_13775_amd import AdamwTensors, GradTensors
+    norm = torch.zeros(1, device="cuda")
+    n = (1 << 32) + 1001
+    g = torch.zeros(n, dtype=BF16, device="cuda")
+    at = [0, 1 << 31, (1 << 31) + 5, (1 << 32) - 1, 1 << 32, n - 1]
+    g[at] = 3.0
+    out = torch.empty_like(g)
+    ctx.gsplit_clip_grads(GradTensors([g], [out]), 1.0, norm)
+    want = 3.0 * np.sqrt(len(at))
+    assert abs(float(norm) - want) < 2 * U * want
+    assert int(torch.count_nonzero(out)) == len(at) and float((out[at].double() - 3.0 / want).abs().max()) <= 2.0 ** -8 * 3 / want
+    del g, out
+    n = (1 << 31) + 77
+    p, m, v, g = (torch.zeros(n, device="cuda") for _ in range(4))
+    at = [0, (1 << 31) - 1, 1 << 31, n - 1]
+    g[at] = 2.0
+    ctx.gsplit_adamw_step(AdamwTensors([p], [g], [m], [v]), lr=0.5, step=1, max_norm=100.0, norm=norm)
+    assert abs(float(norm) - 4.0) < 1e-6
+    for t, want in ((p, -0.5), (m, 0.2), (v, 0.004)):       # (the first step moves by lr)
+        assert int(torch.count_nonzero(t)) == len(at) and float((t[at] - want).abs().max()) < 1e-6
 
 
 def test_same_bits_every_time_and_on_another_stream(ctx):
