@@ -5,7 +5,7 @@
 // Memory bounds all of it: a row has to be read and its gradient written, some fifteen vector instructions an element go beside
 // that.  So the policy loss reads a row once: its team of lanes holds it in registers while maximum, sum and slope are formed (16
 // lanes for up to 512 classes, several rows a wave; a wave; a workgroup of up to 1024 threads, which is all registers of a compute
-// unit, for 65536 floats).  8192 x 65536 float 700 us, 5.8 TB/s of reading and writing; 16384 x 8192 176 us, 6.1 TB/s; 4095 x 50001
+// unit, for 98304 floats).  8192 x 65536 float 700 us, 5.8 TB/s of reading and writing; 16384 x 8192 176 us, 6.1 TB/s; 4095 x 50001
 // bfloat16 147 us, 5.3 TB/s.  Read twice, the second time from the caches, 16384 x 8192 takes 252.
 // The preference loss knows no row's slope before all rows of its pair are read, so it reads rows twice: 16 pairs of up to 512 rows
 // of 32768 bfloat16 classes 211 us, 1.3 GB moved at 6.1 TB/s.  (Its launches cut into groups of pairs that fit the 256 MB cache
@@ -394,6 +394,7 @@ void with_form(int form, F f) {
         case ROW_256x32: go(Int<256>{}, Int<256>{}, Int<32>{}); break;
         case ROW_256x64: go(Int<256>{}, Int<256>{}, Int<64>{}); break;
         case ROW_512x64: go(Int<512>{}, Int<512>{}, Int<64>{}); break;
+        case ROW_1024x96: go(Int<1024>{}, Int<1024>{}, Int<96>{}); break;
         case ROW_STREAMED: f(Int<1024>{}, Int<1024>{}, Int<32>{}, Int<STREAMED>{}); break;
         default:
             if constexpr (sizeof(T) == 4) {

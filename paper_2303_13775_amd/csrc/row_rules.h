@@ -5,8 +5,8 @@
 
 // lanes a row x elements a lane holds
 enum : int {
-    ROW_16x8, ROW_16x16, ROW_16x32, ROW_64x16, ROW_64x32, ROW_256x8, ROW_256x32, ROW_256x64, ROW_512x64, ROW_1024x64, ROW_512x128_RAW,
-    ROW_1024x128_RAW, ROW_STREAMED
+    ROW_16x8, ROW_16x16, ROW_16x32, ROW_64x16, ROW_64x32, ROW_256x8, ROW_256x32, ROW_256x64, ROW_512x64, ROW_1024x64, ROW_1024x96,
+    ROW_512x128_RAW, ROW_1024x128_RAW, ROW_STREAMED
 };
 
 // The form of n_rows rows of C elements, `piece` of them in 16 bytes (4: float, 8: bfloat16): the fewest lanes whose registers hold
@@ -18,7 +18,8 @@ enum : int {
 //   bfloat16 rows as they are, exponentials formed twice, in half the registers, where a compute unit then holds two rows instead
 //     of one: 2048 x 65536 94.6 / 100, 2048 x 50001 92.7 / 102; no more rows than compute units: 1 x 65536 9.2 / 7.4.  Narrower ones
 //     gain nothing: 4096 x 32768 95.1 / 91.9, 16384 x 8192 87.2 / 84.7
-//   bfloat16 rows of up to 131072 the same way against reading them twice: 1024 x 131072 107 / 118.
+//   rows in all registers of a compute unit, against reading them twice: 1024 x 70000 float 96 a lane 107 / 127, bf16 61.6 / 64.6 (as
+//     they are), 1024 x 98304 147 / 169, 80.5 / 85.4; 1024 x 131072 bf16 as they are 107 / 118.
 inline int row_form(int64_t n_rows, int C, int piece, int n_cu) {
     const int n = C / piece * piece;        // (what is behind the last whole piece has registers of its own)
     if (n <= 16 * 8) return ROW_16x8;
@@ -30,6 +31,7 @@ inline int row_form(int64_t n_rows, int C, int piece, int n_cu) {
     if (n <= 256 * 64) return ROW_256x64;
     if (n <= 512 * 64) return ROW_512x64;
     if (n <= 1024 * 64) return piece == 4 || n_rows <= n_cu ? ROW_1024x64 : ROW_512x128_RAW;
+    if (n <= 1024 * 96) return ROW_1024x96;
     return piece == 8 && n <= 1024 * 128 ? ROW_1024x128_RAW : ROW_STREAMED;
 }
 
@@ -53,9 +55,9 @@ inline int preference_whole(int64_t n_rows, int64_t n_pairs, int C, int n_cu) {
 }
 
 // Parts of a row where there are few rows: two workgroups a compute unit, parts of at least 4096 elements, at most 64 of them.
-// Policy loss, parts / whole rows: 1 x 131072 float 9.3 / 21, bf16 9.7 / 16.6, 64 x 131072 float 16 / 22.7, bf16 11.3 / 17.1; from
-// half a row a compute unit on whole rows again (250 x 131072 67 / 60).  Preference loss: 1 pair of 65536 12.4 / 28, 120 pairs
-// 39 / 47.
+// Policy loss, parts / whole rows: 1 x 131072 float 9.4 / 21.6, bf16 9.6 / 16.7, 1 x 70000 9.1 / 10.4, 9.1 / 8.9, 64 x 131072 16.3 /
+// 23.1, 11.7 / 17.2, 64 x 70000 12.5 / 12.9, 11.0 / 10.4; 100 x 131072 32.0 / 31.8, 19.2 / 18.5, 100 x 70000 16.3 / 14.5, 12.9 / 10.5.
+// Preference loss: 1 pair of 65536 12.4 / 28, 120 pairs 39 / 47.
 constexpr int GS_ROW_PARTS = 8192;      // (row, part) pairs the context's scratch holds
 inline int row_chunks(int64_t n_rows, int C, int n_cu) {
     int64_t chunks = (2 * n_cu + n_rows - 1) / n_rows;
@@ -63,5 +65,5 @@ inline int row_chunks(int64_t n_rows, int C, int n_cu) {
     if (chunks > GS_ROW_PARTS / n_rows) chunks = GS_ROW_PARTS / n_rows;
     return chunks < 1 ? 1 : chunks > 64 ? 64 : (int)chunks;
 }
-inline bool policy_in_parts(int64_t n_rows, int C, int piece, int n_cu) { return C / piece * piece > 1024 * 64 && n_rows < n_cu / 2; }
+inline bool policy_in_parts(int64_t n_rows, int C, int piece, int n_cu) { return C / piece * piece > 1024 * 64 && n_rows <= n_cu / 4; }
 inline bool preference_in_parts(int64_t n_rows, int C, int n_cu) { return C > 8192 && n_rows < n_cu; }

@@ -8,7 +8,7 @@ import tempfile
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2303_13775_amd", "csrc")
 N_CU = 256
-FORMS = ["16x8", "16x16", "16x32", "64x16", "64x32", "256x8", "256x32", "256x64", "512x64", "1024x64", "512x128_RAW", "1024x128_RAW", "STREAMED"]
+FORMS = ["16x8", "16x16", "16x32", "64x16", "64x32", "256x8", "256x32", "256x64", "512x64", "1024x64", "1024x96", "512x128_RAW", "1024x128_RAW", "STREAMED"]
 
 _SOURCE = r"""
 #include "row_rules.h"
