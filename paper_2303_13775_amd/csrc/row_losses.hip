@@ -8,9 +8,9 @@
 // unit, for 98304 floats).  8192 x 65536 float 700 us, 5.8 TB/s of reading and writing; 16384 x 8192 176 us, 6.1 TB/s; 4095 x 50001
 // bfloat16 147 us, 5.3 TB/s.  Read twice, the second time from the caches, 16384 x 8192 takes 252.
 // The preference loss knows no row's slope before all rows of its pair are read, so it reads rows twice: 16 pairs of up to 512 rows
-// of 32768 bfloat16 classes 211 us, 1.3 GB moved at 6.1 TB/s.  (Its launches cut into groups of pairs that fit the 256 MB cache
+// of 32768 bfloat16 classes 215 us, 1.29 GB moved at 6.0 TB/s.  (Its launches cut into groups of pairs that fit the 256 MB cache
 // came out slower, 225 us in groups of 180 MB, 258 of 128.)
-// Of small calls the launches are all: 1024 x 47 4.2 us on the device, 8.6 with the host.
+// Of small calls the launches are all: 1024 x 47 4.3 us on the device, 7.8 with the host.
 #include <algorithm>
 #include <cmath>
 

@@ -68,8 +68,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 
 // Squares are formed and summed in double, which holds those of every float: neither 1e30 nor 1e-30 leaves its range, and the norm
-// is the float next to the exact one.  (A conversion and a double multiply-add an element: a fifth of what the chip could do in
-// the time the elements take to come.)
+// is the float next to the exact one.  (A conversion and a double multiply-add an element do not show: 400 M elements at 6 TB/s.)
 template <class T>
 __device__ __forceinline__ double squares(u32x4 q, double s) {
     float x[PIECE<T>];
