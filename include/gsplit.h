@@ -484,7 +484,8 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
  * The loss is the sum of loss(r).  w = d_row_weight [n_rows], or 1 / n_rows if NULL; a row of weight 0
  * takes no part (its logits are not read, all its outputs are 0).  Where both sides of the maximum
  * are equal the gradient is that of the unclipped one.  An action with a logit of -inf has log p = -inf and
- * rho = 0, and with a reference kl(r) = inf (with a kl_coef, loss and gradient of the row are then not finite).
+ * rho = 0, and with a reference kl(r) = inf (with a kl_coef, loss and gradient of the row are then not finite); one that
+ * the reference rules out (d_ref_logp[r] = -inf) has kl(r) = inf too, with the slope kl_coef.
  * d_ref_logp may be NULL if kl_coef is 0.  d_row_loss,
  * d_row_logp (log p) and d_row_kl [n_rows] may be NULL; kl(r) is 0 without d_ref_logp.  EINVAL for NULL
  * inputs, n_rows < 0, n_classes out of range, strides below n_classes, an unknown dtype, addresses that are no

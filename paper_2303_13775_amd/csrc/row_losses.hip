@@ -63,7 +63,7 @@ __device__ __forceinline__ float policy_row(const Policy &P, double logp, float 
     if (P.ref_logp) {
         const float x = (float)((double)ref_logp - logp);
         *kl = exp_above_tangent(x);
-        if (P.kl_coef > 0.f) { l += P.kl_coef * *kl; slope -= P.kl_coef * (*kl + x); }
+        if (P.kl_coef > 0.f) { l += P.kl_coef * *kl; slope -= P.kl_coef * expm1f(x); }      // (kl + x, without their difference)
     }
     *loss = w * l;
     return w * slope;

@@ -199,6 +199,33 @@ def test_policy_far_ratios(ctx):
     _policy(ctx, _logits(rng, 500, 47, F32), _actions(rng, 500, 47), spread=10.0, kl=None)
 
 
+def test_policy_far_reference(ctx):
+    """References far from the policy, down to probability 0: the KL term's slope is kl_coef (1 - exp(delta)), which stays a number."""
+    rng = np.random.default_rng(17)
+    far = np.array([-np.inf, torch.finfo(F32).min, -1e8, -1e6, -1e4, -300, -90, -30, -20, -17, -5, -1.01, 1.01, 3, 9, 30], np.float32)
+    n, C, b = len(far), 47, 0.5
+    z, a = _logits(rng, n, C, F32), _actions(rng, n, C)
+    z64 = z.double().numpy()
+    lp = _chosen_logp(z64, a)
+    old, ref, adv = lp.astype(np.float32), np.where(far < -200, far, lp + far).astype(np.float32), rng.standard_normal(n).astype(np.float32)
+    w = np.ones(n, np.float32)
+    want = T.policy_loss(z64, a, old, adv, ref_logp=ref, weight=w, kl_coef=b)
+    g, loss, kl = torch.zeros(n, C, device="cuda"), *(torch.zeros(n, device="cuda") for _ in range(2))
+    ctx.gsplit_policy_loss(z.cuda(), _dev(a), _dev(old), _dev(adv), g, ref_logp=_dev(ref), row_weight=_dev(w), kl_coef=b, row_loss=loss, row_kl=kl)
+    dlp, dgrad = K.terms(z64, want["slope"])
+    ed = np.exp(ref.astype(np.float64) - lp)
+    # delta rounds by u |delta|, its exponential by that and 2 u: u (|delta| + 2) e^delta; a KL term near |delta| by u |delta| and its last
+    # steps, u (|kl| + 1) each; the loss and the slope by three roundings of their terms
+    delta = np.where(np.isfinite(ref), np.abs(ref.astype(np.float64) - lp), 0.0)
+    rel = np.where(ed > 0, K.U * (delta + 2) * ed, 0.0)
+    dkl = np.abs(ed - 1) * dlp + rel + K.U * (delta + 3)
+    K.check("kl", kl, want["kl"], dkl)
+    K.check("loss", loss, want["loss"], np.abs(adv) * dlp + b * dkl + 3 * K.U * (np.abs(adv) + np.nan_to_num(b * want["kl"], posinf=0.0)))
+    dslope = (np.abs(adv) + b * ed) * dlp + b * rel + 3 * K.U * (np.abs(adv) + b * (ed + 1))
+    assert np.isfinite(want["slope"]).all() and (np.abs(want["slope"]) > 1e-3).all()
+    K.check("grad", g, want["grad"], dgrad + dslope[:, None])
+
+
 def test_policy_gradient_against_differences(ctx):
     """The gradient against differences of the device's own loss: a step h changes the loss of a row by slope h (1 - p) + O(h^2)."""
     rng = np.random.default_rng(2)
