@@ -510,6 +510,7 @@ GSPLIT_API int gsplit_policy_loss(gsplit_ctx *ctx, const gsplit_policy_config *c
  * sums under the reference; NULL: 0):
  *     margin(p) = beta * ( (S(2p) - R(2p)) - (S(2p+1) - R(2p+1)) )
  *     loss(p)   = w(p) * ( -(1 - e) log sigmoid(margin) - e log sigmoid(-margin) ),  e = label_smoothing
+ * (a term whose factor is 0 is 0 also where the margin is infinite).
  * The loss is the sum of loss(p).  w = d_pair_weight [n_pairs], or 1 / n_pairs if NULL; the gradient of the
  * rows of a pair of weight 0 is 0.  Rows before d_seq_ptr[0] and from d_seq_ptr[2 * n_pairs] on are
  * neither read nor written, in any buffer.  d_row_logp [n_rows], d_pair_loss and d_pair_margin

@@ -75,7 +75,7 @@ def preference_loss(logits, actions, seq_ptr, *, ref_logp=None, weight=None, bet
         if w == 0.0:
             continue
         minus_log_sig = lambda x: np.logaddexp(0.0, -x)
-        out["loss"][p] = w * ((1 - smoothing) * minus_log_sig(h) + smoothing * minus_log_sig(-h))
+        out["loss"][p] = w * sum(k * minus_log_sig(x) for k, x in ((1 - smoothing, h), (smoothing, -h)) if k)
         sig = lambda x: np.exp(-np.logaddexp(0.0, -x))
         slope = beta * w * (-(1 - smoothing) * sig(-h) + smoothing * sig(h))
         for k, sign in ((0, 1.0), (1, -1.0)):

@@ -244,8 +244,9 @@ __device__ __forceinline__ float pair_row(const Pairs &Q, int64_t p, double rati
     const double w = Q.weight ? Q.weight[p] : Q.even_weight;
     if (threadIdx.x == 0) {
         const double soft = log1p(exp(-fabs(h)));
+        const auto side = [&](double k, double x) { return k == 0.0 ? 0.0 : k * (soft + fmax(x, 0.0)); };       // (the margin may be infinite)
         if (Q.margin) Q.margin[p] = (float)h;
-        if (Q.loss) Q.loss[p] = w == 0.0 ? 0.f : (float)(w * ((1.0 - e) * (soft + fmax(-h, 0.0)) + e * (soft + fmax(h, 0.0))));
+        if (Q.loss) Q.loss[p] = w == 0.0 ? 0.f : (float)(w * (side(1.0 - e, -h) + side(e, h)));
     }
     // d loss / d margin = w (e - sigmoid(-margin))
     return w == 0.0 ? 0.f : (float)((double)Q.beta * w * (e - 1.0 / (1.0 + exp(h))));

@@ -383,6 +383,19 @@ def test_preference_left_out_rows_and_classes(ctx, C):
     _preference(ctx, z, a, _ptr(lengths))
 
 
+@pytest.mark.parametrize("C", [9, 47, 3001, 20000])
+@pytest.mark.parametrize("e", [0.0, 0.25, 1.0])
+def test_preference_impossible_answers(ctx, C, e):
+    """Answers of probability 0 (an action whose logit is -inf): the rejected one's makes the margin inf, the chosen one's -inf; a term of
+    the loss whose factor is 0 is 0 whatever the margin."""
+    rng = np.random.default_rng(C)
+    z, a = _logits(rng, 12, C, F32), _actions(rng, 12, C)
+    z[3, a[3]] = -np.inf            # pair 0: the rejected answer
+    z[4, a[4]] = -np.inf            # pair 1: the chosen one
+    g = _preference(ctx, z, a, _ptr([2, 2, 2, 2, 2, 2]), e=e)[1]
+    assert bool(g[:4].any()) == (e > 0) and bool(g[4:8].any()) == (e < 1) and bool(torch.isfinite(g).all())
+
+
 def test_preference_offsets_that_make_no_sense_stay_inside(ctx):
     """Descending offsets and such outside the buffers: wrong values, but nothing outside the rows is written."""
     rng = np.random.default_rng(1)
