@@ -56,7 +56,8 @@ __device__ __forceinline__ float exp_above_tangent(float x) {
 __device__ __forceinline__ float policy_row(const Policy &P, double logp, float old_logp, float ref_logp, float adv, float w, float *loss, float *kl) {
     const double d = logp - (double)old_logp;
     // an advantage above 0 gains nothing from a ratio over the upper border, one below 0 nothing from one under the lower
-    const bool held = adv >= 0.f ? d > P.log_hi : d < P.log_lo;
+    // (no number is on neither side: it shows in the gradient as in the loss)
+    const bool held = adv >= 0.f ? d > P.log_hi : adv < 0.f && d < P.log_lo;
     const float ratio = adv == 0.f && d > 80.0 ? 1.f : expf((float)d);      // (no advantage: 0 times a ratio that leaves the floats)
     float l = -adv * (held ? (adv >= 0.f ? P.hi : P.lo) : ratio), slope = held ? 0.f : l;
     *kl = 0.f;

@@ -193,6 +193,26 @@ def test_policy_impossible_action(ctx, n, C):
     assert (g.any(1).cpu().numpy() == (want["slope"] != 0)).all() and not want["slope"][1:5].any()
 
 
+@pytest.mark.parametrize("n, C", [(12, 47), (12, 3000), (12, 40000), (12, 90001)])
+def test_policy_row_without_a_number(ctx, n, C):
+    """A NaN among what a row brings (advantage, old log p, weight) shows in its loss and in its whole gradient, on either side of the
+    clip and inside it; the other rows do not see it."""
+    rng = np.random.default_rng(C + 1)
+    z, a = _logits(rng, n, C, F32), _actions(rng, n, C)
+    logp = _chosen_logp(z.double().numpy(), a)
+    off = np.tile(np.array([1.0, -1.0, 0.01]), n // 3)              # ratios of e, 1 / e and within the clip
+    old, adv, w = (logp - off).astype(np.float32), rng.standard_normal(n).astype(np.float32), np.ones(n, np.float32)
+    adv[0:3], old[3:5], w[6:9] = np.nan, np.nan, np.nan
+    want = T.policy_loss(z.double().numpy(), a, old, adv, weight=w)
+    bad = np.isnan(want["loss"])
+    assert list(np.flatnonzero(bad)) == [0, 1, 2, 3, 4, 6, 7, 8]
+    g, loss = torch.zeros(n, C, device="cuda"), torch.zeros(n, device="cuda")
+    ctx.gsplit_policy_loss(z.cuda(), _dev(a), _dev(old), _dev(adv), g, row_weight=_dev(w), row_loss=loss)
+    assert (torch.isnan(loss).cpu().numpy() == bad).all()
+    nan = torch.isnan(g)
+    assert (nan.all(1).cpu().numpy() == bad).all() and (nan.any(1).cpu().numpy() == bad).all()
+
+
 def test_policy_far_ratios(ctx):
     """Ratios from e^-30 to e^30, on either side of an advantage."""
     rng = np.random.default_rng(8)
