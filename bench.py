@@ -106,7 +106,12 @@ class Runner:
                            sampler_blocks_per_cu=sampler_blocks_per_cu)
         if model == "gat":
             self.heads = [heads] * (w.n_layers - 1) + [1]
-            self.gat_w = workloads.gat_weights(w.dims, self.heads, seed=w.seed, device=dev)
+            if not hasattr(w, "gat_w"):         # the workload's, as GraphSAGE's are: all slots train one model
+                w.gat_w = {}
+            shape = (*w.dims, *self.heads)
+            if shape not in w.gat_w:
+                w.gat_w[shape] = workloads.gat_weights(w.dims, self.heads, seed=w.seed, device=dev)
+            self.gat_w = w.gat_w[shape]
             self.params = GatParams(w.dims, self.heads, *self.gat_w)
             self.grads = [[torch.empty_like(t) for t in lst] for lst in self.gat_w]
         else:

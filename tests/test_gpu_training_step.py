@@ -153,3 +153,45 @@ def test_bench_trains_with_the_update():
         r.ctx.close()
     finally:
         bench.Runner.with_update = False
+
+
+def _bench_model(r):
+    """The tensors that a benchmark Runner trains, one list."""
+    return [t for lst in (r.gat_w if r.model == "gat" else (r.w.w_self, r.w.w_neigh, r.w.bias)) for t in lst]
+
+
+@pytest.mark.parametrize("model", ["sage", "gat"])
+def test_bench_slots_train_one_model(model):
+    """The benchmark's schedules let several slots run the steps in turn: every step is the update of the weights that the step before
+    left, with the gradients of its own batch, and all slots go on from it."""
+    import bench
+    w = workloads.tiny(device="cuda:0")
+    bench.Runner.with_update = True
+    try:
+        slots = [bench.Runner(w, torch.device("cuda:0"), model, 4) for _ in range(3)]
+        state = [_bench_model(slots[0])] + w.moments
+        for i in range(6):
+            before = [[t.double().cpu().numpy() for t in ts] for ts in state]
+            r = slots[i % 3]
+            r.step(w.targets(i), i)
+            torch.cuda.synchronize()
+            grads = [t.double().cpu().numpy() for lst in r.grads for t in lst]
+            f = T.clip_factor(T.grad_norm(grads), 1.0)
+            for k, g in enumerate(grads):
+                want = T.adamw(before[0][k], g, before[1][k], before[2][k], lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+                               step=i + 1, factor=f)
+                for ts, x in zip(state, want):
+                    # (parameters: a step of about lr off by some roundings; moments: three roundings)
+                    tol = 1e-5 * 1e-3 + 2 ** -22 * np.max(np.abs(x)) if ts is state[0] else 1e-5 * np.max(np.abs(x))
+                    assert np.max(np.abs(ts[k].double().cpu().numpy() - x)) <= tol, (i, k)
+        assert w.updates == 6
+        for r in slots:         # and one batch has one answer, whichever slot computes it
+            r.ctx.gsplit_sample_split(w.targets(9), r.seed, 9)
+            r.load()
+            r.forward()
+        torch.cuda.synchronize()
+        assert all(torch.equal(r.logits, slots[0].logits) for r in slots)
+        for r in slots:
+            r.ctx.close()
+    finally:
+        bench.Runner.with_update = False
