@@ -60,7 +60,7 @@ def parse():
                          "not by the host's launch rate)")
     ap.add_argument("--update", action="store_true",
                     help="end every step with the update: gradients clipped to a global norm of 1 and AdamW "
-                         "(gsplit_adamw_step); not with --graph")
+                         "(gsplit_adamw_step); not with --graph or --redundancy")
     ap.add_argument("--presample", action="store_true",
                     help="measure the offline pre-sampling stage instead (sampling + counting of k_v, k_e)")
     ap.add_argument("--redundancy", action="store_true",
@@ -86,6 +86,8 @@ def parse():
     a = ap.parse_args()
     if a.update and a.graph:
         ap.error("--update changes the weights from step to step: the check of a replayed step against an eager one cannot run with it")
+    if a.update and a.redundancy:
+        ap.error("--update trains one model: --redundancy runs every mini-batch twice, whole and in parts")
     return a
 
 
