@@ -91,6 +91,17 @@ def parse():
     return a
 
 
+def one_call(model):
+    """Whether forward, loss and backward are one call."""
+    return model == "sage" and not Runner.separate_calls
+
+
+def stage_names(model):
+    """The stages of a step, in their order."""
+    train = ["sage_step"] if one_call(model) else [f"{model}_fwd", "loss_grad", f"{model}_bwd"]
+    return ["sample_split", "gather"] + train + (["update"] if Runner.with_update else [])
+
+
 class Runner:
     """Holds the device-resident inputs, the context and the preallocated outputs of a step."""
 
@@ -133,10 +144,9 @@ class Runner:
             self.table = AdamwTensors(params, [t for lst in self.grads for t in lst], *w.moments)
 
     def update(self):
-        """Clipped AdamW step of the weights, if asked for."""
-        if Runner.with_update:
-            self.w.updates += 1
-            self.ctx.gsplit_adamw_step(self.table, lr=1e-3, step=self.w.updates, max_norm=1.0)
+        """Clipped AdamW step of the weights."""
+        self.w.updates += 1
+        self.ctx.gsplit_adamw_step(self.table, lr=1e-3, step=self.w.updates, max_norm=1.0)
 
     def enable_cache(self, host_table, cache_ids, n_cache):
         self.ctx.gsplit_cache_build(host_table, cache_ids, n_cache)
@@ -175,15 +185,21 @@ class Runner:
     def _train(self):
         self.train()
 
-    def train(self):
-        """Forward, loss and backward of the current batch: one call for GraphSAGE unless told otherwise."""
-        if self.model == "sage" and not Runner.separate_calls:
+    def train(self, rec=lambda: None):
+        """Forward, loss, backward and the update (if asked for) of the current batch: forward, loss and backward are one call for
+        GraphSAGE unless told otherwise.  rec is called behind every stage."""
+        if one_call(self.model):
             self.ctx.gsplit_sage_step(self.params, self.x0, self.w.labels, self.logits, *self.grads)
         else:
             self.forward()
+            rec()
             self.loss()
+            rec()
             self.backward()
-        self.update()
+        rec()
+        if Runner.with_update:
+            self.update()
+            rec()
 
     def capture(self, stream, parts):
         """One graph per element of parts ('sample', 'train', or 'step' for both)."""
@@ -215,24 +231,15 @@ class Runner:
             self.ctx.gsplit_sage_bwd(self.params, self.glogits, *self.grads)
 
     def step(self, targets, it, events=None):
-        c = self.ctx
-        rec = (lambda k: events[k].record()) if events is not None else (lambda k: None)
-        rec(0)
-        c.gsplit_sample_split(targets, self.seed, it)
-        rec(1)
+        """events: one more than stage_names gives, recorded around the stages."""
+        left = iter(events) if events is not None else None
+        rec = (lambda: next(left).record()) if events is not None else (lambda: None)
+        rec()
+        self.ctx.gsplit_sample_split(targets, self.seed, it)
+        rec()
         self.load()
-        rec(2)
-        if self.model == "sage" and not Runner.separate_calls:
-            self.train()
-            rec(3)
-            return
-        self.forward()
-        rec(3)
-        self.loss()
-        rec(4)
-        self.backward()
-        self.update()
-        rec(5)
+        rec()
+        self.train(rec)
 
 
 class Pipelined:
@@ -672,14 +679,15 @@ def redundancy_bench(a, w, dev, t_gen):
     print(json.dumps(out))
 
 
-def algorithmic_work(w, model, heads, rows, edges, mixed, row_bytes, ip_bytes, S):
+def algorithmic_work(w, model, heads, rows, edges, mixed, row_bytes, ip_bytes, S, n_params=0):
     """Algorithmic bytes / flops of one launch of every kernel of a step, from the live sizes of a batch.
 
     HBM-bound rows follow the per-unit figures of the scope table: sampling = per destination vertex
     its id and two row pointers read and the count written, per sampled edge 4 bytes read and 4
     written; the kernel also makes the hash-table entries of the dedup step (one 8-byte entry per
     element in each table it enters), which are counted with it.  What a kernel moves beyond that
-    for its own bookkeeping (the entry indices every element remembers) is returned separately."""
+    for its own bookkeeping (the entry indices every element remembers) is returned separately.
+    n_params: parameters that the step updates."""
     L = w.n_layers
     work, extra = {}, {}
 
@@ -690,6 +698,10 @@ def algorithmic_work(w, model, heads, rows, edges, mixed, row_bytes, ip_bytes, S
         if io:      # a matrix product's operand and result bytes (its memory-side ceiling)
             extra["io:" + label] = io
 
+    if n_params:    # gradients for the norm; parameters and two moments read and written, gradients read; a slot per workgroup
+        add("grad_norm", "bytes", 4 * n_params)
+        add("adamw", "bytes", 28 * n_params)
+        add("sum_slots", "bytes", 8 * 1024)
     add("gather_rows", "bytes", rows[0] * (2 * row_bytes + 4))
     add("gather_cached", "bytes", rows[0] * (2 * row_bytes + 8))
     es = w.feat.element_size()
@@ -944,13 +956,11 @@ def measure(a, w, dev, *, workload, dtype, model="sage", heads=4, steps, warmup,
 
     # per-stage device times (separate instrumented pass; events on the stream the kernels run on)
     n_st = max(1, min(stage_iters, steps))
-    ev = [[torch.cuda.Event(enable_timing=True) for _ in range(6)] for _ in range(n_st)]
+    names = stage_names(model)
+    ev = [[torch.cuda.Event(enable_timing=True) for _ in range(len(names) + 1)] for _ in range(n_st)]
     for i in range(n_st):
         r.step(targets[warmup + i], warmup + i, ev[i])
     torch.cuda.synchronize()
-    names = ["sample_split", "gather", f"{model}_fwd", "loss_grad", f"{model}_bwd"]
-    if model == "sage" and not Runner.separate_calls:
-        names = ["sample_split", "gather", "sage_step"]
     stage_ms = {nm: sum(ev[i][k].elapsed_time(ev[i][k + 1]) for i in range(n_st)) / n_st for k, nm in enumerate(names)}
 
     # per-kernel device times: the library brackets each of its launches with HIP events on the
@@ -958,6 +968,7 @@ def measure(a, w, dev, *, workload, dtype, model="sage", heads=4, steps, warmup,
     L, S = w.n_layers, w.n_splits
     row_bytes = w.dims[0] * w.feat.element_size()
     ip_bytes = w.indptr.element_size()
+    n_params = sum(t.numel() for lst in r.grads for t in lst) if Runner.with_update else 0
     totals, own_totals = {}, {}
     r.ctx.gsplit_timing_enable(True)
     n_k = n_st
@@ -969,7 +980,7 @@ def measure(a, w, dev, *, workload, dtype, model="sage", heads=4, steps, warmup,
         edges = [sum(x) for x in n_edges]
         mixed = [sum(x) for x in n_mixed]
         shape = (rows, edges, mixed, bucket)
-        work, own = algorithmic_work(w, model, getattr(r, "heads", None), rows, edges, mixed, row_bytes, ip_bytes, S)
+        work, own = algorithmic_work(w, model, getattr(r, "heads", None), rows, edges, mixed, row_bytes, ip_bytes, S, n_params)
         for k, (kind, amount) in work.items():
             t = totals.setdefault(k, [kind, 0.0])
             t[1] += amount

@@ -195,3 +195,21 @@ def test_bench_slots_train_one_model(model):
             r.ctx.close()
     finally:
         bench.Runner.with_update = False
+
+
+@pytest.mark.parametrize("model, separate", [("sage", False), ("sage", True), ("gat", False)])
+def test_bench_times_the_update_by_itself(monkeypatch, model, separate):
+    """Every stage of a step has its events, the update's behind those of the backward pass."""
+    import bench
+    monkeypatch.setattr(bench.Runner, "with_update", True)
+    monkeypatch.setattr(bench.Runner, "separate_calls", separate)
+    w = workloads.tiny(device="cuda:0")
+    r = bench.Runner(w, torch.device("cuda:0"), model, 4)
+    names = bench.stage_names(model)
+    assert names[-1] == "update"
+    r.step(w.targets(0), 0)
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(len(names) + 1)]
+    r.step(w.targets(1), 1, ev)
+    torch.cuda.synchronize()
+    assert all(ev[k].elapsed_time(ev[k + 1]) > 0 for k in range(len(names))) and w.updates == 2
+    r.ctx.close()
