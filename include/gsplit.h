@@ -537,8 +537,9 @@ GSPLIT_API int gsplit_preference_loss(gsplit_ctx *ctx, const gsplit_preference_c
  * A norm that is not finite (an infinity or a NaN among the gradients, or more than the largest float) is
  * reported, the factor is then 1 for gsplit_clip_grads, and gsplit_adamw_step leaves parameters and moments as they are.  Tensors are
  * dense runs of n elements at any address that is a multiple of the element's size; n may be 0 (then the
- * pointers may be NULL).  What a call writes may overlap none of its other tensors (a tensor may not be
- * listed twice), but for a gradient clipped in place.  The HOST arrays are read during the call.
+ * pointers may be NULL).  What a call writes may overlap none of its other tensors (what is written may not be
+ * listed twice; the calls do not check it), but for a gradient clipped in place; what is only read, as all of
+ * gsplit_grad_norm's tensors, may overlap.  The HOST arrays are read during the call.
  * Asynchronous; may be captured at any time (the addresses are then fixed).  Scratch memory as for the losses above.
  * EINVAL for NULL or misaligned pointers, negative counts, unknown dtypes, max_norm not above 0. */
 typedef struct {

@@ -356,16 +356,20 @@ def _assert_apart(written, read):
 
 class GradTensors:
     """Holds the marshalled gradient tensors of gsplit_grad_norm and gsplit_clip_grads (and keeps them
-    alive).  outs: where the clipped gradients go; None, or the gradients themselves: in place."""
+    alive).  outs: where the clipped gradients go; None, or the gradients themselves: in place.  norm_only: a
+    table for gsplit_grad_norm alone, which writes none of its tensors: they may overlap, or be listed twice."""
 
-    def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+    def __init__(self, grads: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, norm_only: bool = False):
+        assert not (norm_only and outs is not None)
+        self.norm_only = norm_only
         outs = grads if outs is None else outs
         assert len(outs) == len(grads)
         self.device = _same_device([*grads, *outs])
         for g, o in zip(grads, outs):
             assert g.dtype in _DTYPES and g.is_contiguous()
             assert o.dtype == g.dtype and o.is_contiguous() and o.numel() == g.numel()
-        _assert_apart(outs, [g for g, o in zip(grads, outs) if g.data_ptr() != o.data_ptr()])
+        if not norm_only:
+            _assert_apart(outs, [g for g, o in zip(grads, outs) if g.data_ptr() != o.data_ptr()])
         self.tensors = (list(grads), list(outs))
         self.n = len(self.tensors[0])
         self.c = (_GradTensor * max(1, self.n))(*[_GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), _DTYPES[g.dtype])
@@ -664,6 +668,7 @@ class Context:
 
     def gsplit_clip_grads(self, grads: GradTensors, max_norm: float, norm: Optional[torch.Tensor] = None):
         """Gradients times min(1, max_norm / their global norm) into the table's outputs."""
+        assert not grads.norm_only
         self._check(self.lib.gsplit_clip_grads(self.h, grads.c, grads.n, max_norm, self._table(grads, norm), self._own_stream()))
 
     def gsplit_adamw_step(self, tensors: AdamwTensors, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,

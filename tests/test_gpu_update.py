@@ -327,3 +327,24 @@ def test_refusals(ctx):
     GradTensors([x[:0], x, x[:0]])
     ctx.gsplit_grad_norm(GradTensors([g]), norm)
     assert abs(float(norm) - np.sqrt(8)) < 1e-6
+
+
+@pytest.mark.parametrize("n", [500, 70_000])
+def test_norm_of_tensors_that_overlap(ctx, n):
+    """The norm writes none of its tensors: one listed twice counts twice, overlapping views count where they overlap; a table for it
+    alone is refused where its tensors would be written."""
+    from paper_2303_13775_amd import GradTensors
+    x = torch.randn(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    h = x.bfloat16()
+    ts = [x, x, x[: n // 2 + 3], x[n // 3:], h, h[1:], x[:0]]
+    table = GradTensors(ts, norm_only=True)
+    norm = torch.zeros(1, device="cuda")
+    ctx.gsplit_grad_norm(table, norm)
+    want = T.grad_norm(_np(ts))
+    assert abs(float(norm) - want) <= 1.5 * U * want
+    with pytest.raises(AssertionError):
+        ctx.gsplit_clip_grads(table, 1.0)
+    with pytest.raises(AssertionError):
+        GradTensors(ts)
+    with pytest.raises(AssertionError):
+        GradTensors([x], [torch.zeros_like(x)], norm_only=True)
