@@ -434,6 +434,42 @@ def test_preference_offsets_that_make_no_sense_stay_inside(ctx):
         assert all(bool(t[0] == 9) and bool(t[-1] == 9) for t in outs)
 
 
+# (rows, classes) of the launches over all rows, with teams of 16, 64 and 256 lanes, and of the rows in parts
+OFFSET_FORMS = [(1100, 172, 16, False), (300, 900, 64, False), (300, 9001, 256, False), (20, 20000, 256, True), (250, 9001, 256, True)]
+
+
+@pytest.mark.parametrize("n, C, lanes, parts", OFFSET_FORMS)
+@pytest.mark.parametrize("grad", ["out", "in place"])
+def test_preference_offsets_that_make_no_sense_in_several_launches(ctx, n, C, lanes, parts, grad):
+    """The same offsets where the rows' statistics, the pairs and the gradient are launches of their own: nothing around the rows of any
+    buffer is written, nothing but rows between the first and the last offset gets a gradient, and the context stays usable."""
+    import row_rules as R
+    rng = np.random.default_rng(n + C)
+    for ptr in ([-5, n // 2, n + 30], [n - 5, 3, 8], [2 ** 40, 3, -2 ** 40], [0, 2 ** 62, n], [0, -2 ** 62, n], [7, n - 3, 2, n - 1, n // 2]):
+        pairs = len(ptr) // 2
+        assert R.lib().part(C) == lanes and not R.lib().whole(n, pairs, C, R.N_CU)
+        assert bool(lanes == 256 and R.lib().preference_parts(n, C, R.N_CU)) == parts
+        z0 = _logits(rng, n, C, F32)
+        whole, z = K.rows_buffer(z0, F32, 2, 1)
+        gw, g = (whole, z) if grad == "in place" else K.rows_buffer(torch.full((n, C), 7.0), F32, 2, 1)
+        a = _actions(rng, n, C)
+        a[rng.random(n) < 0.2] = -1
+        work = torch.full((n + 2, 4), 9.0, device="cuda")
+        logp = torch.full((n + 2,), 9.0, device="cuda")
+        outs = [torch.full((pairs + 2,), 9.0, device="cuda") for _ in range(2)]
+        ctx.gsplit_preference_loss(z, _dev(a), _dev(np.array(ptr, np.int64)), g, work[1:n + 1], row_logp=logp[1:n + 1],
+                                   pair_loss=outs[0][1:pairs + 1], pair_margin=outs[1][1:pairs + 1])
+        torch.cuda.synchronize()
+        assert K.untouched(gw, g) and K.untouched(whole, z)
+        assert bool((work[0] == 9).all() and (work[n + 1] == 9).all())
+        assert all(bool(t[0] == 9) and bool(t[-1] == 9) for t in outs + [logp])
+        lo, hi = (min(max(ptr[k], 0), n) for k in (0, -1))
+        kept = z0.cuda() if grad == "in place" else torch.full((n, C), 7.0, device="cuda")
+        hi = max(lo, hi)
+        assert torch.equal(g[:lo], kept[:lo]) and torch.equal(g[hi:], kept[hi:])
+    _preference(ctx, _logits(rng, n, C, F32), _actions(rng, n, C), _ptr([n // 2, n - n // 2]))
+
+
 def test_preference_gradient_against_differences(ctx):
     rng = np.random.default_rng(6)
     lengths, C = [3, 2, 1, 4], 11
