@@ -473,7 +473,9 @@ GSPLIT_API int gsplit_softmax_xent(gsplit_ctx *ctx, const float *d_logits, int32
  * -inf (no class is possible): its log p is reported as 0 and its gradient is 0.  Classes with a logit of
  * -inf have the probability 0 and the gradient 0.  NaN, and logits of +inf, make their row's results NaN.
  * A lane's part of a row's sum is float; the parts' sum, log p, its differences and the margins are double,
- * losses and slopes float.  The buffers' padding (columns n_classes .. stride) is neither read nor written.  Asynchronous; may be captured into a graph at any
+ * losses and slopes float, and so are the exponentials: with 2^-24 = u, a class whose logit lies x below its row's
+ * largest has an e^-x that is off by up to u (3 x + 4) of itself (some 5e-7 for x = 20).  The buffers' padding
+ * (columns n_classes .. stride) is neither read nor written.  Asynchronous; may be captured into a graph at any
  * time.  The context lends its scratch memory: a replay of a captured call counts as a call on the
  * context (one stream at a time). */
 
@@ -505,7 +507,10 @@ GSPLIT_API int gsplit_policy_loss(gsplit_ctx *ctx, const gsplit_policy_config *c
 
 /* Preference loss over pairs of sequences of rows (paired log ratios).  Sequence q holds the rows
  * d_seq_ptr[q] .. d_seq_ptr[q + 1] - 1 (DEVICE [2 * n_pairs + 1] int64, ascending, values in
- * [0, n_rows]; sequences may be empty); pair p prefers sequence 2 p to sequence 2 p + 1.  With
+ * [0, n_rows]; sequences may be empty); pair p prefers sequence 2 p to sequence 2 p + 1.  So the rows of a
+ * sequence, and the two sequences of a pair, have to be neighbours.  gsplit_sage_fwd and gsplit_gat_fwd write rows in the
+ * order of local_cat[L], grouped by split: a caller whose sequences are target vertices copies their rows into the
+ * order of the sequences first, and the gradient back to d_grad_logits of the backward pass.  With
  * S(q) = the sum of log p over the rows of q that take part, and R = d_ref_logp [2 * n_pairs] (the same
  * sums under the reference; NULL: 0):
  *     margin(p) = beta * ( (S(2p) - R(2p)) - (S(2p+1) - R(2p+1)) )

@@ -213,3 +213,63 @@ def test_bench_times_the_update_by_itself(monkeypatch, model, separate):
     torch.cuda.synchronize()
     assert all(ev[k].elapsed_time(ev[k + 1]) > 0 for k in range(len(names))) and w.updates == 2
     r.ctx.close()
+
+
+@pytest.mark.parametrize("n_splits", [1, 4])
+def test_preference_of_chosen_targets(n_splits):
+    """Pairs of sequences of chosen target vertices.  The forward pass leaves its rows grouped by split: a caller brings them into the
+    order of the sequences, and the gradient back; the weights' gradients are those of the loss of these vertices."""
+    from paper_2303_13775_amd import Context, SageParams
+    w = workloads.custom(3000, 40000, dims=[32, 48, 8], fanouts=[6, 4], batch=200, n_splits=n_splits, name="pairs")
+    dev = torch.device("cuda:0")
+    ctx = Context(w.indptr.to(dev), w.indices.to(dev), w.pmap.to(dev), w.n_splits, w.fanouts, w.batch)
+    params = SageParams(w.dims, *[[t.to(dev) for t in lst] for lst in (w.w_self, w.w_neigh, w.bias)])
+    tg = w.targets(0)
+    x0 = torch.zeros((ctx.gsplit_max_rows(0), w.dims[0]), device=dev)
+    ctx.gsplit_sample_split(tg.to(dev), 11, 0)
+    ctx.gsplit_gather_features(w.feat.to(dev), x0)
+    logits = torch.zeros((w.batch, w.dims[-1]), device=dev)
+    ctx.gsplit_sage_fwd(params, x0, logits)
+    # sequences of targets in an order of their own, ten targets in none
+    rng = np.random.default_rng(3)
+    used = rng.permutation(w.batch)[:190]
+    lengths = [7, 12, 1, 30, 0, 25, 40, 75]
+    assert sum(lengths) == len(used)
+    ptr = np.concatenate([[0], np.cumsum(lengths)])
+    action = rng.integers(0, w.dims[-1], w.batch)       # of every target
+    # where each target's row is
+    cat = torch.cat(ctx.fetch_batch()["local_front"][w.n_layers]).cpu().numpy()
+    row_of = {int(v): r for r, v in enumerate(cat)}
+    rows = np.array([row_of[int(tg[k])] for k in used])
+    if n_splits > 1:
+        assert (np.diff(rows) != 1).any()
+    rows_dev = torch.from_numpy(rows).to(dev)
+    z = logits[rows_dev].contiguous()
+    g, work, loss = torch.zeros_like(z), torch.zeros((len(used), 4), device=dev), torch.zeros(4, device=dev)
+    ctx.gsplit_preference_loss(z, torch.from_numpy(action[used]).to(dev), torch.from_numpy(ptr).to(dev), g, work, beta=0.5, pair_loss=loss)
+    glog = torch.zeros_like(logits).index_copy_(0, rows_dev, g)
+    grads = [[torch.zeros_like(t) for t in lst] for lst in params.tensors]
+    ctx.gsplit_sage_bwd(params, glog, *grads)
+    torch.cuda.synchronize()
+    op = R.SageParams(*[[t.numpy() for t in lst] for lst in (w.w_self, w.w_neigh, w.bias)])
+    ob = R.sp_sample(w.indptr.numpy(), w.indices.numpy(), w.pmap.numpy(), w.n_splits, w.fanouts, tg.numpy(), 11, 0)
+    of = R.sp_forward(ob, R.gather_rows(w.feat.numpy(), ob.local_cat(0)), op)
+    # the oracle's rows by its own map from targets to rows
+    back = np.empty(w.batch, np.int64)
+    back[np.asarray(ob.target_perm)] = np.arange(w.batch)
+    z64 = logits.double().cpu().numpy()
+    assert R.max_rel_err(z64, of.logits) < TOL_F32
+    want = T.preference_loss(z64[back[used]], action[used], ptr, beta=0.5)
+    assert np.abs(loss.cpu().numpy() - want["loss"]).max() < 1e-5 * np.abs(want["loss"]).max()
+    full = np.zeros((w.batch, w.dims[-1]))
+    full[back[used]] = want["grad"]
+    assert R.max_rel_err(glog.cpu().numpy(), full) < 1e-5
+    act = [None] + [ctx.fetch_sage_activations(l, w.dims[l]).cpu().numpy() for l in range(1, w.n_layers)]
+    masks, report = R.conditioned_relu_masks(ob, of, act, 1e-5)
+    assert all(r[2] == 0 for r in report), report
+    # the weights' gradients of the gradient that the device formed
+    bw = R.sp_backward(ob, of, op, glog.double().cpu().numpy(), relu_mask=masks)
+    for got, ref in zip(grads, (bw.gw_self, bw.gw_neigh, bw.gbias)):
+        for x, y in zip(got, ref):
+            assert R.max_rel_err(x.cpu().numpy(), y) < TOL_F32
+    ctx.close()
