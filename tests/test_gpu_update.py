@@ -348,3 +348,16 @@ def test_norm_of_tensors_that_overlap(ctx, n):
         GradTensors(ts)
     with pytest.raises(AssertionError):
         GradTensors([x], [torch.zeros_like(x)], norm_only=True)
+
+
+@pytest.mark.parametrize("n", [100, 50_000])
+@pytest.mark.parametrize("eps", [1e-50, 1e-40, 1e-30])
+def test_adamw_of_an_eps_that_floats_do_not_hold(ctx, n, eps):
+    """An element without a gradient and without moments moves by its decay alone for any eps above 0: 0 / (0 + eps) is 0."""
+    from paper_2303_13775_amd import AdamwTensors
+    p, g, m, v = torch.full((n,), 0.5, device="cuda"), *(torch.zeros(n, device="cuda") for _ in range(3))
+    g[1::3] = 0.25
+    ctx.gsplit_adamw_step(AdamwTensors([p], [g], [m], [v]), lr=0.125, step=1, eps=eps, weight_decay=0.5)
+    want = torch.full((n,), 0.5 * (1 - 0.0625), device="cuda")
+    want[1::3] -= 0.125                 # the first step moves by lr
+    assert float((p - want).abs().max()) <= 10 * U * 0.125 + 2 * U * 0.5
