@@ -40,18 +40,32 @@ inline int row_part(int C) { return C <= 256 ? 16 : C <= 4096 ? 64 : 256; }
 
 // Threads of the workgroup that takes a pair of the preference loss from its rows to their gradient; 0: three launches, over all
 // rows, all pairs and all rows.  A row a team up to what fills the chip with all pairs (in us, 1024 / 256 threads: 512 pairs of
-// 2 x 32 rows of 172 17.4 / 20.9, 2048 of 2 x 16 40 / 26.6).  A workgroup pays where its teams go round a few times only (one
-// launch / three, float: 256 x 2 x 17 x 172 7.8 / 12.4, 256 x 2 x 16 x 2048 34 / 41, 1024 x 2 x 16 x 2048, eight rounds, 126 / 128,
-// 600 x 2 x 64 x 1000, 32 rounds, 209 / 156); a team that is the whole workgroup also needs pairs for the whole chip (512 x 2 x 1 x
-// 65536 123 / 135, 128 x 2 x 2 x 20000 43 / 32), or next to nothing to do.
+// 2 x 32 rows of 172 17.4 / 20.9, 2048 of 2 x 16 40 / 26.6).  The call takes as long as its longest pair at least, and the host
+// knows their mean alone: a workgroup pays where its teams go round once for a mean pair, and a few times more where there are pairs
+// enough for the long ones to come out even.  In us, float, lengths all alike / uniform from 0 / exponential / one pair of eight times the
+// others' (three launches, whatever the lengths):
+//   once        256 pairs of 32 x 172 7.7 / 8.3 / 12 / 19 (14.7), 512 of 64 x 172 18 / 21 / 28 / 37 (25), 512 of 16 x 2048 31 / 34 / 47 / 63
+//               (40), 64 of 16 x 2048 10.5 / 15 / 29 / 47 (14)
+//   twice       256 of 32 x 2048 34 / 36 / 64 / 107 (40), 128 of 32 x 2048 19 / 28 / 60 / 100 (25): launches; 1024 of 32 x 172 16 / 19 / 30 / 45
+//               (25), 2048 of 32 x 172 27 / 32 / 40 / 54 (43), 4096 of 8 x 2048 109 / 115 / 130 / 125 (138): workgroups
+//   four times  16 of 64 x 2048 29 / 43 / 83 / 137 (15), 1024 of 64 x 172 30 / 38 / 58 / 98 (40): launches; 8192 of 16 x 172 56 / 64 / 84 / 104
+//               (85), 16384 of 16 x 172 102 / 113 / 137 / 136 (157): workgroups
+//   eight       1024 of 32 x 2048 125 / 135 / 200 / 326 (130), 8192 of 32 x 47 68 / 88 / 129 / 165 (86): launches
+// Where the team is the whole workgroup its rows come one after the other: 512 pairs of 8 x 65536 547 / 757 / 1096 / 1957 (549), of 2 x
+// 65536 123 / 149 / 269 / 430 (134).  So those pairs have a row a sequence (as many rows as sequences, and pairs for the chip: 2 x 65536
+// above, alike; or narrow ones, 100 of 2 x 8000 12 / 20 / 40 / 64 (15)), or are very many (4096 of 2 x 20000 288 / 297 / 324 / 319 (345)).
 inline int preference_whole(int64_t n_rows, int64_t n_pairs, int C, int n_cu) {
     if (n_pairs >= (1 << 24)) return 0;         // (a launch has less than 2^32 threads)
     const int lanes = row_part(C);
     const int64_t rows = (n_rows + n_pairs - 1) / n_pairs;      // of a pair, on average
-    if (lanes == 256) return (n_pairs >= 2 * n_cu && rows <= 8) || rows * ((C + 8191) / 8192) <= 2 ? 256 : 0;
+    if (lanes == 256) {
+        const bool one_each = n_rows == 2 * n_pairs || n_rows <= 2;
+        return (one_each && (n_pairs >= 2 * n_cu || C <= 8192)) || (rows <= 2 && n_pairs >= 16 * n_cu) ? 256 : 0;
+    }
     const int64_t room = (int64_t)n_cu * 2048 / n_pairs, want = rows * lanes < room ? rows * lanes : room;
     const int threads = want <= 64 ? 64 : want <= 256 || room < 1024 ? 256 : 1024;
-    return rows * lanes <= 8 * threads ? threads : 0;
+    const int quarters = n_pairs < 4 * n_cu ? 5 : n_pairs < 32 * n_cu ? 8 : 16;         // of a round
+    return 4 * rows * lanes <= quarters * threads ? threads : 0;
 }
 
 // Parts of a row where there are few rows: two workgroups a compute unit, parts of at least 4096 elements, at most 64 of them.

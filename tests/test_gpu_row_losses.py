@@ -366,6 +366,20 @@ def test_preference_forms(ctx, lengths, C):
         _preference(ctx, _logits(rng, n, C, dtype), a, _ptr(lengths, 1), dtype=dtype, pad=3, gpad=3, grad="in place")
 
 
+@pytest.mark.parametrize("lengths, C", [([5, 1, 0, 0, 1, 0, 0, 1], 8191), ([0, 2, 1, 1, 0, 4, 0, 0], 4097), ([1] * 990 + [20, 14] + [0] * 32, 9001)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_preference_wide_rows_by_a_workgroup_a_pair(ctx, lengths, C, dtype):
+    """As many rows as sequences, but not one each: a workgroup takes several wide rows one after the other."""
+    import row_rules as R
+    n = int(np.sum(lengths))
+    assert n == len(lengths) and R.lib().part(C) == 256 == R.lib().whole(n, n // 2, C, R.N_CU)
+    rng = np.random.default_rng(C)
+    a = _actions(rng, n, C)
+    a[rng.random(n) < 0.2] = -1
+    _preference(ctx, _logits(rng, n, C, dtype), a, _ptr(lengths), dtype=dtype)
+    _preference(ctx, _logits(rng, n, C, dtype), a, _ptr(lengths), dtype=dtype, pad=3, gpad=3, grad="in place")
+
+
 @pytest.mark.parametrize("lengths, C", [([1, 1], 65537), ([2, 1], 131072), ([1, 0], 140001), ([3, 4, 1, 0], 50001), ([150, 160], 9001)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_preference_wide_rows(ctx, lengths, C, dtype):

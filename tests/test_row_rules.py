@@ -70,3 +70,17 @@ def test_gpu_tests_reach_every_form():
     assert got == {(16, 64), (16, 256), (16, 1024), (16, 0), (64, 64), (64, 256), (64, 1024), (64, 0), (256, 256), (256, 0)}, got
     parts = {bool(R.lib().preference_parts(n, C, R.N_CU)) for p, n, C in pairs if not R.lib().whole(n, p, C, R.N_CU) and R.lib().part(C) == 256}
     assert parts == {False, True}
+
+
+@pytest.mark.parametrize("rows, pairs, C", [(8 * 512, 512, 65536), (8 * 512, 512, 20000), (4 * 512, 512, 20000), (2 * 512 - 100, 512, 65536), (190, 100, 8000), (64 * 16, 16, 2048),
+                                            (32 * 128, 128, 2048), (32 * 256, 256, 2048), (32 * 1024, 1024, 2048), (64 * 1024, 1024, 172), (128 * 64, 64, 172)])
+def test_pairs_whose_longest_may_be_all_of_the_call(rows, pairs, C):
+    """Pairs of which one alone keeps a workgroup busy for several rounds: the host knows their mean only, a batch of ragged ones would
+    wait for the longest (512 pairs of 65536 classes, one of them with half of 4096 rows: 57.6 ms, 0.55 by three launches)."""
+    assert R.lib().whole(rows, pairs, C, R.N_CU) == 0
+
+
+@pytest.mark.parametrize("rows, pairs, C", [(2 * 512, 512, 47), (33 * 256, 256, 172), (2 * 512, 512, 65536), (2, 1, 5000), (64 * 512, 512, 172), (32 * 2048, 2048, 172),
+                                            (8 * 4096, 4096, 2048), (16 * 16384, 16384, 172), (2 * 4096, 4096, 20000), (8 * 512, 512, 172)])
+def test_pairs_of_a_workgroup_each(rows, pairs, C):
+    assert R.lib().whole(rows, pairs, C, R.N_CU)
