@@ -210,6 +210,7 @@ __global__ __launch_bounds__(UT) void k_clip(Clip G, const double *__restrict__ 
 // a chunk a wave: taken by the whole workgroup one after the other, the six tensors of 64-64-16 were twelve trips to memory in a
 // row, 10.9 us.
 constexpr int ST = 1024;
+static_assert(UPDATE_CLIP_SMALL_CHUNKS <= CLIP_TENSORS, "one launch holds them");
 __global__ __launch_bounds__(ST) void k_clip_small(Clip G, float max_norm, float *__restrict__ norm_out) {
     __shared__ double lds[ST / 64];
     const float norm = (float)sqrt(wg_sum<ST>(share_of_squares<64>(G, G.half, wave_id(), ST / 64), lds));
@@ -422,7 +423,7 @@ extern "C" int gsplit_clip_grads(gsplit_ctx *ctx, const gsplit_grad_tensor *t, i
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_clip_grads: ") + e);
         const auto len = [&](int64_t i) { return t[i].n; };
         const Totals total = totals_of(n_tensors, len);
-        const bool small = total.tensors <= CLIP_TENSORS && update_clip_small(total.elements);
+        const bool small = update_clip_small(total.elements, total.tensors);
         const int chunk = update_chunk(total.elements, 4096, ctx->n_cu);
         const Slots slots = small ? Slots{nullptr, 0} : launch_norm(ctx, n_tensors, total, total.elements / chunk, [&](int64_t i) { return t[i]; }, st);
         in_groups<CLIP_TENSORS, Clip>(

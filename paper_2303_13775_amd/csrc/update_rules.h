@@ -30,10 +30,14 @@ constexpr int UPDATE_LARGE_LDS = 52 << 10;
 // clipped 612 us, 636).
 inline bool norm_in_one_slot(int64_t workgroups, int n_cu) { return workgroups > 8 * n_cu; }
 
-// Norm and clipping in one launch of one workgroup of 1024 threads, against two launches: 10 k elements 5.4 us / 8.6, 20 k 6.6 / 8.7,
-// 40 k 8.4 / 8.7, 65 k 11.4 / 8.7.
-constexpr int UPDATE_CLIP_SMALL = 32768;
-inline bool update_clip_small(int64_t total) { return total <= UPDATE_CLIP_SMALL; }
-// The norm formed by every workgroup (of 1024 threads) of the update, against a launch of its own: 10 k elements 5.8 / 7.7, 20 k 6.4 /
-// 7.7, 40 k 7.5 / 7.7, 65 k 8.6 / 7.7.
+// Norm and clipping in one launch of one workgroup of 1024 threads, against two launches.  Its sixteen waves take a chunk each (1024
+// elements of a tensor, of which every tensor has one at least) and go round for the norm and again for clipping.  One tensor of
+// 10 k elements 5.2 us / 9.4, of 20 k 5.7 / 9.4, of 32 k 6.8 / 9.4; 16 tensors of 50 5.5 / 9.4, 32 7.7 / 9.3, 48 9.5 to 10.0 / 9.6, 72 13.7 / 9.9,
+// 144 26.4 / 10.2.  (total / 1024 + tensors: not less than the chunks)
+constexpr int UPDATE_CLIP_SMALL = 32768, UPDATE_CLIP_SMALL_CHUNKS = 48;
+inline bool update_clip_small(int64_t total, int64_t tensors = 1) {
+    return total <= UPDATE_CLIP_SMALL && total / 1024 + tensors <= UPDATE_CLIP_SMALL_CHUNKS;
+}
+// The norm formed by every workgroup (of 1024 threads) of the update, against a launch of its own: one tensor of 10 k elements 5.8 / 9.7,
+// of 20 k 5.9 / 9.9, of 32 k 6.3 / 9.9, of 65 k 8.6 / 7.7 on another card; 32 tensors of 50 7.5 / 10.0, 72 (which a launch takes) 10.5 / 10.6.
 inline bool update_norm_here(int64_t total) { return total <= 32768; }

@@ -27,6 +27,13 @@ def test_gpu_tests_reach_every_form():
 def test_borders_of_the_update():
     bar = 16 << 20
     assert R.adamw_form([bar], True)[0] == "small" and R.adamw_form([bar + 1], True)[0] == "large"
-    _, clip, adamw = R.tensors_of_a_launch()
-    assert R.clip_form([1] * clip) == ("one workgroup",) != R.clip_form([1] * (clip + 1))
+    adamw = R.tensors_of_a_launch()[2]
     assert R.adamw_form([1] * adamw, True)[2] == "norm here" != R.adamw_form([1] * (adamw + 1), True)[2]
+
+
+def test_one_workgroup_clips_few_chunks():
+    """Its waves go round once for sixteen chunks, and every tensor is one at least: 144 tensors of 50 elements took it 26 us, launches 10."""
+    for sizes in ([32768], [20480] + [50] * 16, [64 * 64, 64 * 64, 64, 64 * 16, 64 * 16, 16], [50] * 40, [0] * 500 + [7]):
+        assert R.clip_form(sizes) == ("one workgroup",), sizes
+    for sizes in ([32769], [50] * 70, [50] * 144, [1] * 60, [20480] + [50] * 60):
+        assert R.clip_form(sizes) != ("one workgroup",), sizes

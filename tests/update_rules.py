@@ -15,7 +15,7 @@ _SOURCE = r"""
 typedef long long I;
 extern "C" int chunk(I total, int most, int n_cu) { return update_chunk(total, most, n_cu); }
 extern "C" int chunk_norm(I total, int n_cu) { return norm_chunk(total, n_cu); }
-extern "C" int clip_small(I total) { return update_clip_small(total); }
+extern "C" int clip_small(I total, I tensors) { return update_clip_small(total, tensors); }
 extern "C" int norm_here(I total) { return update_norm_here(total); }
 extern "C" int large(I total) { return update_large(total); }
 extern "C" int one_slot(I workgroups, int n_cu) { return norm_in_one_slot(workgroups, n_cu); }
@@ -31,7 +31,7 @@ def _lib():
         subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, src, "-o", out], check=True)
         L = C.CDLL(out)
     i, q = C.c_int, C.c_longlong
-    for name, args in dict(chunk=[q, i, i], chunk_norm=[q, i], clip_small=[q], norm_here=[q], large=[q], one_slot=[q, i]).items():
+    for name, args in dict(chunk=[q, i, i], chunk_norm=[q, i], clip_small=[q, q], norm_here=[q], large=[q], one_slot=[q, i]).items():
         getattr(L, name).argtypes = args
     return L
 
@@ -48,7 +48,7 @@ def clip_form(sizes):
     L, (norm, clip, _) = _lib(), tensors_of_a_launch()
     full, total = [n for n in sizes if n], sum(sizes)
     chunk = L.chunk(total, 4096, N_CU)
-    if len(full) <= clip and L.clip_small(total):
+    if L.clip_small(total, len(full)):
         return ("one workgroup",)
     return ("launches", L.chunk_norm(total, N_CU), chunk, "one slot" if L.one_slot(total // chunk, N_CU) else "slots", _parts(full, norm), _parts(full, clip))
 
