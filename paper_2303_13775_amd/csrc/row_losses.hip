@@ -10,7 +10,7 @@
 // The preference loss knows no row's slope before all rows of its pair are read, so it reads rows twice: 16 pairs of up to 512 rows
 // of 32768 bfloat16 classes 215 us, 1.29 GB moved at 6.0 TB/s.  (Its launches cut into groups of pairs that fit the 256 MB cache
 // came out slower, 225 us in groups of 180 MB, 258 of 128.)
-// Of small calls the launches are all: 1024 x 47 4.3 us on the device, 7.8 with the host.
+// Of small calls the launches are all: 1024 x 47 4.3 us on the device, 7.1 to 8.2 with the host.
 #include <algorithm>
 #include <cmath>
 
