@@ -238,8 +238,7 @@ def prepare(c, seed):
     if own:
         s.ctx = _context()
         if c["op"] == "backward":
-            from paper_2303_13775_amd import grouped_linear_work
-            s.room = grouped_linear_work(s.x, s.w)
+            s.room = s.ctx.gsplit_grouped_linear_work(s.x, s.w)
         elif c["op"] == "orth":
             from paper_2303_13775_amd import MatrixTensors
             s.table = MatrixTensors(s.grads, s.outs)
