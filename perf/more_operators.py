@@ -185,7 +185,8 @@ def _prepare_grouped(s, c, seed, gen):
         s.order = None
     else:
         order = group.long().sort(stable=True)[1]
-        s.order = order[int(counts[0]):].to(torch.int32).to(dev)
+        # (those of no group behind the last one, where nobody asks for them)
+        s.order = torch.roll(order, -int(counts[0])).to(torch.int32).to(dev)
     s.sizes = counts[1:].tolist()
     s.ptr = first.to(torch.int32).to(dev)
 
