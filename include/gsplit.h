@@ -589,6 +589,53 @@ typedef struct {
 GSPLIT_API int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *config, const gsplit_adamw_tensor *tensors,
                                  int64_t n_tensors, float *d_norm, void *stream);
 
+/* Weights in stacks: a matrix for every type of vertex, task or expert, chosen for each row by its group.  Heads over the rows
+ * that gsplit_sage_fwd or gsplit_gat_fwd wrote, projections of gathered features, or any other model's layers.
+ *
+ * gsplit_group_rows sorts rows by their group: d_group [n_rows] int32; a row whose group lies outside
+ * [0, n_groups) belongs to none.  d_group_ptr [n_groups + 1] receives where each group starts, d_rows [n_rows] the rows in that
+ * order, those of a group ascending; d_rows behind d_group_ptr[n_groups] is left as it was.  n_rows < 2^31, n_groups at most
+ * GSPLIT_MAX_GROUPS.  EINVAL for NULL (d_group and d_rows may be NULL without rows) or misaligned pointers and sizes out of range.
+ * Asynchronous; may be captured at any time; scratch memory as for the losses above. */
+#define GSPLIT_MAX_GROUPS 512
+
+GSPLIT_API int gsplit_group_rows(gsplit_ctx *ctx, const int32_t *d_group, int64_t n_rows, int32_t n_groups,
+                                 int32_t *d_group_ptr, int32_t *d_rows, void *stream);
+
+/* Products of grouped rows.  For every group g and every place i of d_group_ptr[g] .. d_group_ptr[g + 1] - 1, with
+ * r = d_rows[i] (as gsplit_group_rows left them: no row twice), or r = i if d_rows is NULL (the rows lie sorted already):
+ *     y[r] = x[r] W[g] + b[g]
+ * and backward
+ *     dx[r] = dy[r] W[g]^T,   dW[g] = sum over the rows r of g of x[r]^T dy[r],   db[g] = sum of dy[r]
+ * x, dx: n_rows rows of n_in values, y, dy: of n_out, rows *_stride elements apart; W [n_groups x n_in x n_out] dense; all of
+ * type dtype.  b and db [n_groups x n_out], dW [n_groups x n_in x n_out] are float whatever the type.  Rows of no group are neither
+ * read nor written, the buffers' padding neither; a group without rows has the gradient 0.  Sums are float; float products go through
+ * the bfloat16 matrix unit in six partial products (2^-24 of each product, infinities and NaN as in float arithmetic), those of
+ * bfloat16 values are exact; y and dx are rounded once.  The sums are formed in a fixed order: the same bits on every call.
+ * d_bias may be NULL (0).  d_dx, d_dw or d_dbias may be NULL: not asked for (d_dbias needs d_dw).  No output
+ * may overlap anything.  Offsets that are not ascending or outside [0, n_rows] and rows outside it give wrong values, but no access
+ * outside the buffers.
+ * d_work: 16-byte aligned working memory of gsplit_grouped_linear_work() bytes (NULL if that is 0, or without d_dw); one call
+ * uses it at a time.  Asynchronous; may be captured at any time.
+ * EINVAL for NULL or misaligned pointers, an unknown dtype, strides below their width, n_groups above GSPLIT_MAX_GROUPS, widths
+ * outside 1 .. 2^20, n_rows outside 0 .. 2^31 - 1, a backward call that asks for nothing. */
+typedef struct {
+    int32_t dtype;
+    int32_t n_groups, n_in, n_out;
+} gsplit_grouped_config;
+
+GSPLIT_API int gsplit_grouped_linear_fwd(gsplit_ctx *ctx, const gsplit_grouped_config *config, const void *d_x, int64_t n_rows,
+                                         int64_t x_stride, const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w,
+                                         const float *d_bias, void *d_y, int64_t y_stride, void *stream);
+
+/* Bytes of working memory of the backward call; negative: an error. */
+GSPLIT_API int64_t gsplit_grouped_linear_work(gsplit_ctx *ctx, const gsplit_grouped_config *config, int64_t n_rows);
+
+GSPLIT_API int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_config *config, const void *d_x, int64_t n_rows,
+                                         int64_t x_stride, const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w,
+                                         const void *d_dy, int64_t dy_stride, void *d_dx, int64_t dx_stride, float *d_dw,
+                                         float *d_dbias, void *d_work, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

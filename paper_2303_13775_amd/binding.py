@@ -29,6 +29,7 @@ EXPORTS = [
     "gsplit_batch_shuffle", "gsplit_sage_activations", "gsplit_gat_score_terms", "gsplit_sample_split_noalloc",
     "gsplit_sample_split_multi", "gsplit_sage_step", "gsplit_gather_features_multi",
     "gsplit_policy_loss", "gsplit_preference_loss", "gsplit_grad_norm", "gsplit_clip_grads", "gsplit_adamw_step",
+    "gsplit_group_rows", "gsplit_grouped_linear_fwd", "gsplit_grouped_linear_work", "gsplit_grouped_linear_bwd",
 ]
 
 
@@ -109,6 +110,10 @@ class _AdamwConfig(C.Structure):
         ("step", C.c_int64), ("d_step", C.c_void_p), ("d_lr", C.c_void_p)]
 
 
+class _GroupedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_groups", "n_in", "n_out")]
+
+
 _lib = None
 
 
@@ -166,8 +171,13 @@ def load_library():
     L.gsplit_grad_norm.argtypes = [vp, C.POINTER(_GradTensor), i64, vp, vp]
     L.gsplit_clip_grads.argtypes = [vp, C.POINTER(_GradTensor), i64, C.c_double, vp, vp]
     L.gsplit_adamw_step.argtypes = [vp, C.POINTER(_AdamwConfig), C.POINTER(_AdamwTensor), i64, vp, vp]
+    L.gsplit_group_rows.argtypes = [vp, vp, i64, i32, vp, vp, vp]
+    L.gsplit_grouped_linear_fwd.argtypes = [vp, C.POINTER(_GroupedConfig), vp, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+    L.gsplit_grouped_linear_work.argtypes = [vp, C.POINTER(_GroupedConfig), i64]
+    L.gsplit_grouped_linear_work.restype = i64
+    L.gsplit_grouped_linear_bwd.argtypes = [vp, C.POINTER(_GroupedConfig), vp, i64, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
     for name in EXPORTS:
-        if name not in ("gsplit_last_error", "gsplit_max_rows", "gsplit_timing_read"):
+        if name not in ("gsplit_last_error", "gsplit_max_rows", "gsplit_timing_read", "gsplit_grouped_linear_work"):
             getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -683,6 +693,72 @@ class Context:
         cfg = _AdamwConfig(lr, beta1, beta2, eps, weight_decay, max_norm, step, None if step_dev is None else step_dev.data_ptr(),
                            self._vectors((lr_dev,), 1)[0])
         self._check(self.lib.gsplit_adamw_step(self.h, C.byref(cfg), tensors.c, tensors.n, norm, self._own_stream()))
+
+    def gsplit_group_rows(self, group: torch.Tensor, group_ptr: torch.Tensor, rows: torch.Tensor):
+        """Rows sorted by their group: group [n] int32 -> group_ptr [groups + 1], rows [n] int32."""
+        dev = self.device.index
+        for t in (group, group_ptr, rows):
+            assert t.dtype is torch.int32 and t.is_contiguous() and t.get_device() == dev
+        assert rows.numel() == group.numel()
+        rc = self.lib.gsplit_group_rows(self.h, group.data_ptr(), group.numel(), group_ptr.numel() - 1, group_ptr.data_ptr(),
+                                        rows.data_ptr(), self._own_stream())
+        if rc:
+            self._check(rc)
+
+    def _grouped(self, x, group_ptr, rows, w):
+        """(config, n_rows, address of the offsets, of the list of rows or None)"""
+        dt, dev = _DTYPES.get(x.dtype), self.device.index
+        assert dt is not None and x.dim() == 2 and w.dim() == 3 and w.dtype is x.dtype and w.is_contiguous() and w.get_device() == dev
+        groups, n_in, n_out = w.shape
+        assert group_ptr.dtype is torch.int32 and group_ptr.is_contiguous() and group_ptr.numel() == groups + 1 and group_ptr.get_device() == dev
+        if rows is not None:
+            assert rows.dtype is torch.int32 and rows.is_contiguous() and rows.numel() == x.shape[0] and rows.get_device() == dev
+        return _GroupedConfig(dt, groups, n_in, n_out), x.shape[0], group_ptr.data_ptr(), None if rows is None else rows.data_ptr()
+
+    def _matrix(self, t, like, width):
+        """(address, row stride) of a matrix of `like`'s rows and type."""
+        assert t.dtype is like.dtype and t.dim() == 2 and t.shape[0] == like.shape[0] and t.shape[1] == width and t.get_device() == self.device.index
+        ld, step = t.stride()
+        assert step == 1 or width == 1
+        return t.data_ptr(), ld if t.shape[0] > 1 else width
+
+    def gsplit_grouped_linear_fwd(self, x: torch.Tensor, group_ptr: torch.Tensor, rows: Optional[torch.Tensor], w: torch.Tensor,
+                                  bias: Optional[torch.Tensor], y: torch.Tensor):
+        """y[r] = x[r] W[g] + bias[g] for the rows r of every group g; rows None: they lie sorted by group."""
+        cfg, n, ptr, order = self._grouped(x, group_ptr, rows, w)
+        xp, ldx = self._matrix(x, x, cfg.n_in)
+        yp, ldy = self._matrix(y, x, cfg.n_out)
+        b, = self._vectors((bias,), cfg.n_groups * cfg.n_out)
+        rc = self.lib.gsplit_grouped_linear_fwd(self.h, C.byref(cfg), xp, n, ldx, ptr, order, w.data_ptr(), b, yp, ldy, self._own_stream())
+        if rc:
+            self._check(rc)
+
+    def gsplit_grouped_linear_work(self, x: torch.Tensor, w: torch.Tensor) -> torch.Tensor:
+        """Working memory for gsplit_grouped_linear_bwd with these rows and weights."""
+        cfg = _GroupedConfig(_DTYPES[x.dtype], *w.shape)
+        n = self.lib.gsplit_grouped_linear_work(self.h, C.byref(cfg), x.shape[0])
+        if n < 0:
+            self._check(int(n))
+        return torch.empty(n // 4, dtype=torch.float32, device=self.device)
+
+    def gsplit_grouped_linear_bwd(self, x: torch.Tensor, group_ptr: torch.Tensor, rows: Optional[torch.Tensor], w: torch.Tensor,
+                                  dy: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor],
+                                  dbias: Optional[torch.Tensor], work: Optional[torch.Tensor] = None):
+        """The gradients of gsplit_grouped_linear_fwd (None: not asked for); dw and dbias are float32."""
+        cfg, n, ptr, order = self._grouped(x, group_ptr, rows, w)
+        xp, ldx = self._matrix(x, x, cfg.n_in)
+        dyp, lddy = self._matrix(dy, x, cfg.n_out)
+        dxp, lddx = (None, 0) if dx is None else self._matrix(dx, x, cfg.n_in)
+        dwp, = self._vectors((dw,), w.numel())
+        dbp, = self._vectors((dbias,), cfg.n_groups * cfg.n_out)
+        if dw is not None:
+            need = self.lib.gsplit_grouped_linear_work(self.h, C.byref(cfg), n)
+            assert need <= 0 or (work is not None and work.is_contiguous() and work.numel() * work.element_size() >= need
+                                 and work.get_device() == self.device.index)
+        rc = self.lib.gsplit_grouped_linear_bwd(self.h, C.byref(cfg), xp, n, ldx, ptr, order, w.data_ptr(), dyp, lddy, dxp, lddx, dwp, dbp,
+                                                None if work is None else work.data_ptr(), self._own_stream())
+        if rc:
+            self._check(rc)
 
     def gsplit_presample_accumulate(self, vertex_count: Optional[torch.Tensor], edge_count: Optional[torch.Tensor]):
         # torch has no unsigned 32-bit arithmetic: int32 tensors carry the uint32 counters

@@ -23,49 +23,10 @@
 // from global memory.
 #pragma once
 
+#include "split_parts.h"
 #include "split_rules.h"
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
 constexpr int SNT = 256;                // threads of a workgroup: four waves
-constexpr int SPLIT_MIN_K = 3;          // shorter contractions are formed with fp32 MFMAs
-constexpr float SPLIT_SCALE = 0x1p16f, SPLIT_UNSCALE = 0x1p-32f;        // of an operand, of a product of two
-
-__device__ __forceinline__ uint32_t cvt2bf(float a, float b) {      // round to nearest even, a in the low half
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){a, b}, bf16x2_t));
-}
-// two values -> one word (two bfloat16) of each of the three parts
-__device__ __forceinline__ void split2(float a, float b, uint32_t &p1, uint32_t &p2, uint32_t &p3) {
-    p1 = cvt2bf(a, b);
-    a -= __uint_as_float(p1 << 16); b -= __uint_as_float(p1 & 0xFFFF0000u);
-    p2 = cvt2bf(a, b);
-    a -= __uint_as_float(p2 << 16); b -= __uint_as_float(p2 & 0xFFFF0000u);
-    p3 = cvt2bf(a, b);
-}
-__device__ __forceinline__ void split8(const float (&v)[8], uint4 (&p)[3]) {
-    split2(v[0], v[1], p[0].x, p[1].x, p[2].x);
-    split2(v[2], v[3], p[0].y, p[1].y, p[2].y);
-    split2(v[4], v[5], p[0].z, p[1].z, p[2].z);
-    split2(v[6], v[7], p[0].w, p[1].w, p[2].w);
-}
-__device__ __forceinline__ floatx16 mfma_bf(const uint4 &a, const uint4 &b, const floatx16 &c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ floatx16 zero16() {
-    floatx16 z;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) z[r] = 0.f;
-    return z;
-}
-__device__ __forceinline__ bool finite16(const floatx16 &v) {
-    bool ok = true;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) ok = ok && fabsf(v[r]) < INFINITY;
-    return ok;
-}
-
 // ---- operand laid out once per call: the weights --------------------------------------------------
 // Matrix B (k x n) as the fragments a wave feeds the MFMA: block (nb, ks) covers 32 columns x 16 k in
 // three planes of 64 lanes x 16 bytes (of the scaled values); lane l holds column 32 nb + l % 32 and the eight k of granule
@@ -76,7 +37,6 @@ __host__ __device__ inline int split_halves(int K) { return 2 * ((K + 31) / 32);
 __host__ __device__ inline int64_t split_frag_words(int K, int N) {     // 16-byte words
     return (int64_t)((N + 31) / 32) * split_halves(K) * 192;
 }
-__device__ __forceinline__ int granule_k(int g, int j) { return 4 * g + j + (j < 4 ? 0 : 12); }
 template <class Get>
 __device__ __forceinline__ void split_frag_fill(uint4 *frag, int K, int N, int64_t x, int64_t stride, const Get &get) {
     const int KS = split_halves(K);
@@ -104,24 +64,6 @@ struct SplitA { const float *p; int64_t ld; int rows; int K; };
 // B: fragments of K x N, and the matrix itself: element (k, n) at ref[k * rk + n * rn]
 struct SplitB { const uint4 *frag; const float *ref; int64_t rk, rn; int N; };
 
-// The products of k_begin .. k_end - 1 with fp32 MFMAs, sums of 16 k added up (a single chain of 64 k rounded more
-// often than the fp32 tiles whose waves each took a part of the contraction: 2.4 units of 2^-24 against 1.4).
-template <class GetA, class GetB>
-__device__ __forceinline__ floatx16 exact_sum(int k_begin, int k_end, int half, const GetA &get_a, const GetB &get_b) {
-    floatx16 sum = zero16();
-#pragma unroll 1
-    for (int k0 = k_begin; k0 < k_end; k0 += 16) {
-        floatx16 part = zero16();
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const int k = k0 + 8 * half + q;
-            part = __builtin_amdgcn_mfma_f32_32x32x2f32(get_a(k), get_b(k), part, 0, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum[r] += part[r];
-    }
-    return sum;
-}
 // one 32 x 32 block with fp32 MFMAs from global memory (non-finite results and short contractions only)
 __device__ __forceinline__ floatx16 split_exact_block(const SplitA &a, const SplitB &b, int m, int n, int half) {
     const float *ap = a.p + (int64_t)min(m, a.rows - 1) * a.ld;

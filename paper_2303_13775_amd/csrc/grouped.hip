@@ -1,0 +1,640 @@
+// Products grouped by row: y[r] = x[r] W[g] + b[g] for the rows r of every group g, and the gradients of x, W and b.
+//
+// One tile product serves all three.  A tile of BM rows x BN columns of the result goes to a workgroup of four waves, a quarter of it
+// each; the contraction is taken KT at a time: operands are fetched into registers while the matrix unit works on the tile in
+// front, and laid out in LDS as granules of eight contraction indices, the way a lane feeds the matrix unit.  An operand lies in
+// memory with the contraction along its rows (`Along`: x and dy as rows, W of the input gradient) or across them (`Across`: W of the
+// forward product, x and dy of the weight gradient); there a thread fetches the same columns of eight rows and transposes them in
+// its registers.
+// Floats go through the bfloat16 matrix unit as three parts and six products (gemm_split.h); products of bfloat16 are exact there.
+// Sums are float.
+// The columns of the result run along the matrix unit's rows: a lane then holds four consecutive columns of one row.
+#include <algorithm>
+#include <type_traits>
+
+#include "group_rules.h"
+#include "gsplit_internal.h"
+#include "op_checks.h"
+
+namespace {
+
+#include "gemm_common.h"
+#include "split_parts.h"
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// rows start at any multiple of their elements' size, which the vector loads and stores of the chip take
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+
+constexpr int NT = 256;
+
+template <class T> struct Kind;
+template <> struct Kind<float> {
+    static constexpr int PLANES = 3, KT = 32, KG = 4;       // parts of an operand, contraction of a tile, its granules
+    // contraction index j of granule g: four threads that fetch a row's granules read 64 bytes side by side
+    static __device__ __forceinline__ int k_of(int g, int j) { return granule_k(g, j); }
+    static __device__ __forceinline__ int turn(int row) { return (row >> 2) & 3; }
+};
+template <> struct Kind<uint16_t> {
+    static constexpr int PLANES = 1, KT = 64, KG = 8;
+    static __device__ __forceinline__ int k_of(int g, int j) { return 8 * g + j; }
+    static __device__ __forceinline__ int turn(int row) { return ((row >> 1) ^ (row >> 4)) & 7; }
+};
+// where granule g of a row lies: rows that are read or written side by side fall into different banks
+template <class T> __device__ __forceinline__ int slot(int row, int g) { return row * Kind<T>::KG + (g ^ Kind<T>::turn(row)); }
+
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(uint16_t x) { return bf2f(x); }
+
+// eight values of a granule -> LDS, as `planes` parts
+template <class T, int ROWS>
+__device__ __forceinline__ void land(uint4 *lds, int at, const float (&v)[8]) {
+    uint4 p[3];
+    float s[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = v[j] * SPLIT_SCALE;
+    split8(s, p);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) lds[q * ROWS * Kind<T>::KG + at] = p[q];
+}
+
+// An operand with the contraction along its rows: element (i, k) at row(i)[k]
+template <class T, int ROWS>
+struct Along {
+    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, N = ROWS * KG / NT;
+    static_assert(N * NT == ROWS * KG, "whole items");
+    const T *p[N];
+    int K;
+    typedef typename std::conditional<sizeof(T) == 4, float[8], uint4>::type Item;
+    Item r[N];
+
+    template <class Row>
+    __device__ __forceinline__ void init(int k_len, const Row &row) {
+        K = k_len;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = row(((int)threadIdx.x + i * NT) / KG);
+    }
+    __device__ __forceinline__ void load(int t) {
+        const int g = threadIdx.x % KG, k0 = t * KT;
+        if (k0 + KT <= K) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if constexpr (sizeof(T) == 4) {
+                    const u32x4 a = *(const u32x4_any *)(p[i] + k0 + 4 * g), b = *(const u32x4_any *)(p[i] + k0 + 16 + 4 * g);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { r[i][j] = __uint_as_float(a[j]); r[i][4 + j] = __uint_as_float(b[j]); }
+                } else {
+                    const u32x4 a = *(const u32x4_any *)(p[i] + k0 + 8 * g);
+                    r[i] = make_uint4(a[0], a[1], a[2], a[3]);
+                }
+            }
+        } else {            // the last tile: element by element, zeros past the end
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                T v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = p[i][min(k0 + Kind<T>::k_of(g, j), K - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (k0 + Kind<T>::k_of(g, j) >= K) v[j] = 0;
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) r[i][j] = v[j];
+                } else {
+                    r[i] = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                                      v[6] | (uint32_t)v[7] << 16);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(uint4 *lds) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int x = (int)threadIdx.x + i * NT, at = slot<T>(x / KG, x % KG);
+            if constexpr (sizeof(T) == 4) land<T, ROWS>(lds, at, r[i]);
+            else lds[at] = r[i];
+        }
+    }
+};
+
+// An operand with the contraction across its rows: element (i, k) at row(k)[i], i < cols; of these the ones from `first` on
+template <class T, int ROWS>
+struct Across {
+    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, W = ROWS * KG / NT;       // W columns of eight rows a thread
+    static_assert(W * NT == ROWS * KG && (W == 1 || W == 2 || W == 4), "one item a thread");
+    int K, cols, col, base;         // this thread's first column; LDS row of it
+    T r[8][W];
+
+    __device__ __forceinline__ void init(int k_len, int n_cols, int first) {
+        K = k_len; cols = n_cols;
+        const int want = first + (int)threadIdx.x % (ROWS / W) * W;
+        // past the last column: the last ones once more, whose granules are then written twice, with the same values
+        col = max(0, min(want, cols - W));
+        base = col - first;
+    }
+    template <class Row>
+    __device__ __forceinline__ void load(int t, const Row &row) {
+        const int g = threadIdx.x / (ROWS / W), k0 = t * KT;
+        const bool whole = k0 + KT <= K;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = k0 + Kind<T>::k_of(g, j);
+            const T *p = row(whole ? k : min(k, K - 1)) + col;
+            if (W > 1 && cols < W) {
+#pragma unroll
+                for (int c = 0; c < W; ++c) r[j][c] = p[min(c, cols - 1)];
+            } else if constexpr (W * sizeof(T) == 4) {
+                const uint32_t a = *(const u32_any *)p;
+                __builtin_memcpy(r[j], &a, 4);
+            } else if constexpr (W * sizeof(T) == 8) {
+                const u32x2 a = *(const u32x2_any *)p;
+                __builtin_memcpy(r[j], &a, 8);
+            } else {
+                r[j][0] = p[0];
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k0 + Kind<T>::k_of(g, j) >= K)
+#pragma unroll
+                    for (int c = 0; c < W; ++c) r[j][c] = 0;
+        }
+    }
+    __device__ __forceinline__ void store(uint4 *lds) const {
+        const int g = threadIdx.x / (ROWS / W);
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+            const int row = base + c;
+            if (row < 0 || row >= ROWS) continue;
+            const int at = slot<T>(row, g);
+            if constexpr (sizeof(T) == 4) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = r[j][c];
+                land<T, ROWS>(lds, at, v);
+            } else {
+                lds[at] = make_uint4(r[0][c] | (uint32_t)r[1][c] << 16, r[2][c] | (uint32_t)r[3][c] << 16,
+                                     r[4][c] | (uint32_t)r[5][c] << 16, r[6][c] | (uint32_t)r[7][c] << 16);
+            }
+        }
+    }
+};
+
+// Rows of LDS that an `Across` of a tile's last columns leaves unwritten: zeros, or what was there would decide whether the tile's
+// sums look finite.
+template <class T, int ROWS>
+__device__ __forceinline__ void clear_rows(uint4 *lds) {
+    for (int i = threadIdx.x; i < ROWS * Kind<T>::KG * Kind<T>::PLANES; i += NT) lds[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// A workgroup's tile of the result: BM rows x BN columns, waves 2 x 2
+template <int BM_, int BN_> struct Tile {
+    static constexpr int BM = BM_, BN = BN_, MI = BM / 64, NI = BN / 64;       // blocks of 32 x 32 of a wave
+};
+
+template <class T, class TL>
+struct Sums {
+    floatx16 hi[TL::NI][TL::MI], lo[sizeof(T) == 4 ? TL::NI : 1][sizeof(T) == 4 ? TL::MI : 1];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int n = 0; n < TL::NI; ++n)
+#pragma unroll
+            for (int m = 0; m < TL::MI; ++m) {
+                hi[n][m] = zero16();
+                if constexpr (sizeof(T) == 4) lo[n][m] = zero16();
+            }
+    }
+    // one tile of the contraction: rows (the result's) in a, columns in b
+    __device__ __forceinline__ void multiply(const uint4 *a, const uint4 *b) {
+        constexpr int KG = Kind<T>::KG, P = Kind<T>::PLANES;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+        const int wm = (wave & 1) * (TL::BM / 2), wn = (wave >> 1) * (TL::BN / 2);
+#pragma unroll
+        for (int s = 0; s < KG / 2; ++s) {
+            uint4 fa[TL::MI][P], fb[TL::NI][P];
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+#pragma unroll
+                for (int m = 0; m < TL::MI; ++m) fa[m][q] = a[q * TL::BM * KG + slot<T>(wm + 32 * m + l32, 2 * s + half)];
+#pragma unroll
+                for (int n = 0; n < TL::NI; ++n) fb[n][q] = b[q * TL::BN * KG + slot<T>(wn + 32 * n + l32, 2 * s + half)];
+            }
+#pragma unroll
+            for (int n = 0; n < TL::NI; ++n)
+#pragma unroll
+                for (int m = 0; m < TL::MI; ++m) {
+                    hi[n][m] = mfma_bf(fb[n][0], fa[m][0], hi[n][m]);
+                    if constexpr (P == 3) {
+                        lo[n][m] = mfma_bf(fb[n][0], fa[m][2], lo[n][m]);
+                        lo[n][m] = mfma_bf(fb[n][0], fa[m][1], lo[n][m]);
+                        lo[n][m] = mfma_bf(fb[n][1], fa[m][0], lo[n][m]);
+                        lo[n][m] = mfma_bf(fb[n][1], fa[m][1], lo[n][m]);
+                        lo[n][m] = mfma_bf(fb[n][2], fa[m][0], lo[n][m]);
+                    }
+                }
+        }
+    }
+    // Calls f(row of the tile, first of four consecutive columns, their values) for all of them.  Values that the parts of floats
+    // cannot carry (infinities, NaN, very large ones) have made a sum that is not finite: a wave that finds one, and contractions
+    // of one or two products, are formed again with the float matrix instructions, block by block.
+    // a(i, k), b(i, k): element of row / column i of the tile, 0 past the contraction's end
+    template <class GetA, class GetB, class F>
+    __device__ __forceinline__ void finish(int K, const GetA &a, const GetB &b, const F &f) {
+        int lane = threadIdx.x & 63;
+        const int wave = threadIdx.x >> 6, wm = (wave & 1) * (TL::BM / 2), wn = (wave >> 1) * (TL::BN / 2);
+        const auto block = [&](int m, int n, const floatx16 &x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                f(wm + 32 * m + (lane & 31), wn + 32 * n + 8 * q + 4 * (lane >> 5), v);
+            }
+        };
+        bool ok = K >= SPLIT_MIN_K || sizeof(T) != 4;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int n = 0; n < TL::NI; ++n)
+#pragma unroll
+                for (int m = 0; m < TL::MI; ++m) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) hi[n][m][r] = (hi[n][m][r] + lo[n][m][r]) * SPLIT_UNSCALE;
+                    ok = ok && finite16(hi[n][m]);
+                }
+        }
+        if (sizeof(T) != 4 || __ballot(!ok) == 0ull) {
+#pragma unroll
+            for (int m = 0; m < TL::MI; ++m)
+#pragma unroll
+                for (int n = 0; n < TL::NI; ++n) block(m, n, hi[n][m]);
+        } else {
+            // (the lane made opaque, or what follows from it is worked out in front of the contraction and kept there)
+            asm volatile("" : "+v"(lane));
+#pragma unroll 1
+            for (int x = 0; x < TL::MI * TL::NI; ++x) {
+                const int m = x / TL::NI, n = x % TL::NI;
+                block(m, n, exact_sum(0, K, lane >> 5, [&](int k) { return b(wn + 32 * n + (lane & 31), k); },
+                                      [&](int k) { return a(wm + 32 * m + (lane & 31), k); }));
+            }
+        }
+    }
+};
+
+// Which rows a tile takes: its group, the place of its first row among the sorted ones, how many.  Tiles are numbered group by
+// group; every wave works it out for itself, 64 groups at a time.  Offsets that make no sense are held inside 0 .. n_rows.
+struct Spot { int g, first, rows, chunk, chunks, slab; };
+template <bool EMPTY_TOO>
+__device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G, int n_rows, int per, int j, Spot &s) {
+    const int lane = threadIdx.x & 63;
+    int slab = 0;
+    for (int base = 0; base < G; base += 64) {
+        const int g = base + lane;
+        const int lo = min(max(ptr[min(g, G)], 0), n_rows), hi = min(max(ptr[min(g + 1, G)], lo), n_rows);
+        int tiles = (int)(((int64_t)(hi - lo) + per - 1) / per);
+        if (EMPTY_TOO) tiles = max(tiles, 1);
+        if (g >= G) tiles = 0;
+        int sum = tiles, slabs = tiles > 1 ? tiles : 0;
+        const int own_slabs = slabs;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(sum, o), up2 = __shfl_up(slabs, o);
+            if (lane >= o) { sum += up; slabs += up2; }
+        }
+        const int all = __builtin_amdgcn_readlane(sum, 63);
+        if (j < all) {
+            const int l = __builtin_ctzll(__ballot(sum > j));
+            const int c = j - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(tiles, l));
+            s.g = base + l;
+            s.chunk = c;
+            s.chunks = __builtin_amdgcn_readlane(tiles, l);
+            s.first = __builtin_amdgcn_readlane(lo, l) + c * per;
+            s.rows = min(per, __builtin_amdgcn_readlane(hi, l) - s.first);
+            s.slab = slab + __builtin_amdgcn_readlane(slabs, l) - __builtin_amdgcn_readlane(own_slabs, l) + c;
+            return true;
+        }
+        j -= all;
+        slab += __builtin_amdgcn_readlane(slabs, 63);
+    }
+    return false;
+}
+
+// The list of rows; a number outside the rows reads row 0 and is not written
+struct RowList {
+    const int32_t *rows;
+    int32_t n;
+    __device__ __forceinline__ int at(int place) const {
+        const int r = rows ? rows[place] : place;
+        return (uint32_t)r < (uint32_t)n ? r : -1;
+    }
+};
+
+// Which tile a workgroup takes: workgroups are dealt round-robin to the eight XCDs, and consecutive tiles (the same rows, the same
+// matrix) belong into the L2 of one
+__device__ __forceinline__ int64_t tile_number(int64_t block, int64_t total) {
+    const int64_t per = (total + 7) / 8;
+    return (block & 7) * per + (block >> 3);
+}
+
+struct RowsArgs {
+    const void *a, *w;
+    const float *bias;
+    void *c;
+    int64_t lda, ldc, ldw;
+    int32_t K, N, G;
+    const int32_t *ptr;
+    RowList list;
+    int64_t tiles_m;
+    int32_t tiles_n;
+};
+
+template <class T>
+__device__ __forceinline__ void store4(T *p, const float (&v)[4], int n) {
+    if (n >= 4) {
+        if constexpr (sizeof(T) == 4) *(u32x4_any *)p = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else *(u32x2_any *)p = u32x2{cvt2bf(v[0], v[1]), cvt2bf(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (j < n) {
+                if constexpr (sizeof(T) == 4) p[j] = v[j];
+                else p[j] = f2bf(v[j]);
+            }
+    }
+}
+
+// c[r] = a[r] W[g] (+ bias), W as K x N, or as N x K (TRANSPOSED)
+template <class T, class TL, bool TRANSPOSED>
+__global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
+    constexpr int BM = TL::BM, BN = TL::BN, KG = Kind<T>::KG, P = Kind<T>::PLANES;
+    __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
+    __shared__ int s_row[BM];
+    const int64_t total = A.tiles_m * A.tiles_n, room = (total + 7) / 8 * 8;
+    for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
+        const int64_t x = tile_number(block, total);
+        Spot s;
+        if (x >= total || !find_spot<false>(A.ptr, A.G, A.list.n, BM, (int)(x / A.tiles_n), s)) continue;
+        const int n0 = (int)(x % A.tiles_n) * BN;
+        if (threadIdx.x < BM) s_row[threadIdx.x] = (int)threadIdx.x < s.rows ? A.list.at(s.first + threadIdx.x) : -1;
+        if (!TRANSPOSED && n0 + BN > A.N) clear_rows<T, BN>(s_b);
+        __syncthreads();
+        const T *a = (const T *)A.a, *w = (const T *)A.w + (int64_t)s.g * A.K * A.N;
+        const auto a_row = [&](int i) { return a + (int64_t)max(s_row[i < s.rows ? i : 0], 0) * A.lda; };
+        Along<T, BM> la;
+        la.init(A.K, a_row);
+        typename std::conditional<TRANSPOSED, Along<T, BN>, Across<T, BN>>::type lb;
+        const auto w_row = [&](int k) { return w + (int64_t)k * A.ldw; };
+        const auto w_col = [&](int i) { return w + (int64_t)min(n0 + i, A.N - 1) * A.ldw; };
+        if constexpr (TRANSPOSED) lb.init(A.K, w_col);
+        else lb.init(A.K, A.N, n0);
+        const auto load = [&](int t) __attribute__((always_inline)) {
+            la.load(t);
+            if constexpr (TRANSPOSED) lb.load(t);
+            else lb.load(t, w_row);
+        };
+        Sums<T, TL> sums;
+        sums.clear();
+        const int KT = (A.K + Kind<T>::KT - 1) / Kind<T>::KT;
+        load(0);
+        for (int t = 0; t < KT; ++t) {
+            la.store(s_a);
+            lb.store(s_b);
+            __syncthreads();
+            if (t + 1 < KT) load(t + 1);
+            sums.multiply(s_a, s_b);
+            __syncthreads();
+        }
+        const float *bias = A.bias ? A.bias + (int64_t)s.g * A.N : nullptr;
+        sums.finish(A.K, [&](int i, int k) { return k < A.K ? as_float(a_row(i)[k]) : 0.f; },
+                    [&](int i, int k) {
+                        if (k >= A.K) return 0.f;
+                        if constexpr (TRANSPOSED) return as_float(w_col(i)[k]);
+                        else return as_float(w_row(k)[min(n0 + i, A.N - 1)]);
+                    },
+                    [&](int i, int j, const float (&v)[4]) {
+            const int r = s_row[i], n = n0 + j, left = A.N - n;
+            if (r < 0 || left <= 0) return;
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = v[q] + (bias ? bias[min(n + q, A.N - 1)] : 0.f);
+            store4((T *)A.c + (int64_t)r * A.ldc + n, y, left);
+        });
+        __syncthreads();        // s_row is the next tile's
+    }
+}
+
+struct WeightArgs {
+    const void *x, *dy;
+    int64_t ldx, lddy;
+    int32_t K, N, G;            // rows and columns of a gradient
+    const int32_t *ptr;
+    RowList list;
+    int32_t per;                // rows of a chunk
+    int64_t items;              // chunks, at most
+    int32_t tiles_m, tiles_n;
+    float *dw, *db;
+    float *slab;                // [slabs x (K + 1) x N]: the chunks' gradients of W, then of b
+    int64_t slabs;
+};
+
+// dW[g] = sum of x[r]^T dy[r], db[g] = sum of dy[r]: of a chunk of a group's rows, into the slab of the chunk where a group has several
+template <class T, class TL>
+__global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
+    constexpr int BM = TL::BM, BN = TL::BN, KG = Kind<T>::KG, P = Kind<T>::PLANES;
+    __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
+    __shared__ double s_sum[KG][BN];
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, total = A.items * tiles, room = (total + 7) / 8 * 8;
+    for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
+        const int64_t x = tile_number(block, total);
+        Spot s;
+        if (x >= total || !find_spot<true>(A.ptr, A.G, A.list.n, A.per, (int)(x / tiles), s)) continue;
+        const bool whole = s.chunks == 1;
+        if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
+        const int m0 = (int)(x % tiles / A.tiles_n) * BM, n0 = (int)(x % A.tiles_n) * BN;
+        const T *xs = (const T *)A.x, *dys = (const T *)A.dy;
+        const auto row = [&](int k) { return (int64_t)max(A.list.at(s.first + k), 0); };
+        const auto x_row = [&](int k) { return xs + row(k) * A.ldx; };
+        const auto dy_row = [&](int k) { return dys + row(k) * A.lddy; };
+        Across<T, BM> la;
+        Across<T, BN> lb;
+        la.init(s.rows, A.K, m0);
+        lb.init(s.rows, A.N, n0);
+        Sums<T, TL> sums;
+        sums.clear();
+        double col[Across<T, BN>::W] = {};
+        const bool bias = A.db && m0 == 0;
+        if (m0 + BM > A.K) clear_rows<T, BM>(s_a);
+        if (n0 + BN > A.N) clear_rows<T, BN>(s_b);
+        __syncthreads();
+        const int KT = (s.rows + Kind<T>::KT - 1) / Kind<T>::KT;
+        if (KT > 0) { la.load(0, x_row); lb.load(0, dy_row); }
+        for (int t = 0; t < KT; ++t) {
+            la.store(s_a);
+            lb.store(s_b);
+            if (bias) {
+#pragma unroll
+                for (int c = 0; c < Across<T, BN>::W; ++c) {
+                    float f = 0.f, h = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) { f += as_float(lb.r[j][c]); h += as_float(lb.r[j + 1][c]); }
+                    col[c] += (double)f + (double)h;
+                }
+            }
+            __syncthreads();
+            if (t + 1 < KT) { la.load(t + 1, x_row); lb.load(t + 1, dy_row); }
+            sums.multiply(s_a, s_b);
+            __syncthreads();
+        }
+        const int64_t words = (int64_t)A.K * A.N;
+        float *out = whole ? A.dw + s.g * words : A.slab + s.slab * (words + A.N);
+        sums.finish(s.rows, [&](int i, int k) { return k < s.rows ? as_float(x_row(k)[min(m0 + i, A.K - 1)]) : 0.f; },
+                    [&](int i, int k) { return k < s.rows ? as_float(dy_row(k)[min(n0 + i, A.N - 1)]) : 0.f; },
+                    [&](int i, int j, const float (&v)[4]) {
+            const int m = m0 + i, n = n0 + j;
+            if (m < A.K && n < A.N) store4(out + (int64_t)m * A.N + n, v, A.N - n);
+        });
+        if (bias) {
+            constexpr int W = Across<T, BN>::W;
+            const int g = threadIdx.x / (BN / W);
+#pragma unroll
+            for (int c = 0; c < W; ++c)
+                if (lb.base + c >= 0 && lb.base + c < BN) s_sum[g][lb.base + c] = col[c];
+            __syncthreads();
+            for (int j = threadIdx.x; j < BN && n0 + j < A.N; j += NT) {
+                double sum = 0.0;
+                for (int q = 0; q < KG; ++q) sum += s_sum[q][j];
+                (whole ? A.db + (int64_t)s.g * A.N : out + words)[n0 + j] = (float)sum;
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// the slabs of every group that has several, added up in their order: blockIdx.y counts those groups
+__global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
+    const int64_t words = (int64_t)A.K * A.N, all = words + (A.db ? A.N : 0);
+    // the blockIdx.y-th group of several chunks
+    int g = 0, slab = 0, chunks = 0, seen = -1;
+    for (; g < A.G; ++g) {
+        const int lo = min(max(A.ptr[g], 0), A.list.n), hi = min(max(A.ptr[g + 1], lo), A.list.n);
+        chunks = (int)(((int64_t)(hi - lo) + A.per - 1) / A.per);
+        if (chunks > 1 && ++seen == (int)blockIdx.y) break;
+        slab += chunks > 1 ? chunks : 0;
+    }
+    if (g == A.G || slab + chunks > A.slabs) return;
+    const float *part = A.slab + slab * (words + A.N);
+    for (int64_t i = blockIdx.x * (int64_t)NT + threadIdx.x; i < all; i += (int64_t)gridDim.x * NT) {
+        float sum = 0.f;
+        int c = 0;
+        for (; c + 8 <= chunks; c += 8) {
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = part[(c + q) * (words + A.N) + i];
+            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+        for (; c < chunks; ++c) sum += part[c * (words + A.N) + i];
+        if (i < words) A.dw[g * words + i] = sum;
+        else A.db[(int64_t)g * A.N + (i - words)] = sum;
+    }
+}
+
+// -- launches ---------------------------------------------------------------------------------
+
+constexpr int64_t MOST_BLOCKS = 1 << 22;        // (a launch has less than 2^32 threads; workgroups go round)
+inline unsigned blocks(int64_t total) { return (unsigned)std::min<int64_t>((total + 7) / 8 * 8, MOST_BLOCKS); }
+
+template <class T, class TL, bool TRANSPOSED>
+void launch_rows(RowsArgs A, hipStream_t st) {
+    A.tiles_m = group_row_tiles(A.list.n, A.G, TL::BM);
+    A.tiles_n = (int32_t)group_ceil(A.N, TL::BN);
+    hipLaunchKernelGGL((k_grouped_rows<T, TL, TRANSPOSED>), dim3(blocks(A.tiles_m * A.tiles_n)), dim3(NT), 0, st, A);
+}
+template <bool TRANSPOSED>
+void launch_rows(const gsplit_ctx *ctx, int32_t dtype, const RowsArgs &A, hipStream_t st) {
+    const bool large = group_row_tiles(A.list.n, A.G, 128) * group_ceil(A.N, 128) >= ctx->n_cu;
+    if (dtype == GSPLIT_F32) {
+        if (large) launch_rows<float, Tile<128, 128>, TRANSPOSED>(A, st);
+        else launch_rows<float, Tile<64, 64>, TRANSPOSED>(A, st);
+    } else {
+        if (large) launch_rows<uint16_t, Tile<128, 128>, TRANSPOSED>(A, st);
+        else launch_rows<uint16_t, Tile<64, 64>, TRANSPOSED>(A, st);
+    }
+}
+
+bool weights_large(int32_t n_in, int32_t n_out) { return n_in > 64 && n_out > 64 && (int64_t)n_in * n_out >= 1 << 18; }
+int weights_tile(int32_t n_in, int32_t n_out) { return weights_large(n_in, n_out) ? 128 : 64; }
+int64_t weights_chunk(int n_cu, int64_t n_rows, int32_t n_in, int32_t n_out) {
+    const int t = weights_tile(n_in, n_out);
+    return group_chunk(n_rows, group_ceil(n_in, t) * group_ceil(n_out, t), n_cu);
+}
+
+}  // namespace
+
+extern "C" int gsplit_grouped_linear_fwd(gsplit_ctx *ctx, const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                         const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const float *d_bias,
+                                         void *d_y, int64_t y_stride, void *stream) {
+    if (!ctx) return GSPLIT_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    return gs_call(ctx, st, [&] {
+        if (const char *e = op_check_grouped_fwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_bias, d_y, y_stride))
+            return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_fwd: ") + e);
+        if (n_rows == 0) return (int)GSPLIT_OK;
+        GsTimeScope ts(ctx, "grouped_fwd", -1, st);
+        launch_rows<false>(ctx, c->dtype, RowsArgs{d_x, d_w, d_bias, d_y, x_stride, y_stride, c->n_out, c->n_in, c->n_out, c->n_groups,
+                                                   d_group_ptr, {d_rows, (int32_t)n_rows}, 0, 0}, st);
+        return (int)GSPLIT_OK;
+    });
+}
+
+extern "C" int64_t gsplit_grouped_linear_work(gsplit_ctx *ctx, const gsplit_grouped_config *c, int64_t n_rows) {
+    if (!ctx) return GSPLIT_EINVAL;
+    if (const char *e = op_check_grouped(c, n_rows)) {
+        try { return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_work: ") + e); } catch (...) { return GSPLIT_ENOMEM; }
+    }
+    const int64_t slabs = group_slabs(n_rows, weights_chunk(ctx->n_cu, n_rows, c->n_in, c->n_out));
+    return slabs * ((int64_t)c->n_in + 1) * c->n_out * (int64_t)sizeof(float);
+}
+
+extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                         const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const void *d_dy,
+                                         int64_t dy_stride, void *d_dx, int64_t dx_stride, float *d_dw, float *d_dbias, void *d_work,
+                                         void *stream) {
+    if (!ctx) return GSPLIT_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    return gs_call(ctx, st, [&] {
+        const char *e = op_check_grouped_bwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_dy, dy_stride, d_dx, dx_stride, d_dw,
+                                             d_dbias, d_work);
+        int64_t chunk = 1, slabs = 0;
+        if (!e && d_dw) {
+            chunk = weights_chunk(ctx->n_cu, n_rows, c->n_in, c->n_out);
+            slabs = group_slabs(n_rows, chunk);
+            if (slabs && !d_work) e = "NULL d_work";
+        }
+        if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_bwd: ") + e);
+        const RowList list{d_rows, (int32_t)n_rows};
+        if (d_dx && n_rows > 0) {
+            GsTimeScope ts(ctx, "grouped_dx", -1, st);
+            launch_rows<true>(ctx, c->dtype, RowsArgs{d_dy, d_w, nullptr, d_dx, dy_stride, dx_stride, c->n_out, c->n_out, c->n_in,
+                                                      c->n_groups, d_group_ptr, list, 0, 0}, st);
+        }
+        if (d_dw) {
+            const int t = weights_tile(c->n_in, c->n_out);
+            WeightArgs A{d_x, d_dy, x_stride, dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)chunk,
+                         n_rows / chunk + c->n_groups, (int32_t)group_ceil(c->n_in, t), (int32_t)group_ceil(c->n_out, t), d_dw, d_dbias,
+                         (float *)d_work, slabs};
+            const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));
+            {
+                GsTimeScope ts(ctx, "grouped_dw", -1, st);
+                const auto kernel = c->dtype == GSPLIT_F32 ? t == 128 ? k_grouped_weights<float, Tile<128, 128>> : k_grouped_weights<float, Tile<64, 64>>
+                                                           : t == 128 ? k_grouped_weights<uint16_t, Tile<128, 128>> : k_grouped_weights<uint16_t, Tile<64, 64>>;
+                hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, A);
+            }
+            if (slabs) {
+                GsTimeScope ts(ctx, "grouped_dw_sum", -1, st);
+                const int64_t words = ((int64_t)c->n_in + 1) * c->n_out;
+                hipLaunchKernelGGL(k_grouped_weights_sum, dim3((unsigned)std::min<int64_t>(group_ceil(words, NT), 1024),
+                                                               (unsigned)std::min<int64_t>(c->n_groups, n_rows / chunk)), dim3(NT), 0, st, A);
+            }
+        }
+        return (int)GSPLIT_OK;
+    });
+}

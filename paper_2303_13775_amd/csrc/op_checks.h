@@ -103,3 +103,61 @@ inline const char *op_check_adamw(const gsplit_adamw_config *c, const gsplit_ada
     }
     return nullptr;
 }
+
+inline const char *op_check_group_rows(const int32_t *d_group, int64_t n_rows, int32_t n_groups, const int32_t *d_group_ptr,
+                                       const int32_t *d_rows) {
+    if (n_rows < 0 || n_rows > INT32_MAX) return "n_rows out of range";
+    if (n_groups < 1 || n_groups > GSPLIT_MAX_GROUPS) return "n_groups out of range";
+    if (!d_group_ptr || (n_rows > 0 && (!d_group || !d_rows))) return "NULL buffer";
+    if (op_misaligned(d_group, 4) || op_misaligned(d_group_ptr, 4) || op_misaligned(d_rows, 4)) return "misaligned buffer";
+    return nullptr;
+}
+
+inline const char *op_check_grouped(const gsplit_grouped_config *c, int64_t n_rows) {
+    if (!c) return "NULL config";
+    if (!op_elem_size(c->dtype)) return "unknown dtype";
+    if (c->n_groups < 1 || c->n_groups > GSPLIT_MAX_GROUPS) return "n_groups out of range";
+    if (c->n_in < 1 || c->n_in > 1 << 20 || c->n_out < 1 || c->n_out > 1 << 20) return "width out of range";
+    if (n_rows < 0 || n_rows > INT32_MAX) return "n_rows out of range";
+    return nullptr;
+}
+// a matrix of the rows, `needed` if there are any
+inline const char *op_check_grouped_rows(const void *p, int64_t n_rows, int64_t width, int64_t stride, int size, bool needed) {
+    if (!p) return needed && n_rows > 0 ? "NULL buffer" : nullptr;
+    if (op_misaligned(p, size)) return "misaligned buffer";
+    return stride < width || stride > (int64_t)1 << 40 ? "stride below its width or out of range" : nullptr;
+}
+inline const char *op_check_grouped_lists(const gsplit_grouped_config *c, const int32_t *d_group_ptr, const int32_t *d_rows) {
+    if (!d_group_ptr) return "NULL buffer";
+    return op_misaligned(d_group_ptr, 4) || op_misaligned(d_rows, 4) ? "misaligned buffer" : nullptr;
+}
+
+inline const char *op_check_grouped_fwd(const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                        const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const float *d_bias,
+                                        const void *d_y, int64_t y_stride) {
+    if (const char *e = op_check_grouped(c, n_rows)) return e;
+    const int size = op_elem_size(c->dtype);
+    if (const char *e = op_check_grouped_rows(d_x, n_rows, c->n_in, x_stride, size, true)) return e;
+    if (const char *e = op_check_grouped_rows(d_y, n_rows, c->n_out, y_stride, size, true)) return e;
+    if (n_rows == 0) return nullptr;
+    if (const char *e = op_check_grouped_lists(c, d_group_ptr, d_rows)) return e;
+    if (!d_w) return "NULL buffer";
+    return op_misaligned(d_w, size) || op_misaligned(d_bias, 4) ? "misaligned buffer" : nullptr;
+}
+
+inline const char *op_check_grouped_bwd(const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                        const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const void *d_dy,
+                                        int64_t dy_stride, const void *d_dx, int64_t dx_stride, const float *d_dw, const float *d_dbias,
+                                        const void *d_work) {
+    if (const char *e = op_check_grouped(c, n_rows)) return e;
+    const int size = op_elem_size(c->dtype);
+    if (const char *e = op_check_grouped_rows(d_x, n_rows, c->n_in, x_stride, size, d_dw)) return e;
+    if (const char *e = op_check_grouped_rows(d_dy, n_rows, c->n_out, dy_stride, size, true)) return e;
+    if (const char *e = op_check_grouped_rows(d_dx, n_rows, c->n_in, dx_stride, size, false)) return e;
+    if (d_dbias && !d_dw) return "d_dbias needs d_dw";
+    if (!d_dx && !d_dw) return "nothing to compute";
+    if (const char *e = op_check_grouped_lists(c, d_group_ptr, d_rows)) return e;
+    if (d_dx && n_rows > 0 && !d_w) return "NULL buffer";
+    return op_misaligned(d_w, size) || op_misaligned(d_dw, 4) || op_misaligned(d_dbias, 4) || op_misaligned(d_work, 16) ? "misaligned buffer"
+                                                                                                                        : nullptr;
+}

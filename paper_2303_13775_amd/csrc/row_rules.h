@@ -73,6 +73,7 @@ inline int preference_whole(int64_t n_rows, int64_t n_pairs, int C, int n_cu) {
 // 23.1, 11.7 / 17.2, 64 x 70000 12.5 / 12.9, 11.0 / 10.4; 100 x 131072 32.0 / 31.8, 19.2 / 18.5, 100 x 70000 16.3 / 14.5, 12.9 / 10.5.
 // Preference loss: 1 pair of 65536 12.4 / 28, 120 pairs 39 / 47.
 constexpr int GS_ROW_PARTS = 8192;      // (row, part) pairs the context's scratch holds
+constexpr int GS_ROW_PART_BYTES = 20;   // of each
 inline int row_chunks(int64_t n_rows, int C, int n_cu) {
     int64_t chunks = (2 * n_cu + n_rows - 1) / n_rows;
     if (chunks > C / 4096) chunks = C / 4096;
