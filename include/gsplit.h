@@ -636,6 +636,69 @@ GSPLIT_API int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
                                          const void *d_dy, int64_t dy_stride, void *d_dx, int64_t dx_stride, float *d_dw,
                                          float *d_dbias, void *d_work, void *stream);
 
+/* Matrices orthogonalised by Newton-Schulz steps.  For every matrix G [rows x cols] of a stack, with X = G / (|G| + eps)
+ * (the Frobenius norm) and `steps` times
+ *     A = X X^T,   X = (a I + b A + c A^2) X
+ * out = X: G's directions with all singular values moved towards 1.  The default coefficients of the binding (3.4445, -4.7750,
+ * 2.0315) do not converge but bring values from 0.01 on into 0.7 .. 1.2 within five steps; 1.875, -1.25, 0.375 converge.  A matrix
+ * of zeros gives zeros (where |G| + eps is 0, X is 0); one with a value that is not finite gives NaN throughout.  d_in and d_out are
+ * dense [count x rows x cols], each float or bfloat16; d_out may be d_in if their types are the same.  The
+ * products' factors are held in two halves (24 bits) and summed in float; results of bfloat16 are rounded once.  The same bits on every call.
+ * Coefficients have to keep singular values from 0 to 1 below 2, and |a + b s^2 + c s^4| below 15, in every step.
+ * d_work: 16-byte aligned working memory of gsplit_orthogonalize_work() bytes, which depends on the sizes alone; one call uses
+ * it at a time.  What a call writes may overlap nothing else of it.  The HOST arrays are read during the call.  Asynchronous; may be captured at any time (the
+ * addresses are then fixed).  EINVAL for NULL or misaligned pointers, unknown dtypes, negative counts, rows or cols outside
+ * 0 .. 65536, steps outside 1 .. 64, coefficients as above, eps negative or not finite. */
+typedef struct {
+    const void *d_in;
+    void       *d_out;
+    int64_t     count;
+    int32_t     rows, cols;
+    int32_t     in_dtype, out_dtype;
+} gsplit_matrix_tensor;
+
+typedef struct {
+    double  a, b, c, eps;
+    int32_t steps;
+} gsplit_newton_config;
+
+/* Bytes of working memory (needs no context); EINVAL for tensors that the call refuses. */
+GSPLIT_API int64_t gsplit_orthogonalize_work(const gsplit_matrix_tensor *tensors, int64_t n_tensors);
+GSPLIT_API int gsplit_orthogonalize(gsplit_ctx *ctx, const gsplit_newton_config *config, const gsplit_matrix_tensor *tensors,
+                                    int64_t n_tensors, void *d_work, void *stream);
+
+/* One step of orthogonalised momentum, beside gsplit_adamw_step: for the matrices of a model, whose vectors AdamW updates.
+ *     m = momentum m + (1 - momentum) g,   u = nesterov ? momentum m + (1 - momentum) g : m
+ *     p = (1 - lr * weight_decay) p - lr * scale * orthogonalised(u)
+ * scale: GSPLIT_MUON_PLAIN 1; GSPLIT_MUON_SHAPE sqrt(max(1, cols / rows)) (weights are n_in x n_out: the output
+ * changes by about lr whatever the shape); GSPLIT_MUON_RMS 0.2 sqrt(max(rows, cols)) (elements change by about what AdamW's do).
+ * Parameters, their float copies and gradients as for gsplit_adamw_step, dense [count x rows x cols]; momenta are float.  A
+ * gradient or momentum that is not finite makes its matrix' momentum what it is, and its parameters NaN.  The learning rate is *d_lr if given (DEVICE, read
+ * when the kernels run), else lr.  EINVAL also for momentum outside [0, 1), lr or weight_decay negative or not finite, an
+ * unknown scaling, a missing d_master (or one that a float parameter has). */
+enum { GSPLIT_MUON_PLAIN = 0, GSPLIT_MUON_SHAPE = 1, GSPLIT_MUON_RMS = 2 };
+
+typedef struct {
+    void       *d_param;
+    float      *d_master;        /* bfloat16 parameters: their float copy; NULL for float ones */
+    const void *d_grad;
+    float      *d_momentum;
+    int64_t     count;
+    int32_t     rows, cols;
+    int32_t     param_dtype, grad_dtype;
+} gsplit_muon_tensor;
+
+typedef struct {
+    gsplit_newton_config newton;
+    double               lr, momentum, weight_decay;
+    const float         *d_lr;
+    int32_t              nesterov, scaling;
+} gsplit_muon_config;
+
+GSPLIT_API int64_t gsplit_muon_work(const gsplit_muon_tensor *tensors, int64_t n_tensors);
+GSPLIT_API int gsplit_muon_step(gsplit_ctx *ctx, const gsplit_muon_config *config, const gsplit_muon_tensor *tensors,
+                                int64_t n_tensors, void *d_work, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

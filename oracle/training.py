@@ -105,3 +105,28 @@ def adamw(p, g, m, v, *, lr, beta1, beta2, eps, weight_decay, step, factor=1.0):
     with np.errstate(invalid="ignore", divide="ignore"):
         change = (m / (1 - beta1 ** step)) / (np.sqrt(v / (1 - beta2 ** step)) + eps)
     return (1 - lr * weight_decay) * p - lr * change, m, v
+
+
+def orthogonalize(g, steps, a, b, c, eps):
+    """Newton-Schulz steps of one matrix."""
+    x = np.asarray(g, np.float64)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        norm = np.sqrt(np.sum(np.square(x))) + eps
+        if not np.isfinite(norm):
+            return np.full(x.shape, np.nan)
+        x = x / norm if norm > 0 else x
+    tall = x.shape[0] > x.shape[1]
+    x = x.T if tall else x
+    for _ in range(steps):
+        q = x @ x.T
+        x = (a * np.eye(len(q)) + b * q + c * q @ q) @ x
+    return x.T if tall else x
+
+
+def muon(p, g, m, *, lr, momentum, nesterov, weight_decay, scale, steps, coefficients, eps):
+    """(p, m, the orthogonalised matrix) after the step, for one matrix."""
+    p, g, m = (np.asarray(x, np.float64) for x in (p, g, m))
+    with np.errstate(invalid="ignore"):
+        m = momentum * m + (1 - momentum) * g
+        o = orthogonalize(momentum * m + (1 - momentum) * g if nesterov else m, steps, *coefficients, eps)
+        return (1 - lr * weight_decay) * p - lr * scale * o, m, o

@@ -30,6 +30,7 @@ EXPORTS = [
     "gsplit_sample_split_multi", "gsplit_sage_step", "gsplit_gather_features_multi",
     "gsplit_policy_loss", "gsplit_preference_loss", "gsplit_grad_norm", "gsplit_clip_grads", "gsplit_adamw_step",
     "gsplit_group_rows", "gsplit_grouped_linear_fwd", "gsplit_grouped_linear_work", "gsplit_grouped_linear_bwd",
+    "gsplit_orthogonalize_work", "gsplit_orthogonalize", "gsplit_muon_work", "gsplit_muon_step",
 ]
 
 
@@ -114,6 +115,25 @@ class _GroupedConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("dtype", "n_groups", "n_in", "n_out")]
 
 
+class _MatrixTensor(C.Structure):
+    _fields_ = [("d_in", C.c_void_p), ("d_out", C.c_void_p), ("count", C.c_int64)] + [
+        (n, C.c_int32) for n in ("rows", "cols", "in_dtype", "out_dtype")]
+
+
+class _NewtonConfig(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("a", "b", "c", "eps")] + [("steps", C.c_int32)]
+
+
+class _MuonTensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("d_param", "d_master", "d_grad", "d_momentum")] + [("count", C.c_int64)] + [
+        (n, C.c_int32) for n in ("rows", "cols", "param_dtype", "grad_dtype")]
+
+
+class _MuonConfig(C.Structure):
+    _fields_ = [("newton", _NewtonConfig), ("lr", C.c_double), ("momentum", C.c_double), ("weight_decay", C.c_double), ("d_lr", C.c_void_p),
+                ("nesterov", C.c_int32), ("scaling", C.c_int32)]
+
+
 _lib = None
 
 
@@ -176,8 +196,15 @@ def load_library():
     L.gsplit_grouped_linear_work.argtypes = [vp, C.POINTER(_GroupedConfig), i64]
     L.gsplit_grouped_linear_work.restype = i64
     L.gsplit_grouped_linear_bwd.argtypes = [vp, C.POINTER(_GroupedConfig), vp, i64, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp]
+    L.gsplit_orthogonalize_work.argtypes = [C.POINTER(_MatrixTensor), i64]
+    L.gsplit_orthogonalize_work.restype = i64
+    L.gsplit_orthogonalize.argtypes = [vp, C.POINTER(_NewtonConfig), C.POINTER(_MatrixTensor), i64, vp, vp]
+    L.gsplit_muon_work.argtypes = [C.POINTER(_MuonTensor), i64]
+    L.gsplit_muon_work.restype = i64
+    L.gsplit_muon_step.argtypes = [vp, C.POINTER(_MuonConfig), C.POINTER(_MuonTensor), i64, vp, vp]
     for name in EXPORTS:
-        if name not in ("gsplit_last_error", "gsplit_max_rows", "gsplit_timing_read", "gsplit_grouped_linear_work"):
+        if name not in ("gsplit_last_error", "gsplit_max_rows", "gsplit_timing_read", "gsplit_grouped_linear_work", "gsplit_orthogonalize_work",
+                        "gsplit_muon_work"):
             getattr(L, name).restype = C.c_int
     _lib = L
     return L
@@ -407,6 +434,64 @@ class AdamwTensors:
             _AdamwTensor(p.data_ptr(), None if w is None else w.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
                          p.numel(), _DTYPES[p.dtype], _DTYPES[g.dtype])
             for p, g, a, b, w in zip(params, grads, m, v, masters)])
+
+
+NEWTON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+MUON_SCALINGS = {"plain": 0, "shape": 1, "rms": 2}
+
+
+def _stack_shape(t):
+    """(count, rows, cols) of a matrix or a stack of them."""
+    assert t.dim() in (2, 3) and t.is_contiguous()
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def _newton_work(bytes_, device):
+    if bytes_ < 0:
+        raise GsplitError(int(bytes_), "sizes out of range")
+    return torch.empty(bytes_, dtype=torch.uint8, device=device)
+
+
+class MatrixTensors:
+    """Holds the marshalled matrices of gsplit_orthogonalize, [rows, cols] or stacks [count, rows, cols], and the working memory of
+    a call (and keeps them alive).  outs: where the results go; None, or the matrices themselves: in place."""
+
+    def __init__(self, matrices: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None):
+        outs = matrices if outs is None else outs
+        assert len(outs) == len(matrices)
+        self.device = _same_device([*matrices, *outs])
+        for g, o in zip(matrices, outs):
+            assert g.dtype in _DTYPES and o.dtype in _DTYPES and o.shape == g.shape and o.is_contiguous()
+            assert g.data_ptr() != o.data_ptr() or g.dtype == o.dtype or g.numel() == 0
+        _assert_apart(outs, [g for g, o in zip(matrices, outs) if g.data_ptr() != o.data_ptr()])
+        self.tensors = (list(matrices), list(outs))
+        self.n = len(self.tensors[0])
+        self.c = (_MatrixTensor * max(1, self.n))(*[
+            _MatrixTensor(g.data_ptr(), o.data_ptr(), *_stack_shape(g), _DTYPES[g.dtype], _DTYPES[o.dtype]) for g, o in zip(matrices, outs)])
+        self.work = _newton_work(load_library().gsplit_orthogonalize_work(self.c, self.n), self.device)
+
+
+class MuonTensors:
+    """Holds the marshalled tensors of gsplit_muon_step, [rows, cols] or stacks [count, rows, cols], and the working memory of a
+    call (and keeps them alive).  masters: the float copies of the bfloat16 parameters, None for the float ones (or None if there
+    are none)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], momenta: Sequence[torch.Tensor],
+                 masters: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        masters = [None] * len(params) if masters is None else masters
+        assert len(grads) == len(momenta) == len(masters) == len(params)
+        self.device = _same_device([*params, *grads, *momenta, *[t for t in masters if t is not None]])
+        for p, g, m, w in zip(params, grads, momenta, masters):
+            assert p.dtype in _DTYPES and g.dtype in _DTYPES and (w is not None) == (p.dtype == torch.bfloat16)
+            assert all(t is None or (t.is_contiguous() and t.shape == p.shape) for t in (g, m, w))
+            assert all(t is None or t.dtype == torch.float32 for t in (m, w))
+        _assert_apart([*params, *masters, *momenta], grads)
+        self.tensors = (list(params), list(grads), list(momenta), list(masters))
+        self.n = len(self.tensors[0])
+        self.c = (_MuonTensor * max(1, self.n))(*[
+            _MuonTensor(p.data_ptr(), None if w is None else w.data_ptr(), g.data_ptr(), m.data_ptr(), *_stack_shape(p), _DTYPES[p.dtype],
+                        _DTYPES[g.dtype]) for p, g, m, w in zip(params, grads, momenta, masters)])
+        self.work = _newton_work(load_library().gsplit_muon_work(self.c, self.n), self.device)
 
 
 class Context:
@@ -759,6 +844,23 @@ class Context:
                                                 None if work is None else work.data_ptr(), self._own_stream())
         if rc:
             self._check(rc)
+
+    def gsplit_orthogonalize(self, matrices: MatrixTensors, steps: int = 5,
+                             coefficients: Sequence[float] = NEWTON_COEFFICIENTS, eps: float = 1e-7):
+        """Newton-Schulz steps X <- (a I + b X X^T + c (X X^T)^2) X from every matrix over its norm, into the table's outputs."""
+        assert matrices.device is None or matrices.device == self.device
+        cfg = _NewtonConfig(*coefficients, eps, steps)
+        self._check(self.lib.gsplit_orthogonalize(self.h, C.byref(cfg), matrices.c, matrices.n, matrices.work.data_ptr(), self._own_stream()))
+
+    def gsplit_muon_step(self, tensors: MuonTensors, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                         weight_decay: float = 0.0, scaling: str = "shape", steps: int = 5,
+                         coefficients: Sequence[float] = NEWTON_COEFFICIENTS, eps: float = 1e-7, lr_dev: Optional[torch.Tensor] = None):
+        """One step of orthogonalised momentum for matrices.  scaling: "plain", "shape" or "rms" (see gsplit.h); lr_dev (float32): the
+        learning rate in device memory, for captured steps."""
+        assert tensors.device is None or tensors.device == self.device
+        cfg = _MuonConfig(_NewtonConfig(*coefficients, eps, steps), lr, momentum, weight_decay, self._vectors((lr_dev,), 1)[0], int(nesterov),
+                          MUON_SCALINGS[scaling])
+        self._check(self.lib.gsplit_muon_step(self.h, C.byref(cfg), tensors.c, tensors.n, tensors.work.data_ptr(), self._own_stream()))
 
     def gsplit_presample_accumulate(self, vertex_count: Optional[torch.Tensor], edge_count: Optional[torch.Tensor]):
         # torch has no unsigned 32-bit arithmetic: int32 tensors carry the uint32 counters

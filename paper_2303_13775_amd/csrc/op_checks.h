@@ -161,3 +161,80 @@ inline const char *op_check_grouped_bwd(const gsplit_grouped_config *c, const vo
     return op_misaligned(d_w, size) || op_misaligned(d_dw, 4) || op_misaligned(d_dbias, 4) || op_misaligned(d_work, 16) ? "misaligned buffer"
                                                                                                                         : nullptr;
 }
+
+// Singular values s of [0, 1] under s -> |s (a + b s^2 + c s^4)|: the bounds of what the halves hold (newton.hip).
+inline bool op_newton_bounded(double a, double b, double c, int steps) {
+    double top = 1.0;           // of the values in front of a step
+    for (int k = 0; k < steps; ++k) {
+        // largest |s (a + b s^2 + c s^4)| and |a + b x + c x^2| (x = s^2) on [0, top]: at an end or where a derivative is 0
+        const auto p = [&](double s) { const double x = s * s; return s * (a + x * (b + x * c)); };
+        const auto q = [&](double x) { return std::fabs(a + x * (b + x * c)); };
+        double next = std::fabs(p(top)), most = std::fmax(q(0.0), q(top * top));
+        if (c != 0.0) {
+            const double turn = -b / (2.0 * c), root = 9.0 * b * b - 20.0 * a * c;
+            if (turn > 0.0 && turn < top * top) most = std::fmax(most, q(turn));
+            if (root >= 0.0)
+                for (const double sign : {-1.0, 1.0}) {
+                    const double x = (-3.0 * b + sign * std::sqrt(root)) / (10.0 * c);
+                    if (x > 0.0 && x < top * top) next = std::fmax(next, std::fabs(p(std::sqrt(x))));
+                }
+        } else if (b != 0.0 && -a / (3.0 * b) > 0.0 && -a / (3.0 * b) < top * top) {
+            next = std::fmax(next, std::fabs(p(std::sqrt(-a / (3.0 * b)))));
+        }
+        if (!(next <= 1.99 && most <= 15.0)) return false;
+        top = std::fmax(next, 1e-300);
+    }
+    return true;
+}
+
+inline const char *op_check_newton(const gsplit_newton_config *c) {
+    if (!c) return "NULL config";
+    if (c->steps < 1 || c->steps > 64) return "steps out of range";
+    if (!op_not_negative(c->eps)) return "eps negative or not finite";
+    if (!std::isfinite(c->a) || !std::isfinite(c->b) || !std::isfinite(c->c) || !op_newton_bounded(c->a, c->b, c->c, c->steps))
+        return "coefficients that do not keep singular values in bounds";
+    return nullptr;
+}
+inline const char *op_check_shape(int64_t count, int32_t rows, int32_t cols) {
+    if (rows < 0 || rows > 65536 || cols < 0 || cols > 65536) return "rows or cols out of range";
+    return count < 0 || count > (int64_t)1 << 31 || count * rows > (int64_t)1 << 40 || count * rows * cols > (int64_t)1 << 46
+               ? "number of matrices out of range" : nullptr;
+}
+inline const char *op_check_matrices(const gsplit_matrix_tensor *t, int64_t n_tensors) {
+    if (n_tensors < 0 || (n_tensors > 0 && !t)) return "bad tensor list";
+    for (int64_t i = 0; i < n_tensors; ++i) {
+        if (const char *e = op_check_shape(t[i].count, t[i].rows, t[i].cols)) return e;
+        const int64_t n = t[i].count * t[i].rows * t[i].cols;
+        if (const char *e = op_check_run(t[i].d_in, n, op_elem_size(t[i].in_dtype))) return e;
+        if (const char *e = op_check_run(t[i].d_out, n, op_elem_size(t[i].out_dtype))) return e;
+        if (n > 0 && t[i].d_in == t[i].d_out && t[i].in_dtype != t[i].out_dtype) return "in place needs one type";
+    }
+    return nullptr;
+}
+inline const char *op_check_muon(const gsplit_muon_config *c) {
+    if (!c) return "NULL config";
+    if (const char *e = op_check_newton(&c->newton)) return e;
+    if (!(c->momentum >= 0.0 && c->momentum < 1.0)) return "momentum outside [0, 1)";
+    if (!(c->d_lr || op_not_negative(c->lr)) || !op_not_negative(c->weight_decay)) return "lr or weight_decay negative or not finite";
+    if (c->scaling < GSPLIT_MUON_PLAIN || c->scaling > GSPLIT_MUON_RMS) return "unknown scaling";
+    return op_misaligned(c->d_lr, 4) ? "misaligned buffer" : nullptr;
+}
+inline const char *op_check_muon_tensors(const gsplit_muon_tensor *t, int64_t n_tensors) {
+    if (n_tensors < 0 || (n_tensors > 0 && !t)) return "bad tensor list";
+    for (int64_t i = 0; i < n_tensors; ++i) {
+        const gsplit_muon_tensor &x = t[i];
+        if (const char *e = op_check_shape(x.count, x.rows, x.cols)) return e;
+        const int64_t n = x.count * x.rows * x.cols;
+        if (const char *e = op_check_run(x.d_param, n, op_elem_size(x.param_dtype))) return e;
+        if (const char *e = op_check_run(x.d_grad, n, op_elem_size(x.grad_dtype))) return e;
+        if (const char *e = op_check_run(x.d_momentum, n, 4)) return e;
+        if (x.param_dtype == GSPLIT_F32 && x.d_master) return "a float parameter has no d_master";
+        if (x.param_dtype == GSPLIT_BF16)
+            if (const char *e = op_check_run(x.d_master, n, 4)) return e;
+    }
+    return nullptr;
+}
+inline const char *op_check_work(const void *d_work, int64_t bytes) {
+    if (bytes > 0 && !d_work) return "NULL d_work";
+    return op_misaligned(d_work, 16) ? "misaligned buffer" : nullptr;
+}

@@ -1,0 +1,316 @@
+"""Newton-Schulz orthogonalisation and the update by orthogonalised momentum against their float64 forms: matrices of all shapes, wide
+and tall, stacks, both types, several launches, zeros and values that are not finite, and the ways a caller may run them.
+
+Tolerances.  The steps raise small singular values by their first coefficient each, and with them what was rounded off in front, so a
+bound that takes the worst of every step says nothing.  Instead the float64 form runs beside itself with errors planted: with u = 2^-24,
+a product's element of K terms is a float sum of 3 K / 16 instructions (sixteen terms of one of three partial products each), whose partial sums are at most |row||column|
+(Cauchy-Schwarz); each rounds by at most u of that, in random directions: u sqrt(3 K / 16) |row||column|, and 2 u |row||column| for what
+the two halves of the factors do not hold and what is dropped of their product (2^-24 |x||y| a term).  A uniform error of that size is planted in every element of
+every product; results may be off by three times the largest deviation of three such runs, and by the rounding to their type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import row_loss_check as K
+from oracle import training as T
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+U = K.U
+ABC = (3.4445, -4.7750, 2.0315)
+CONVERGING = (1.875, -1.25, 0.375)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = K.context()
+    yield c
+    c.close()
+
+
+def _product(p, q, gen):
+    """p q^T, with errors planted if there is a generator"""
+    out = p @ q.transpose(1, 2)
+    if gen is not None:
+        size = p.norm(dim=2, keepdim=True) * q.norm(dim=2)[:, None, :]
+        out += size * (U * (2 + math.sqrt(3 * p.shape[2] / 16))) * (2 * torch.rand(out.shape, dtype=out.dtype, device=out.device, generator=gen) - 1)
+    return out
+
+
+def _steps(g, steps, abc, eps, gen=None):
+    a, b, c = abc
+    x = g / (g.flatten(1).norm(dim=1)[:, None, None] + eps)
+    tall = x.shape[1] > x.shape[2]
+    x = (x.transpose(1, 2) if tall else x).contiguous()
+    one = torch.eye(x.shape[1], dtype=x.dtype, device=x.device)
+    for _ in range(steps):
+        q = _product(x, x, gen)
+        x = _product(a * one + b * q + c * _product(q, q, gen), x.transpose(1, 2).contiguous(), gen)
+    return x.transpose(1, 2) if tall else x
+
+
+def _expected(g, steps=5, abc=ABC, eps=1e-7):
+    """(result, how far a matrix' results may be off) of a stack in float64"""
+    want = _steps(g, steps, abc, eps)
+    off = torch.zeros(len(g), dtype=g.dtype, device=g.device)
+    for seed in range(3):
+        gen = torch.Generator(device=g.device).manual_seed(seed)
+        off = torch.maximum(off, (_steps(g, steps, abc, eps, gen) - want).flatten(1).abs().amax(1))
+    return want, 3 * off
+
+
+def _close(name, got, want, off, dtype=F32):
+    over = (got.double() - want).abs() - (off[:, None, None] + (K.EPS[dtype] + U) * want.abs())
+    assert bool((over <= 0).all()), (name, float(over.max()), float(off.max()), int((over > 0).sum()), got.shape)
+
+
+def _matrices(shapes, seed, scale=1e-3, rank=6):
+    """Gradients: a few strong directions over noise; (count, rows, cols), from a stack's seed."""
+    out = []
+    for k, (count, rows, cols) in enumerate(shapes):
+        gen = torch.Generator(device="cuda").manual_seed(1000 * seed + k)
+        r = lambda *s: torch.randn(s, device="cuda", generator=gen)
+        out.append((r(count, rows, rank) @ r(count, rank, cols) + 0.5 * r(count, rows, cols)) * scale)
+    return out
+
+
+def _room(tensors, fill=7.0):
+    """The tensors again, in buffers with 3 values in front of and 5 behind each: (buffers, views)."""
+    whole = [torch.full((t.numel() + 8,), fill, dtype=t.dtype, device="cuda") for t in tensors]
+    views = [w[3:3 + t.numel()].view(t.shape) for w, t in zip(whole, tensors)]
+    for v, t in zip(views, tensors):
+        v.copy_(t)
+    return whole, views
+
+
+def _kept(whole, fill=7.0):
+    return all(bool((w[:3] == fill).all()) and bool((w[-5:] == fill).all()) for w in whole)
+
+
+SETS = [    # stacks (count, rows, cols)
+    [(1, 1, 1)], [(1, 1, 9), (1, 9, 1), (2, 3, 2)], [(1, 64, 64)], [(2, 64, 64), (2, 64, 16)], [(1, 65, 64), (1, 63, 130), (1, 128, 129)],
+    [(2, 100, 256), (2, 256, 256), (2, 256, 47)], [(5, 33, 70), (3, 70, 33)], [(1, 300, 1000), (1, 1000, 300)], [(1, 31, 4097)], [(1, 2500, 5)],
+    [(1, 8 + k, 40 - k) for k in range(30)], [(0, 5, 5), (1, 0, 7), (2, 7, 0), (1, 12, 12)], [], [(300, 24, 40)]]
+LARGE = [[(26, 512, 520)], [(1, 2944, 2900)], [(30, 500, 640), (7, 40, 900), (9, 700, 300)], [(20, 1280, 1408)]]
+
+
+@pytest.mark.parametrize("which", range(len(SETS) + len(LARGE)))
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16), (BF16, F32)])
+def test_orthogonalize(ctx, which, types):
+    from paper_2303_13775_amd import MatrixTensors
+    shapes = (SETS + LARGE)[which]
+    gi, mats = _room([g.to(types[0]) for g in _matrices(shapes, which)])
+    go, outs = _room([torch.full(s, 9.0, dtype=types[1], device="cuda") for s in shapes])
+    before = [g.clone() for g in mats]
+    table = MatrixTensors(mats, outs)
+    ctx.gsplit_orthogonalize(table)
+    for g, o in zip(mats, outs):
+        if g.numel():
+            _close(g.shape, o, *_expected(g.double()), types[1])
+    assert _kept(gi) and _kept(go) and all(torch.equal(a, b) for a, b in zip(mats, before))
+    first = [o.clone() for o in outs]
+    table.work.fill_(0xFF)
+    ctx.gsplit_orthogonalize(table)
+    assert all(torch.equal(a, b) for a, b in zip(outs, first))      # the same bits, whatever the working memory holds
+    if types[0] == types[1] and which < len(SETS):
+        ctx.gsplit_orthogonalize(MatrixTensors(mats))               # in place
+        assert all(torch.equal(a, b) for a, b in zip(mats, first)) and _kept(gi)
+
+
+def test_the_float64_form_is_the_oracles():
+    for s in ((1, 7, 12), (2, 12, 7)):
+        g, = _matrices([s], 1)
+        g = g.double()
+        for x, y in zip(_steps(g, 5, ABC, 1e-7), g):
+            assert np.abs(x.cpu().numpy() - T.orthogonalize(y.cpu().numpy(), 5, *ABC, 1e-7)).max() < 1e-12
+
+
+@pytest.mark.parametrize("shape", [(2, 40, 90), (3, 200, 150)])
+@pytest.mark.parametrize("kw", [dict(steps=1), dict(steps=2, coefficients=CONVERGING), dict(steps=12, coefficients=CONVERGING), dict(steps=8), dict(eps=1e-2),
+                                dict(eps=0.0), dict(steps=3, coefficients=(1.5, -0.5, 0.0)), dict(steps=4, coefficients=(1.0, 0.0, 0.0))])
+def test_settings(ctx, shape, kw):
+    from paper_2303_13775_amd import MatrixTensors
+    g, = _matrices([shape], 3)
+    out = torch.zeros_like(g)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), **kw)
+    _close("settings", out, *_expected(g.double(), kw.get("steps", 5), kw.get("coefficients", ABC), kw.get("eps", 1e-7)))
+
+
+def test_converging_steps_give_orthonormal_rows(ctx):
+    from paper_2303_13775_amd import MatrixTensors
+    g = torch.randn((2, 60, 200), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    out = torch.zeros_like(g)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), steps=20, coefficients=CONVERGING)
+    one = torch.eye(60, dtype=torch.float64, device="cuda")
+    assert float((out.double() @ out.double().transpose(1, 2) - one).abs().max()) < 300 * U
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-25, 1e25, 3e37])
+@pytest.mark.parametrize("shape", [(1, 20, 30), (2, 130, 140)])
+def test_values_of_any_size(ctx, scale, shape):
+    """The norm is a double sum: neither small nor large floats leave its range, and with eps 0 the size does not matter."""
+    from paper_2303_13775_amd import MatrixTensors
+    g = torch.randn(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)).clamp(-5, 5) * scale
+    out = torch.zeros_like(g)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), eps=0.0)
+    _close(scale, out, *_expected(g.double(), eps=0.0))
+
+
+@pytest.mark.parametrize("rows, cols", [(10, 20), (200, 130)])
+def test_zeros_and_values_that_are_not_finite(ctx, rows, cols):
+    """A matrix of zeros gives zeros, one with an infinity or a NaN is NaN throughout; the others of the stack do not notice."""
+    from paper_2303_13775_amd import MatrixTensors
+    for eps in (1e-7, 0.0):
+        g, = _matrices([(5, rows, cols)], 4)
+        alone = torch.zeros_like(g)
+        ctx.gsplit_orthogonalize(MatrixTensors([g], [alone]), eps=eps)
+        g[1], g[2, 3, 4], g[3, rows - 1, cols - 1] = 0.0, float("inf"), float("nan")
+        out = torch.zeros_like(g)
+        ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), eps=eps)
+        assert not out[1].any() and bool(out[2:4].isnan().all())
+        assert torch.equal(out[0], alone[0]) and torch.equal(out[4], alone[4])
+
+
+def test_rank_one_and_repeated_rows(ctx):
+    """Matrices whose singular values are mostly 0: their direction comes out, the rest stays at rounding times what the steps raise it by."""
+    from paper_2303_13775_amd import MatrixTensors
+    a, b = torch.linspace(-1, 1, 50, device="cuda"), torch.linspace(0.5, 2, 80, device="cuda")
+    g = torch.stack([torch.outer(a, b), torch.ones((50, 80), device="cuda"), torch.eye(50, 80, device="cuda")])
+    out = torch.zeros_like(g)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]))
+    _close("rank", out, *_expected(g.double()))
+
+
+def _types(kind, n):
+    return [F32] * n if kind == "f32" else [BF16] * n if kind == "bf16" else [(F32, BF16)[i % 2] for i in range(n)]
+
+
+def _muon_case(ctx, shapes, pk, gk, seed, *, lr=0.05, momentum=0.9, nesterov=True, weight_decay=0.1, scaling="shape", dev=False, **kw):
+    from paper_2303_13775_amd import MuonTensors
+    n = len(shapes)
+    ptypes, gtypes = _types(pk, n), _types(gk, n)
+    bg, grads = _room([g.to(t) for g, t in zip(_matrices(shapes, seed), gtypes)])
+    bm, moms = _room(_matrices(shapes, seed + 100))
+    bf, full = _room([p * 300 for p in _matrices(shapes, seed + 200)])
+    bp, params = _room([f.to(t) for f, t in zip(full, ptypes)])
+    masters = [f if t == BF16 else None for f, t in zip(full, ptypes)]
+    old = [[t.double() for t in ts] for ts in ([f if w is not None else p for p, f, w in zip(params, full, masters)], grads, moms)]
+    table = MuonTensors(params, grads, moms, masters)
+    step = dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, scaling=scaling, **kw)
+    if dev:
+        step["lr_dev"], step["lr"] = torch.tensor([lr], device="cuda"), 99.0
+        lr = float(np.float32(lr))
+    ctx.gsplit_muon_step(table, **step)
+    for i, (count, rows, cols) in enumerate(shapes):
+        if params[i].numel() == 0:
+            continue
+        p, g, m = (old[k][i] for k in range(3))
+        m1 = momentum * m + (1 - momentum) * g
+        terms = momentum * m.abs() + (1 - momentum) * g.abs()
+        assert bool(((moms[i].double() - m1).abs() <= 5 * U * terms).all())
+        u = momentum * m1 + (1 - momentum) * g if nesterov else m1
+        # what is orthogonalised is off by the rounding of the momentum and of its own terms: 8 u of them, which the steps raise as they raise the rest
+        want, off = _expected(u, kw.get("steps", 5), kw.get("coefficients", ABC), kw.get("eps", 1e-7))
+        gen = torch.Generator(device="cuda").manual_seed(7)
+        shaken = u + 8 * U * terms * (2 * torch.rand(u.shape, dtype=u.dtype, device="cuda", generator=gen) - 1)
+        off = off + 3 * (_steps(shaken, kw.get("steps", 5), kw.get("coefficients", ABC), kw.get("eps", 1e-7)) - want).flatten(1).abs().amax(1)
+        scale = {"plain": 1.0, "shape": math.sqrt(max(1.0, cols / rows)), "rms": 0.2 * math.sqrt(max(rows, cols))}[scaling]
+        p1 = (1 - lr * weight_decay) * p - lr * scale * want
+        tol = lr * scale * (off[:, None, None] + 3 * U * want.abs()) + 3 * U * p.abs() + 2 * U * p1.abs()
+        got = masters[i] if masters[i] is not None else params[i]
+        over = (got.double() - p1).abs() - tol
+        assert bool((over <= 0).all()), (i, shapes[i], float(over.max()))
+        if masters[i] is not None:
+            assert torch.equal(params[i], masters[i].bfloat16())
+        assert torch.equal(grads[i].double(), g)
+    assert all(_kept(b) for b in (bg, bm, bf, bp))
+
+
+@pytest.mark.parametrize("which", range(len(SETS) + len(LARGE)))
+@pytest.mark.parametrize("pk, gk", [("f32", "f32"), ("mixed", "bf16"), ("bf16", "mixed")])
+def test_muon(ctx, which, pk, gk):
+    _muon_case(ctx, (SETS + LARGE)[which], pk, gk, which)
+
+
+@pytest.mark.parametrize("kw", [dict(nesterov=False), dict(momentum=0.0), dict(weight_decay=0.0, scaling="plain"), dict(scaling="rms"), dict(dev=True), dict(lr=0.0),
+                                dict(steps=3, coefficients=CONVERGING, eps=1e-3)])
+def test_muon_settings(ctx, kw):
+    _muon_case(ctx, [(2, 60, 130), (1, 130, 60), (1, 17, 17)], "mixed", "f32", 5, **kw)
+
+
+def test_muon_of_a_gradient_that_is_not_finite(ctx):
+    from paper_2303_13775_amd import MuonTensors
+    g = torch.ones((3, 20, 30), device="cuda")
+    g[1, 2, 3] = float("inf")
+    p, m = torch.zeros_like(g), torch.zeros_like(g)
+    ctx.gsplit_muon_step(MuonTensors([p], [g], [m]))
+    assert bool(p[1].isnan().all()) and bool(p[0].isfinite().all()) and bool(p[2].isfinite().all())
+    assert int((~m.isfinite()).sum()) == 1
+
+
+@pytest.mark.parametrize("shapes", [[(2, 30, 50), (1, 70, 20)], [(26, 400, 512)]])
+def test_captured_steps(ctx, shapes):
+    """A step captured once, the learning rate in device memory, replayed with new gradients and eager work of the same context
+    between the replays: the bits of eager steps."""
+    from paper_2303_13775_amd import MatrixTensors, MuonTensors
+    grads, lr = _matrices(shapes, 1), torch.zeros(1, device="cuda")
+    state = lambda: ([p * 300 for p in _matrices(shapes, 2)], [torch.zeros_like(g) for g in grads], [torch.zeros_like(g) for g in grads])
+    (p, m, o), (pe, me, oe) = state(), state()
+    table, eager = MuonTensors(p, grads, m), MuonTensors(pe, grads, me)
+    orth, orth_e = MatrixTensors(grads, o), MatrixTensors(grads, oe)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.gsplit_orthogonalize(orth)
+        ctx.gsplit_muon_step(table, lr_dev=lr, weight_decay=0.1)
+    for k in range(4):
+        for g, new in zip(grads, _matrices(shapes, 10 + k)):
+            g.copy_(new)
+        lr.fill_(0.1 / (k + 1))
+        ctx.gsplit_orthogonalize(orth_e)
+        ctx.gsplit_muon_step(eager, lr_dev=lr, weight_decay=0.1)
+        graph.replay()
+        if k % 2:
+            torch.cuda.synchronize()
+        ctx.gsplit_orthogonalize(orth_e)
+        assert all(torch.equal(a, b) for x, y in ((p, pe), (m, me), (o, oe)) for a, b in zip(x, y)), k
+
+
+def test_another_stream(ctx):
+    from paper_2303_13775_amd import MatrixTensors
+    shapes = [(3, 90, 200), (1, 500, 300)]
+    mats, res = _matrices(shapes, 6), []
+    for s in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs = [torch.zeros_like(g) for g in mats]
+            ctx.gsplit_orthogonalize(MatrixTensors(mats, outs))
+            torch.cuda.synchronize()
+            res.append(outs)
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
+def test_refusals(ctx):
+    from paper_2303_13775_amd import GsplitError, MatrixTensors, MuonTensors
+    g = torch.ones((4, 6), device="cuda")
+    o = torch.zeros_like(g)
+    table = MatrixTensors([g], [o])
+    for kw in (dict(steps=0), dict(steps=65), dict(eps=-1.0), dict(coefficients=(4.0, 0.0, 0.0)), dict(coefficients=(float("nan"), 0.0, 0.0))):
+        with pytest.raises(GsplitError) as e:
+            ctx.gsplit_orthogonalize(table, **kw)
+        assert e.value.code == -1 and "gsplit_orthogonalize" in str(e.value)
+    muon = MuonTensors([g.clone()], [g], [o])
+    for kw in (dict(momentum=1.0), dict(lr=-1.0), dict(weight_decay=float("inf")), dict(steps=0)):
+        with pytest.raises(GsplitError) as e:
+            ctx.gsplit_muon_step(muon, **kw)
+        assert e.value.code == -1 and "gsplit_muon_step" in str(e.value)
+    with pytest.raises(KeyError):
+        ctx.gsplit_muon_step(muon, scaling="other")
+    x = torch.ones(100, device="cuda")
+    for bad in (lambda: MatrixTensors([g.t()]), lambda: MatrixTensors([g[0]]), lambda: MatrixTensors([g.half()]), lambda: MatrixTensors([g.cpu()]), lambda: MatrixTensors([g], [o[:3]]),
+                lambda: MatrixTensors([x[:50].view(5, 10)], [x[20:70].view(5, 10)]), lambda: MatrixTensors([g, g], [o, o]), lambda: MuonTensors([g], [g], [o]),
+                lambda: MuonTensors([g.bfloat16()], [g], [o]), lambda: MuonTensors([g.clone()], [g], [o.bfloat16()]), lambda: MuonTensors([g.clone()], [g.view(6, 4)], [o])):
+        with pytest.raises(AssertionError):
+            bad()
+    MatrixTensors([g, g], [o, o.clone()])       # what is only read may be listed twice
