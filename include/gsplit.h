@@ -617,7 +617,7 @@ GSPLIT_API int gsplit_group_rows(gsplit_ctx *ctx, const int32_t *d_group, int64_
  * outside the buffers.
  * d_work: 16-byte aligned working memory of gsplit_grouped_linear_work() bytes (NULL if that is 0, or without d_dw); one call
  * uses it at a time.  Asynchronous; may be captured at any time.
- * EINVAL for NULL or misaligned pointers, an unknown dtype, strides below their width, n_groups above GSPLIT_MAX_GROUPS, widths
+ * EINVAL for NULL or misaligned pointers, an unknown dtype, strides below their width or of 2^31 and more, n_groups above GSPLIT_MAX_GROUPS, widths
  * outside 1 .. 2^20, n_rows outside 0 .. 2^31 - 1, a backward call that asks for nothing. */
 typedef struct {
     int32_t dtype;

@@ -119,65 +119,79 @@ struct Along {
     }
 };
 
-// An operand with the contraction across its rows: element (i, k) at row(k)[i], i < cols; of these the ones from `first` on
+// An operand with the contraction across its rows: element (i, k) at row(k)[i], i < cols; of these the ones from `first` on.  A thread
+// takes W columns of the eight rows of a granule.
 template <class T, int ROWS>
 struct Across {
-    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, W = ROWS * KG / NT;       // W columns of eight rows a thread
-    static_assert(W * NT == ROWS * KG && (W == 1 || W == 2 || W == 4), "one item a thread");
-    int K, cols, col, base;         // this thread's first column; LDS row of it
-    T r[8][W];
+    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, W = ROWS * KG / NT, WORDS = W * (int)sizeof(T) / 4;
+    static_assert(W * NT == ROWS * KG && (WORDS == 1 || WORDS == 2), "one item a thread");
+    int cols, col, base;            // this thread's first column; LDS row of it
+    uint32_t r[8][WORDS];
 
-    __device__ __forceinline__ void init(int k_len, int n_cols, int first) {
-        K = k_len; cols = n_cols;
+    static __device__ __forceinline__ int granule() { return (int)threadIdx.x / (ROWS / W); }
+    __device__ __forceinline__ void init(int n_cols, int first) {
+        cols = n_cols;
         const int want = first + (int)threadIdx.x % (ROWS / W) * W;
         // past the last column: the last ones once more, whose granules are then written twice, with the same values
         col = max(0, min(want, cols - W));
         base = col - first;
     }
+    // from row(j), the row of the granule's contraction index j.  (No branch around a single load: each would wait for the one before.)
     template <class Row>
-    __device__ __forceinline__ void load(int t, const Row &row) {
-        const int g = threadIdx.x / (ROWS / W), k0 = t * KT;
-        const bool whole = k0 + KT <= K;
+    __device__ __forceinline__ void load(const Row &row) {
+        if (W > 1 && cols < W) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int k = k0 + Kind<T>::k_of(g, j);
-            const T *p = row(whole ? k : min(k, K - 1)) + col;
-            if (W > 1 && cols < W) {
+            for (int j = 0; j < 8; ++j) {
+                const T *p = row(j);
+                T v[W];
 #pragma unroll
-                for (int c = 0; c < W; ++c) r[j][c] = p[min(c, cols - 1)];
-            } else if constexpr (W * sizeof(T) == 4) {
-                const uint32_t a = *(const u32_any *)p;
-                __builtin_memcpy(r[j], &a, 4);
-            } else if constexpr (W * sizeof(T) == 8) {
-                const u32x2 a = *(const u32x2_any *)p;
-                __builtin_memcpy(r[j], &a, 8);
-            } else {
-                r[j][0] = p[0];
+                for (int c = 0; c < W; ++c) v[c] = p[min(c, cols - 1)];
+                __builtin_memcpy(r[j], v, sizeof(v));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const T *p = row(j) + col;
+                if constexpr (WORDS == 1) {
+                    r[j][0] = *(const u32_any *)p;
+                } else {
+                    const u32x2 a = *(const u32x2_any *)p;
+                    r[j][0] = a[0]; r[j][1] = a[1];
+                }
             }
         }
-        if (!whole) {
+    }
+    // zeros past the end of the contraction of K, in its tile t
+    __device__ __forceinline__ void cut(int t, int K) {
+        if ((t + 1) * KT <= K) return;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k0 + Kind<T>::k_of(g, j) >= K)
+        for (int j = 0; j < 8; ++j)
+            if (t * KT + Kind<T>::k_of(granule(), j) >= K)
 #pragma unroll
-                    for (int c = 0; c < W; ++c) r[j][c] = 0;
-        }
+                for (int w = 0; w < WORDS; ++w) r[j][w] = 0u;
+    }
+    __device__ __forceinline__ float at(int j, int c) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(r[j][c]);
+        else return __uint_as_float(c & 1 ? r[j][c / 2] & 0xFFFF0000u : r[j][c / 2] << 16);
     }
     __device__ __forceinline__ void store(uint4 *lds) const {
-        const int g = threadIdx.x / (ROWS / W);
 #pragma unroll
         for (int c = 0; c < W; ++c) {
             const int row = base + c;
             if (row < 0 || row >= ROWS) continue;
-            const int at = slot<T>(row, g);
+            const int to = slot<T>(row, granule());
             if constexpr (sizeof(T) == 4) {
                 float v[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = r[j][c];
-                land<T, ROWS>(lds, at, v);
+                for (int j = 0; j < 8; ++j) v[j] = at(j, c);
+                land<T, ROWS>(lds, to, v);
             } else {
-                lds[at] = make_uint4(r[0][c] | (uint32_t)r[1][c] << 16, r[2][c] | (uint32_t)r[3][c] << 16,
-                                     r[4][c] | (uint32_t)r[5][c] << 16, r[6][c] | (uint32_t)r[7][c] << 16);
+                // the low or the high halves of two rows' words side by side
+                const uint32_t pick = c & 1 ? 0x07060302u : 0x05040100u;
+                uint32_t w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] = __builtin_amdgcn_perm(r[2 * q + 1][c / 2], r[2 * q][c / 2], pick);
+                lds[to] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
     }
@@ -328,6 +342,9 @@ struct RowList {
     }
 };
 
+// where row r of a matrix starts: one multiplication (strides are below 2^31)
+__device__ __forceinline__ uint64_t row_at(int r, uint32_t ld) { return (uint64_t)(uint32_t)r * ld; }
+
 // Which tile a workgroup takes: workgroups are dealt round-robin to the eight XCDs, and consecutive tiles (the same rows, the same
 // matrix) belong into the L2 of one
 __device__ __forceinline__ int64_t tile_number(int64_t block, int64_t total) {
@@ -339,7 +356,7 @@ struct RowsArgs {
     const void *a, *w;
     const float *bias;
     void *c;
-    int64_t lda, ldc, ldw;
+    uint32_t lda, ldc, ldw;
     int32_t K, N, G;
     const int32_t *ptr;
     RowList list;
@@ -368,6 +385,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
     constexpr int BM = TL::BM, BN = TL::BN, KG = Kind<T>::KG, P = Kind<T>::PLANES;
     __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
     __shared__ int s_row[BM];
+    __shared__ __attribute__((aligned(16))) float s_bias[BN];
     const int64_t total = A.tiles_m * A.tiles_n, room = (total + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
         const int64_t x = tile_number(block, total);
@@ -375,27 +393,29 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
         if (x >= total || !find_spot<false>(A.ptr, A.G, A.list.n, BM, (int)(x / A.tiles_n), s)) continue;
         const int n0 = (int)(x % A.tiles_n) * BN;
         if (threadIdx.x < BM) s_row[threadIdx.x] = (int)threadIdx.x < s.rows ? A.list.at(s.first + threadIdx.x) : -1;
+        if (threadIdx.x < BN) s_bias[threadIdx.x] = A.bias && n0 + (int)threadIdx.x < A.N ? A.bias[(int64_t)s.g * A.N + n0 + threadIdx.x] : 0.f;
         if (!TRANSPOSED && n0 + BN > A.N) clear_rows<T, BN>(s_b);
         __syncthreads();
         const T *a = (const T *)A.a, *w = (const T *)A.w + (int64_t)s.g * A.K * A.N;
-        const auto a_row = [&](int i) { return a + (int64_t)max(s_row[i < s.rows ? i : 0], 0) * A.lda; };
+        const auto a_row = [&](int i) { return a + row_at(max(s_row[i < s.rows ? i : 0], 0), A.lda); };
         Along<T, BM> la;
         la.init(A.K, a_row);
         typename std::conditional<TRANSPOSED, Along<T, BN>, Across<T, BN>>::type lb;
-        const auto w_row = [&](int k) { return w + (int64_t)k * A.ldw; };
-        const auto w_col = [&](int i) { return w + (int64_t)min(n0 + i, A.N - 1) * A.ldw; };
+        const auto w_row = [&](int k) { return w + row_at(k, A.ldw); };
+        const auto w_col = [&](int i) { return w + row_at(min(n0 + i, A.N - 1), A.ldw); };
         if constexpr (TRANSPOSED) lb.init(A.K, w_col);
-        else lb.init(A.K, A.N, n0);
+        else lb.init(A.N, n0);
         const auto load = [&](int t) __attribute__((always_inline)) {
             la.load(t);
             if constexpr (TRANSPOSED) lb.load(t);
-            else lb.load(t, w_row);
+            else lb.load([&](int j) { return w_row(min(t * Kind<T>::KT + Kind<T>::k_of(lb.granule(), j), A.K - 1)); });
         };
         Sums<T, TL> sums;
         sums.clear();
         const int KT = (A.K + Kind<T>::KT - 1) / Kind<T>::KT;
         load(0);
         for (int t = 0; t < KT; ++t) {
+            if constexpr (!TRANSPOSED) lb.cut(t, A.K);
             la.store(s_a);
             lb.store(s_b);
             __syncthreads();
@@ -403,7 +423,6 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
             sums.multiply(s_a, s_b);
             __syncthreads();
         }
-        const float *bias = A.bias ? A.bias + (int64_t)s.g * A.N : nullptr;
         sums.finish(A.K, [&](int i, int k) { return k < A.K ? as_float(a_row(i)[k]) : 0.f; },
                     [&](int i, int k) {
                         if (k >= A.K) return 0.f;
@@ -413,10 +432,9 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
                     [&](int i, int j, const float (&v)[4]) {
             const int r = s_row[i], n = n0 + j, left = A.N - n;
             if (r < 0 || left <= 0) return;
-            float y[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = v[q] + (bias ? bias[min(n + q, A.N - 1)] : 0.f);
-            store4((T *)A.c + (int64_t)r * A.ldc + n, y, left);
+            const float4 b = *(const float4 *)&s_bias[j];
+            const float y[4] = {v[0] + b.x, v[1] + b.y, v[2] + b.z, v[3] + b.w};
+            store4((T *)A.c + row_at(r, A.ldc) + n, y, left);
         });
         __syncthreads();        // s_row is the next tile's
     }
@@ -424,7 +442,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
 
 struct WeightArgs {
     const void *x, *dy;
-    int64_t ldx, lddy;
+    uint32_t ldx, lddy;
     int32_t K, N, G;            // rows and columns of a gradient
     const int32_t *ptr;
     RowList list;
@@ -451,13 +469,34 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
         const int m0 = (int)(x % tiles / A.tiles_n) * BM, n0 = (int)(x % A.tiles_n) * BN;
         const T *xs = (const T *)A.x, *dys = (const T *)A.dy;
-        const auto row = [&](int k) { return (int64_t)max(A.list.at(s.first + k), 0); };
-        const auto x_row = [&](int k) { return xs + row(k) * A.ldx; };
-        const auto dy_row = [&](int k) { return dys + row(k) * A.lddy; };
+        const auto x_row = [&](int k) { return xs + row_at(max(A.list.at(s.first + k), 0), A.ldx); };
+        const auto dy_row = [&](int k) { return dys + row_at(max(A.list.at(s.first + k), 0), A.lddy); };
         Across<T, BM> la;
         Across<T, BN> lb;
-        la.init(s.rows, A.K, m0);
-        lb.init(s.rows, A.N, n0);
+        la.init(A.K, m0);
+        lb.init(A.N, n0);
+        // the rows of the next tile are looked up a tile ahead: their loads would wait for the list's
+        int next[8];
+        static_assert(BM == BN, "both operands' granules hold the same rows");
+        const auto look_up = [&](int t) __attribute__((always_inline)) {
+            int place[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) place[j] = s.first + min(t * Kind<T>::KT + Kind<T>::k_of(la.granule(), j), s.rows - 1);
+            if (A.list.rows) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) next[j] = A.list.rows[place[j]];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) next[j] = place[j];
+            }
+        };
+        const auto load = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) next[j] = (uint32_t)next[j] < (uint32_t)A.list.n ? next[j] : 0;
+            la.load([&](int j) { return xs + row_at(next[j], A.ldx); });
+            lb.load([&](int j) { return dys + row_at(next[j], A.lddy); });
+            look_up(t + 1);
+        };
         Sums<T, TL> sums;
         sums.clear();
         double col[Across<T, BN>::W] = {};
@@ -466,8 +505,10 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         if (n0 + BN > A.N) clear_rows<T, BN>(s_b);
         __syncthreads();
         const int KT = (s.rows + Kind<T>::KT - 1) / Kind<T>::KT;
-        if (KT > 0) { la.load(0, x_row); lb.load(0, dy_row); }
+        if (KT > 0) { look_up(0); load(0); }
         for (int t = 0; t < KT; ++t) {
+            la.cut(t, s.rows);
+            lb.cut(t, s.rows);
             la.store(s_a);
             lb.store(s_b);
             if (bias) {
@@ -475,12 +516,12 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
                 for (int c = 0; c < Across<T, BN>::W; ++c) {
                     float f = 0.f, h = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) { f += as_float(lb.r[j][c]); h += as_float(lb.r[j + 1][c]); }
+                    for (int j = 0; j < 8; j += 2) { f += lb.at(j, c); h += lb.at(j + 1, c); }
                     col[c] += (double)f + (double)h;
                 }
             }
             __syncthreads();
-            if (t + 1 < KT) { la.load(t + 1, x_row); lb.load(t + 1, dy_row); }
+            if (t + 1 < KT) load(t + 1);
             sums.multiply(s_a, s_b);
             __syncthreads();
         }
@@ -494,7 +535,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         });
         if (bias) {
             constexpr int W = Across<T, BN>::W;
-            const int g = threadIdx.x / (BN / W);
+            const int g = lb.granule();
 #pragma unroll
             for (int c = 0; c < W; ++c)
                 if (lb.base + c >= 0 && lb.base + c < BN) s_sum[g][lb.base + c] = col[c];
@@ -579,7 +620,7 @@ extern "C" int gsplit_grouped_linear_fwd(gsplit_ctx *ctx, const gsplit_grouped_c
             return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_fwd: ") + e);
         if (n_rows == 0) return (int)GSPLIT_OK;
         GsTimeScope ts(ctx, "grouped_fwd", -1, st);
-        launch_rows<false>(ctx, c->dtype, RowsArgs{d_x, d_w, d_bias, d_y, x_stride, y_stride, c->n_out, c->n_in, c->n_out, c->n_groups,
+        launch_rows<false>(ctx, c->dtype, RowsArgs{d_x, d_w, d_bias, d_y, (uint32_t)x_stride, (uint32_t)y_stride, (uint32_t)c->n_out, c->n_in, c->n_out, c->n_groups,
                                                    d_group_ptr, {d_rows, (int32_t)n_rows}, 0, 0}, st);
         return (int)GSPLIT_OK;
     });
@@ -613,12 +654,12 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
         const RowList list{d_rows, (int32_t)n_rows};
         if (d_dx && n_rows > 0) {
             GsTimeScope ts(ctx, "grouped_dx", -1, st);
-            launch_rows<true>(ctx, c->dtype, RowsArgs{d_dy, d_w, nullptr, d_dx, dy_stride, dx_stride, c->n_out, c->n_out, c->n_in,
+            launch_rows<true>(ctx, c->dtype, RowsArgs{d_dy, d_w, nullptr, d_dx, (uint32_t)dy_stride, (uint32_t)dx_stride, (uint32_t)c->n_out, c->n_out, c->n_in,
                                                       c->n_groups, d_group_ptr, list, 0, 0}, st);
         }
         if (d_dw) {
             const int t = weights_tile(c->n_in, c->n_out);
-            WeightArgs A{d_x, d_dy, x_stride, dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)chunk,
+            WeightArgs A{d_x, d_dy, (uint32_t)x_stride, (uint32_t)dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)chunk,
                          n_rows / chunk + c->n_groups, (int32_t)group_ceil(c->n_in, t), (int32_t)group_ceil(c->n_out, t), d_dw, d_dbias,
                          (float *)d_work, slabs};
             const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));

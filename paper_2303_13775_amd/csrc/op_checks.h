@@ -125,7 +125,7 @@ inline const char *op_check_grouped(const gsplit_grouped_config *c, int64_t n_ro
 inline const char *op_check_grouped_rows(const void *p, int64_t n_rows, int64_t width, int64_t stride, int size, bool needed) {
     if (!p) return needed && n_rows > 0 ? "NULL buffer" : nullptr;
     if (op_misaligned(p, size)) return "misaligned buffer";
-    return stride < width || stride > (int64_t)1 << 40 ? "stride below its width or out of range" : nullptr;
+    return stride < width || stride > INT32_MAX ? "stride below its width or out of range" : nullptr;
 }
 inline const char *op_check_grouped_lists(const gsplit_grouped_config *c, const int32_t *d_group_ptr, const int32_t *d_rows) {
     if (!d_group_ptr) return "NULL buffer";
