@@ -3,7 +3,7 @@
 //     X = G / (|G| + eps);   A = X X^T,   B = a I + b A + c A^2,   X <- B X      for X with no more rows than columns
 //
 // (a tall matrix' transpose: (X X^T) X = X (X^T X)).  A and B are symmetric: only the tiles of their lower triangles are formed.
-// All three products have both factors' contraction along the rows: X is kept with its transpose beside it.
+// The last product's X is read transposed on its way out of LDS (tile_core.h), so X is kept one way only.
 //
 // The steps start from singular values far below 1 and raise the small ones by a at most each, 485 in all: what the products round
 // off small directions is raised with them, so a step's products have to be as good as float's.  Float matrix instructions reach a
@@ -20,7 +20,9 @@
 
 namespace {
 
-typedef float floatx16 __attribute__((ext_vector_type(16)));
+#include "tile_core.h"
+
+typedef floatx16_t floatx16;
 typedef _Float16 half;
 typedef half halfx4 __attribute__((ext_vector_type(4)));
 typedef half halfx8 __attribute__((ext_vector_type(8)));
@@ -53,11 +55,13 @@ struct Call {
     // words of matrix i of the stack
     __device__ __forceinline__ uint4 *x(const Stack &s, int i, int which) const {
         return work + s.at + ((int64_t)which * s.count + i) * ((int64_t)s.mp * s.np / 4);
-    }       // which: 0, 1 X and its transpose, 2, 3 the other pair
+    }       // (a step reads one and writes the other)
     __device__ __forceinline__ uint4 *a(const Stack &s, int i, int which) const {
-        return work + s.at + s.count * (int64_t)s.mp * s.np + ((int64_t)which * s.count + i) * ((int64_t)s.mp * s.mp / 4);
+        return work + s.at + s.count * ((int64_t)s.mp * s.np / 2) + ((int64_t)which * s.count + i) * ((int64_t)s.mp * s.mp / 4);
+    }       // 0: A, 1: B
+    __device__ __forceinline__ double *sums(const Stack &s) const {
+        return (double *)(work + s.at + s.count * ((int64_t)s.mp * s.np / 2 + (int64_t)s.mp * s.mp / 2));
     }
-    __device__ __forceinline__ double *sums(const Stack &s) const { return (double *)(work + s.at + s.count * ((int64_t)s.mp * s.np + (int64_t)s.mp * s.mp / 2)); }
 };
 static_assert(sizeof(Call) <= 4096 - 256, "kernel arguments");
 
@@ -76,6 +80,16 @@ __device__ __forceinline__ float mixed(const Momentum &M, float m, float g) { re
 template <class T> __device__ __forceinline__ float value(const void *p, int64_t i) { return (float)((const T *)p)[i]; }
 __device__ __forceinline__ float value(const void *p, int64_t i, bool half_type) { return half_type ? value<bf16>(p, i) : value<float>(p, i); }
 
+__device__ __forceinline__ void load4(const Stack &s, int64_t at, float (&g)[4]) {
+    if (s.half_g) {
+        const bf16x4 q = *(const bf16x4_any *)((const bf16 *)s.g + at);
+        for (int k = 0; k < 4; ++k) g[k] = (float)q[k];
+    } else {
+        const floatx4 q = *(const floatx4_any *)((const float *)s.g + at);
+        for (int k = 0; k < 4; ++k) g[k] = q[k];
+    }
+}
+
 // momenta, and a chunk's sum of squares of what is to be orthogonalised (double: any float's square, in a fixed order)
 template <bool MOMENTUM>
 __global__ __launch_bounds__(NT) void k_newton_sums(Call C, Momentum M) {
@@ -89,13 +103,7 @@ __global__ __launch_bounds__(NT) void k_newton_sums(Call C, Momentum M) {
         float g[4] = {}, m[4] = {};
         const int n = (int)min<int64_t>(4, hi - i);
         if (n == 4) {
-            if (s.half_g) {
-                const bf16x4 q = *(const bf16x4_any *)((const bf16 *)s.g + base + i);
-                for (int k = 0; k < 4; ++k) g[k] = (float)q[k];
-            } else {
-                const floatx4 q = *(const floatx4_any *)((const float *)s.g + base + i);
-                for (int k = 0; k < 4; ++k) g[k] = q[k];
-            }
+            load4(s, base + i, g);
             if (MOMENTUM) {
                 floatx4 q = *(const floatx4_any *)(s.mom + base + i);
                 for (int k = 0; k < 4; ++k) q[k] = m[k] = M.keep * q[k] + M.take * g[k];
@@ -118,26 +126,34 @@ __global__ __launch_bounds__(NT) void k_newton_sums(Call C, Momentum M) {
     if (threadIdx.x == 0) C.sums(s)[item] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
 }
 
-__device__ __forceinline__ void split(float v, half &hi, half &lo) {
-    hi = (half)v;
-    lo = (half)(v - (float)hi);
+__device__ __forceinline__ floatx16 mfma_half(const halfx8 &a, const halfx8 &b, const floatx16 &c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ floatx16 zero16() {
+    floatx16 z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z[r] = 0.f;
+    return z;
+}
+
 // where column c of a row of `ld` columns lies, in halves; its lo part 32 further on
 __device__ __forceinline__ int64_t place(int64_t row, int ld, int c) { return row * 2 * ld + (c >> 5) * 64 + (c & 31); }
+__device__ __forceinline__ void split4(const float (&v)[4], halfx4 &hi, halfx4 &lo) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        hi[k] = (half)v[k];
+        lo[k] = (half)(v[k] - (float)hi[k]);
+    }
+}
 // four values side by side (c a multiple of 4)
 __device__ __forceinline__ void put4(half *p, const float (&v)[4]) {
     halfx4 hi, lo;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        half h, l;
-        split(v[k], h, l);
-        hi[k] = h; lo[k] = l;
-    }
+    split4(v, hi, lo);
     *(halfx4 *)p = hi;
     *(halfx4 *)(p + 32) = lo;
 }
 
-// X = u / (|u| + eps), and its transpose: a workgroup a tile of 64 x 64 of the padded matrix
+// X = u / (|u| + eps): a workgroup a tile of 64 x 64 of the padded matrix
 template <bool MOMENTUM>
 __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double eps) {
     __shared__ float s_x[64][65];
@@ -149,6 +165,29 @@ __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double 
     const int tiles = rp / 64 * (cp / 64), item = blockIdx.x - C.first[k], i = item / tiles, tile = item % tiles;
     const int r0 = tile / (cp / 64) * 64, c0 = tile % (cp / 64) * 64;
     const int slots = (int)((size + NEWTON_CHUNK - 1) / NEWTON_CHUNK);
+    const int c = threadIdx.x % 16 * 4, n = min(max(s.cols - c0 - c, 0), 4);
+    float u[4][4] = {};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int r = r0 + (int)threadIdx.x / 16 + 16 * x;
+        const int64_t at = i * size + (int64_t)r * s.cols + c0 + c;
+        if (r >= s.rows) continue;
+        float m[4] = {};
+        if (n == 4) {
+            load4(s, at, u[x]);
+            if (MOMENTUM) {
+                const floatx4 q = *(const floatx4_any *)(s.mom + at);
+                for (int q4 = 0; q4 < 4; ++q4) m[q4] = q[q4];
+            }
+        } else {
+            for (int q = 0; q < n; ++q) {
+                u[x][q] = value(s.g, at + q, s.half_g);
+                if (MOMENTUM) m[q] = s.mom[at + q];
+            }
+        }
+        if (MOMENTUM)
+            for (int q = 0; q < 4; ++q) u[x][q] = mixed(M, m[q], u[x][q]);
+    }
     double sum = 0.0;
     for (int j = threadIdx.x; j < slots; j += NT) sum += C.sums(s)[(int64_t)i * slots + j];
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
@@ -157,25 +196,27 @@ __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double 
     const double norm = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) + eps;
     // a matrix of zeros stays one; of a norm that is not finite nothing is left
     const double factor = norm < INFINITY ? norm > 0.0 ? (double)SCALE_X / norm : 0.0 : NAN;
-    const int c = threadIdx.x % 16 * 4;
-    for (int r = threadIdx.x / 16; r < 64; r += NT / 16) {
+    half *const out = (half *)C.x(s, i, 0);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int r = (int)threadIdx.x / 16 + 16 * x;
         float v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float u = 0.f;
-            if (r0 + r < s.rows && c0 + c + q < s.cols) {
-                const int64_t at = i * size + (int64_t)(r0 + r) * s.cols + c0 + c + q;
-                u = value(s.g, at, s.half_g);
-                if (MOMENTUM) u = mixed(M, s.mom[at], u);
-            }
-            s_x[r][c + q] = v[q] = (float)(u * factor);
+        for (int q = 0; q < 4; ++q) v[q] = (float)(u[x][q] * factor);
+        if (s.tall) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) s_x[r][c + q] = v[q];
+        } else {
+            put4(out + place(r0 + r, cp, c0 + c), v);
         }
-        put4((half *)C.x(s, i, s.tall ? 1 : 0) + place(r0 + r, cp, c0 + c), v);
     }
+    if (!s.tall) return;
     __syncthreads();
-    for (int r = threadIdx.x / 16; r < 64; r += NT / 16) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const int r = (int)threadIdx.x / 16 + 16 * x;
         const float v[4] = {s_x[c][r], s_x[c + 1][r], s_x[c + 2][r], s_x[c + 3][r]};
-        put4((half *)C.x(s, i, s.tall ? 0 : 1) + place(c0 + r, rp, r0 + c), v);
+        put4(out + place(c0 + r, rp, r0 + c), v);
     }
 }
 
@@ -185,7 +226,7 @@ __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double 
 enum : int { FORM_A, FORM_B, FORM_X, FORM_LAST };
 struct Step {
     float a, b, c;
-    int32_t from;               // which pair of X (0 or 2)
+    int32_t from;               // which X (0 or 1)
     float lr, keep, decay;      // the update: p = keep p - lr scale x, keep = 1 - lr decay
     const float *d_lr;
     int32_t update;
@@ -233,50 +274,266 @@ __device__ __forceinline__ void write_result(const Stack &s, int64_t at, const f
     }
 }
 
-// C = P Q^T of padded matrices, a tile of TILE x TILE a workgroup of four waves, SUB x 32 of the contraction a stage.  The stage
-// behind the one in work is fetched straight into LDS, after the one in work has been read into registers.
-template <int TILE, int SUB, int FORM>
-__global__ __launch_bounds__(NT, 2) void k_newton(Call C, Step S) {
-    constexpr int MI = TILE / 64, STAGE = 2 * TILE * 8 * SUB, LOADS = STAGE / NT;
-    __shared__ __attribute__((aligned(16))) uint4 lds[2][STAGE];
-    const int block = blockIdx.x, k = stack_of(C, block);
-    const Stack &s = C.s[k];
+// What of C = P Q^T a workgroup forms
+struct Part { int stack, i, ti, tj; };
+template <int TILE, int FORM>
+__device__ __forceinline__ Part part_of(const Call &C) {
+    Part p;
+    p.stack = stack_of(C, blockIdx.x);
+    const Stack &s = C.s[p.stack];
     const int tm = s.mp / TILE, tn = s.np / TILE;
     const int tiles = FORM <= FORM_B ? tm * (tm + 1) / 2 : tm * tn;
     // consecutive tiles belong into one XCD's L2; workgroups are dealt round-robin to the eight
-    int item = block - C.first[k];
-    const int of = C.first[k + 1] - C.first[k], whole = of / 8 * 8;
+    int item = blockIdx.x - C.first[p.stack];
+    const int of = C.first[p.stack + 1] - C.first[p.stack], whole = of / 8 * 8;
     if (item < whole) item = (item & 7) * (of / 8) + (item >> 3);
-    const int i = item / tiles, tile = item % tiles;
-    int ti, tj;
+    p.i = item / tiles;
+    const int tile = item % tiles;
     if (FORM <= FORM_B) {
-        ti = (int)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
-        while (ti * (ti + 1) / 2 > tile) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
-        tj = tile - ti * (ti + 1) / 2;
+        p.ti = (int)((sqrtf(8.f * (float)tile + 1.f) - 1.f) * 0.5f);
+        while (p.ti * (p.ti + 1) / 2 > tile) --p.ti;
+        while ((p.ti + 1) * (p.ti + 2) / 2 <= tile) ++p.ti;
+        p.tj = tile - p.ti * (p.ti + 1) / 2;
     } else {
-        ti = tile % tm; tj = tile / tm;
+        p.ti = tile % tm; p.tj = tile / tm;
     }
-    const int m0 = ti * TILE, n0 = tj * TILE;
-    const uint4 *P = FORM == FORM_A ? C.x(s, i, S.from) : C.a(s, i, FORM == FORM_B ? 0 : 1);
-    const uint4 *Q = FORM == FORM_A ? P : FORM == FORM_B ? P : C.x(s, i, S.from + 1);
-    const int K = FORM == FORM_A ? s.np : s.mp;
+    return p;
+}
+struct Factors { const uint4 *p, *q; int k; };
+template <int FORM>
+__device__ __forceinline__ Factors factors_of(const Call &C, const Stack &s, int i, const Step &S) {
+    const uint4 *p = FORM == FORM_A ? C.x(s, i, S.from) : C.a(s, i, FORM == FORM_B ? 0 : 1);
+    return {p, FORM <= FORM_B ? p : C.x(s, i, S.from), FORM == FORM_A ? s.np : s.mp};
+}
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    // granule p of row r of LDS holds granule p ^ (r / 2) % 8 of the row: 16 rows of one granule column lie in 16 bank groups
-    const auto turn = [](int row) __attribute__((always_inline)) { return (row >> 1) & 7; };
-    // a wave's instruction fetches eight rows of 128 bytes, a granule a lane
-    const uint32_t ld = (uint32_t)K * 4u;               // bytes of a row
-    const auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
+// the learning rate and what a step keeps of a parameter
+__device__ __forceinline__ void rates(const Step &S, float &keep, float &lr) {
+    lr = S.lr; keep = S.keep;
+    if (S.d_lr) {
+        lr = *S.d_lr;
+        keep = (float)(1.0 - (double)lr * S.decay);
+    }
+}
+
+// What becomes of a wave's block of MI x MI times 32 x 32 sums at (row0, col0).  A lane has four columns side by side of one row, sixteen
+// times; in `lds` (the wave's own) rows are put together, or columns where the transpose is asked for, and go out as they lie in memory.
+// `mirror`: the block lies below the diagonal of a symmetric matrix and fills its mirror image too.
+template <int MI, int FORM>
+__device__ __forceinline__ void finish(const Call &C, const Stack &s, int i, const Step &S, const floatx16 (&acc)[MI][MI], core_u32x4 *lds, int row0, int col0,
+                                       bool mirror) {
+    constexpr int SIDE = 32 * MI, ROW = 8 * MI;         // rows of a block, granules of one
+    const int lane = threadIdx.x & 63, l32 = lane & 31, half_ = lane >> 5;
+    const auto granule = [&](int r, int g) __attribute__((always_inline)) { return lds + r * ROW + (g ^ (r & (ROW - 1))); };
+    // rows of the block, four values side by side: a block's 32 columns are 4 granules of hi and 4 of lo, or 8 of floats
+    const auto pair_at = [&](int r, int c, int lo) __attribute__((always_inline)) { return (halfx4 *)granule(r, c / 32 * 8 + lo * 4 + c % 32 / 8) + (c / 4 & 1); };
+    const auto put_pair = [&](int r, int c, const float (&v)[4]) __attribute__((always_inline)) {
+        halfx4 hi, lo;
+        split4(v, hi, lo);
+        *pair_at(r, c, 0) = hi;
+        *pair_at(r, c, 1) = lo;
+    };
+    // lanes read what others have written, and write what others have read (LDS does a wave's instructions in their order)
+    const auto settle = [] __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    // granules of the block and of its place in memory: f(row, granule, where it lies in LDS)
+    const auto granules = [&](auto f) __attribute__((always_inline)) {
+        settle();
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int x = j * (NT / 64) + wave;         // eight rows of one sub-tile
-            const int sub = x / (2 * TILE / 8), row = x % (2 * TILE / 8) * 8;
-            const char *base = (const char *)(row < TILE ? P : Q) + (int64_t)(row < TILE ? m0 + row : n0 + row - TILE) * ld
-                               + (int64_t)(t * SUB + sub) * 128;
-            const uint32_t off = (uint32_t)(lane >> 3) * ld + (uint32_t)(((lane & 7) ^ turn((row & 8) + (lane >> 3))) * 16);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(base + off),
-                                             (__attribute__((address_space(3))) void *)&lds[stage][x * 64], 16, 0, 0);
+        for (int j = 0; j < SIDE * ROW / 64; ++j) {
+            const int x = j * 64 + lane, r = x / ROW, g = x % ROW;
+            f(r, g, granule(r, g));
+        }
+        settle();
+    };
+    // each(row, column, four values) of the block; turned: transposed
+    const auto each = [&](bool turned, auto value_of, auto f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int a = 0; a < MI; ++a)
+#pragma unroll
+            for (int b = 0; b < MI; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = 32 * a + l32, c = 32 * b + 8 * q + 4 * half_;
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = acc[a][b][4 * q + j];
+                    value_of(r, c, v);
+                    if (turned) transpose4(v);
+                    if (turned) f(c + (lane & 3), r & ~3, v);
+                    else f(r, c, v);
+                }
+    };
+    // rows of granules of a matrix of pairs
+    const auto pairs = [&](uint4 *m, int ld, int r0, int c0) __attribute__((always_inline)) {
+        return [=](int r, int g) __attribute__((always_inline)) { return (core_u32x4 *)m + (int64_t)(r0 + r) * (ld / 4) + c0 / 4 + g; };
+    };
+    if constexpr (FORM == FORM_LAST) {
+        float keep, lr;
+        rates(S, keep, lr);
+        const auto scaled = [&](int, int, float (&v)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= 1.f / (SCALE_B * SCALE_X);
+        };
+        each(s.tall, scaled, [&](int r, int c, const float (&v)[4]) __attribute__((always_inline)) {
+            *(floatx4 *)granule(r, c / 4) = floatx4{v[0], v[1], v[2], v[3]};
+        });
+        const int64_t base = (int64_t)i * s.rows * s.cols;
+        const int first_r = s.tall ? col0 : row0, first_c = s.tall ? row0 : col0;
+        granules([&](int r, int g, const core_u32x4 *from) __attribute__((always_inline)) {
+            const int row = first_r + r, col = first_c + 4 * g;
+            const floatx4 q = *(const floatx4 *)from;
+            const float v[4] = {q[0], q[1], q[2], q[3]};
+            if (row < s.rows && col < s.cols) write_result(s, base + (int64_t)row * s.cols + col, v, s.cols - col, S.update, keep, lr * s.scale);
+        });
+    } else {
+        if constexpr (FORM == FORM_B) {         // A's block
+            const auto at = pairs(C.a(s, i, 0), s.mp, row0, col0);
+            core_u32x4 q[SIDE * ROW / 64];
+            int n = 0;
+            granules([&](int r, int g, core_u32x4 *) __attribute__((always_inline)) { q[n++] = *at(r, g); });
+            n = 0;
+            granules([&](int, int, core_u32x4 *to) __attribute__((always_inline)) { *to = q[n++]; });
+        }
+        const auto scaled = [&](int r, int c, float (&v)[4]) __attribute__((always_inline)) {
+            if constexpr (FORM == FORM_B) {
+                const halfx4 hi = *pair_at(r, c, 0), lo = *pair_at(r, c, 1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    v[j] = S.c * (SCALE_B / (SCALE_A * SCALE_A)) * v[j] + S.b * (SCALE_B / SCALE_A) * ((float)hi[j] + (float)lo[j])
+                           + (row0 + r == col0 + c + j ? S.a * SCALE_B : 0.f);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] *= FORM == FORM_A ? SCALE_A / (SCALE_X * SCALE_X) : 1.f / SCALE_B;
+            }
+        };
+        uint4 *out = FORM == FORM_X ? C.x(s, i, S.from ^ 1) : C.a(s, i, FORM == FORM_A ? 0 : 1);
+        const int ld = FORM == FORM_X ? s.np : s.mp;
+        const auto at = pairs(out, ld, row0, col0);
+        floatx16 kept[FORM == FORM_B ? MI : 1][FORM == FORM_B ? MI : 1];         // (A's block in LDS makes room for the result)
+        if constexpr (FORM == FORM_B) {
+#pragma unroll
+            for (int a = 0; a < MI; ++a)
+#pragma unroll
+                for (int b = 0; b < MI; ++b)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float v[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = acc[a][b][4 * q + j];
+                        scaled(32 * a + l32, 32 * b + 8 * q + 4 * half_, v);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) kept[a][b][4 * q + j] = v[j];
+                    }
+            settle();
+        }
+        const auto final = [&](int r, int c, float (&v)[4]) __attribute__((always_inline)) {
+            if constexpr (FORM == FORM_B) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = kept[r / 32][c / 32][c % 32 / 8 * 4 + j];
+            } else {
+                scaled(r, c, v);
+            }
+        };
+        each(false, final, put_pair);
+        granules([&](int r, int g, const core_u32x4 *from) __attribute__((always_inline)) { *at(r, g) = *from; });
+        if (FORM != FORM_X && mirror) {
+            each(true, final, put_pair);
+            const auto image = pairs(out, ld, col0, row0);
+            granules([&](int r, int g, const core_u32x4 *from) __attribute__((always_inline)) { *image(r, g) = *from; });
+        }
+    }
+}
+
+// A tile of 64 x 64 a workgroup of four waves, 64 of the contraction a stage.  The stage behind the one in work is fetched straight into
+// LDS, after the one in work has been read into registers.  Contractions are short here and so are the sums: lo lo' is summed too, and
+// what is small has a sum of its own (with three products and one sum, matrices of 3 x 6 were 30 times 2^-24 off).
+template <int FORM>
+__global__ __launch_bounds__(NT, 2) void k_newton_small(Call C, Step S) {
+    constexpr int TILE = 64, SUB = 2, HALF = TILE * 8 * SUB;            // granules of a stage of one factor
+    constexpr bool ACROSS = FORM >= FORM_X;
+    __shared__ __attribute__((aligned(16))) core_u32x4 lds[2][2 * HALF];
+    const Part part = part_of<TILE, FORM>(C);
+    const Stack &s = C.s[part.stack];
+    const Factors F = factors_of<FORM>(C, s, part.i, S);
+    const int m0 = part.ti * TILE, n0 = part.tj * TILE, lane = threadIdx.x & 63, wave = core_wave();
+    const uint32_t ld = (uint32_t)F.k * 4u, ldx = (uint32_t)s.np * 4u;          // bytes of a row
+    const auto fetch = [&](int t, core_u32x4 *to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < HALF / NT; ++j) {
+            const int x = j * 4 + wave, sub = x / (TILE / 8), row = x % (TILE / 8) * 8;
+            const uint32_t off = (uint32_t)along_row(lane) * ld + along_granule(x, lane) * 16;
+            core_fetch((const char *)F.p + (int64_t)(m0 + row) * ld + (int64_t)(t * SUB + sub) * 128 + off, to + x * 64);
+            if constexpr (ACROSS) {             // four rows of 256 bytes an instruction
+                const int r = 4 * x + (lane >> 4);
+                core_fetch((const char *)F.q + (int64_t)(t * SUB * 32 + r) * ldx + (int64_t)n0 * 4 + ((lane & 15) ^ (4 * (r & 3))) * 16, to + HALF + x * 64);
+            } else {
+                core_fetch((const char *)F.q + (int64_t)(n0 + row) * ld + (int64_t)(t * SUB + sub) * 128 + off, to + HALF + x * 64);
+            }
+        }
+    };
+    const int half_ = lane >> 5, l32 = lane & 31, wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
+    floatx16 acc[1][1], low = zero16();
+    acc[0][0] = zero16();
+    const int T = F.k / (32 * SUB);
+    fetch(0, lds[0]);
+    for (int t = 0; t < T; ++t) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const core_u32x4 *now = lds[t & 1];
+        halfx8 fp[SUB][2][2], fq[SUB][2][2];            // [sub-tile][16 of it][hi, lo]
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const int g = 4 * q + 2 * h + half_;
+                    fp[u][h][q] = __builtin_bit_cast(halfx8, now[u * TILE * 8 + along_at(wm + l32, g)]);
+                    if constexpr (ACROSS) fq[u][h][q] = __builtin_bit_cast(halfx8, across_fragment<16>(now + HALF, 2 * u + h, wn / 4 + 4 * q));
+                    else fq[u][h][q] = __builtin_bit_cast(halfx8, now[HALF + u * TILE * 8 + along_at(wn + l32, g)]);
+                }
+        if (t + 1 < T) fetch(t + 1, lds[(t + 1) & 1]);
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                low = mfma_half(fq[u][h][1], fp[u][h][1], low);
+                acc[0][0] = mfma_half(fq[u][h][0], fp[u][h][0], acc[0][0]);
+                low = mfma_half(fq[u][h][1], fp[u][h][0], low);
+                low = mfma_half(fq[u][h][0], fp[u][h][1], low);
+            }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] += low[r];
+    __syncthreads();
+    finish<1, FORM>(C, s, part.i, S, acc, &lds[0][0] + wave * 32 * 8, m0 + wm, n0 + wn, part.ti != part.tj);
+}
+
+// A tile of 128 x 128 a workgroup of four waves, 64 x 64 each (tile_core.h), two workgroups a compute unit.  What is small of a product
+// is summed first.
+template <int FORM>
+__global__ __launch_bounds__(NT, 2) void k_newton_large(Call C, Step S) {
+    constexpr int TILE = NEWTON_TILE, MI = 2, WAVES = NT / 64, HALF = TILE * 8;
+    constexpr bool ACROSS = FORM >= FORM_X;
+    __shared__ __attribute__((aligned(16))) core_u32x4 lds[2][2 * HALF];
+    const Part part = part_of<TILE, FORM>(C);
+    const Stack &s = C.s[part.stack];
+    const Factors F = factors_of<FORM>(C, s, part.i, S);
+    const int m0 = part.ti * TILE, n0 = part.tj * TILE, lane = threadIdx.x & 63, wave = core_wave();
+    const uint32_t ld = (uint32_t)F.k * 4u, ldx = (uint32_t)s.np * 4u;          // bytes of a row
+    // (a lane's part of the address is the same in all of a wave's instructions: they are a multiple of sixteen rows apart)
+    const uint32_t off = (uint32_t)along_row(lane) * ld + (uint32_t)along_granule(wave, lane) * 16u;
+    const uint32_t off_q = ACROSS ? (uint32_t)(lane >> 5) * ldx + (uint32_t)((lane & 31) ^ (4 * ((2 * wave + (lane >> 5)) & 3))) * 16u : off;
+    const char *const p0 = (const char *)F.p + (int64_t)(m0 + 8 * wave) * ld;
+    const char *const q0 = (const char *)F.q + (ACROSS ? (int64_t)(2 * wave) * ldx + (int64_t)n0 * 4 : (int64_t)(n0 + 8 * wave) * ld);
+    const auto fetch = [&](int t, core_u32x4 *to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < HALF / NT; ++j) {
+            core_fetch(p0 + (int64_t)(8 * WAVES * j) * ld + (int64_t)t * 128 + off, to + (WAVES * j + wave) * 64);
+            const char *q = ACROSS ? q0 + (int64_t)(32 * t + 2 * WAVES * j) * ldx : q0 + (int64_t)(8 * WAVES * j) * ld + (int64_t)t * 128;
+            core_fetch(q + off_q, to + HALF + (WAVES * j + wave) * 64);
         }
     };
     const int half_ = lane >> 5, l32 = lane & 31, wm = (wave & 1) * (TILE / 2), wn = (wave >> 1) * (TILE / 2);
@@ -284,96 +541,32 @@ __global__ __launch_bounds__(NT, 2) void k_newton(Call C, Step S) {
 #pragma unroll
     for (int a = 0; a < MI; ++a)
 #pragma unroll
-        for (int b = 0; b < MI; ++b)
+        for (int b = 0; b < MI; ++b) acc[a][b] = zero16();
+    struct Frag { halfx8 p[MI][2], q[MI][2]; };
+    core_contract<2, Frag>(F.k / 32, lds, fetch,
+        [&](Frag &f, const core_u32x4 *now, int h) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
-    const int T = K / (32 * SUB);
-    fetch(0, 0);
-    for (int t = 0; t < T; ++t) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        const uint4 *now = lds[t & 1];
-        halfx8 fp[SUB][2][MI][2], fq[SUB][2][MI][2];            // [sub-tile][16 of it][block][hi, lo]
+            for (int q = 0; q < 2; ++q) {
+                const int g = 4 * q + 2 * h + half_;
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+                for (int a = 0; a < MI; ++a) f.p[a][q] = __builtin_bit_cast(halfx8, now[along_at(wm + 32 * a + l32, g)]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int b = 0; b < MI; ++b) {
+                    if constexpr (ACROSS) f.q[b][q] = __builtin_bit_cast(halfx8, across_fragment<32>(now + HALF, h, wn / 4 + 8 * b + 4 * q));
+                    else f.q[b][q] = __builtin_bit_cast(halfx8, now[HALF + along_at(wn + 32 * b + l32, g)]);
+                }
+            }
+        },
+        [&](const Frag &f) __attribute__((always_inline)) {
+#pragma unroll
+            for (int x = 0; x < 3; ++x)         // hi lo', lo hi', hi hi'
 #pragma unroll
                 for (int a = 0; a < MI; ++a)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int rp = wm + 32 * a + l32, rq = wn + 32 * a + l32, g = 4 * q + 2 * h + half_;
-                        fp[u][h][a][q] = __builtin_bit_cast(halfx8, now[(u * 2 * TILE + rp) * 8 + (g ^ turn(rp))]);
-                        fq[u][h][a][q] = __builtin_bit_cast(halfx8, now[(u * 2 * TILE + TILE + rq) * 8 + (g ^ turn(rq))]);
-                    }
-        if (t + 1 < T) fetch(t + 1, (t + 1) & 1);
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int q = 0; q < 3; ++q)
-#pragma unroll
-                    for (int a = 0; a < MI; ++a)
-#pragma unroll
-                        for (int b = 0; b < MI; ++b)
-                            acc[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fq[u][h][b][q == 1], fp[u][h][a][q == 2], acc[a][b], 0, 0, 0);
-    }
-
-    float lr = S.lr, keep = S.keep;
-    if (FORM == FORM_LAST && S.d_lr) {
-        lr = *S.d_lr;
-        keep = (float)(1.0 - (double)lr * S.decay);
-    }
-    // a lane has four columns side by side of one row, sixteen of a block
-#pragma unroll
-    for (int a = 0; a < MI; ++a)
-#pragma unroll
-        for (int b = 0; b < MI; ++b)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int row = m0 + wm + 32 * a + l32, col = n0 + wn + 32 * b + 8 * q + 4 * half_;
-                float v[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[a][b][4 * q + j];
-                // what the transposed place gets: four rows side by side of one column, lane % 4 of the four
-                const int trow = row & ~3, tcol = col + (lane & 3);
-                if (FORM == FORM_A || FORM == FORM_B) {
-                    half *out = (half *)C.a(s, i, FORM == FORM_A ? 0 : 1);
-                    if (FORM == FORM_A) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] *= SCALE_A / (SCALE_X * SCALE_X);
-                    } else {
-                        const half *A = (const half *)P + place(row, s.mp, col);
-                        const halfx4 hi = *(const halfx4 *)A, lo = *(const halfx4 *)(A + 32);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            v[j] = S.c * (SCALE_B / (SCALE_A * SCALE_A)) * v[j] + S.b * (SCALE_B / SCALE_A) * ((float)hi[j] + (float)lo[j])
-                                   + (row == col + j ? S.a * SCALE_B : 0.f);
-                    }
-                    put4(out + place(row, s.mp, col), v);
-                    if (ti != tj) {
-                        transpose4(v);
-                        put4(out + place(tcol, s.mp, trow), v);
-                    }
-                } else if (FORM == FORM_X) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= 1.f / SCALE_B;
-                    put4((half *)C.x(s, i, S.from ^ 2) + place(row, s.np, col), v);
-                    transpose4(v);
-                    put4((half *)C.x(s, i, (S.from ^ 2) + 1) + place(tcol, s.mp, trow), v);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= 1.f / (SCALE_B * SCALE_X);
-                    const int64_t base = (int64_t)i * s.rows * s.cols;
-                    if (s.tall) {
-                        transpose4(v);
-                        if (tcol < s.n && trow < s.m) write_result(s, base + (int64_t)tcol * s.cols + trow, v, s.m - trow, S.update, keep, lr * s.scale);
-                    } else if (row < s.m && col < s.n) {
-                        write_result(s, base + (int64_t)row * s.cols + col, v, s.n - col, S.update, keep, lr * s.scale);
-                    }
-                }
-            }
+                    for (int b = 0; b < MI; ++b) acc[a][b] = mfma_half(f.q[b][x == 0], f.p[a][x == 1], acc[a][b]);
+        });
+    __syncthreads();
+    finish<MI, FORM>(C, s, part.i, S, acc, &lds[0][0] + wave * 64 * 16, m0 + wm, n0 + wn, part.ti != part.tj);
 }
 
 // -- launches ---------------------------------------------------------------------------------
@@ -395,22 +588,22 @@ int deal(Call &C, Count count) {
     return C.first[C.n];
 }
 
-template <int TILE, int SUB>
-void steps(gsplit_ctx *ctx, Call &C, const Settings &S, hipStream_t st) {
-    const auto launch = [&](const char *name, auto kernel, const Step &step) {
+void steps(gsplit_ctx *ctx, Call &C, const Settings &S, int tile, hipStream_t st) {
+    const auto launch = [&](const char *name, auto large, auto small, const Step &step) {
         GsTimeScope ts(ctx, name, -1, st);
-        hipLaunchKernelGGL(kernel, dim3(C.first[C.n]), dim3(NT), 0, st, C, step);
+        if (tile == NEWTON_TILE) hipLaunchKernelGGL(large, dim3(C.first[C.n]), dim3(NT), 0, st, C, step);
+        else hipLaunchKernelGGL(small, dim3(C.first[C.n]), dim3(NT), 0, st, C, step);
     };
-    const auto lower = [](const NewtonSize &z) { return z.count * newton_tiles_a(z, TILE); };
-    const auto all = [](const NewtonSize &z) { return z.count * newton_tiles_x(z, TILE); };
+    const auto lower = [&](const NewtonSize &z) { return z.count * newton_tiles_a(z, tile); };
+    const auto all = [&](const NewtonSize &z) { return z.count * newton_tiles_x(z, tile); };
     for (int k = 0; k < S.steps; ++k) {
-        const Step step{S.a, S.b, S.c, 2 * (k & 1), S.lr, S.keep, S.decay, S.d_lr, S.update};
+        const Step step{S.a, S.b, S.c, k & 1, S.lr, S.keep, S.decay, S.d_lr, S.update};
         deal(C, lower);
-        launch("newton_a", k_newton<TILE, SUB, FORM_A>, step);
-        launch("newton_b", k_newton<TILE, SUB, FORM_B>, step);
+        launch("newton_a", k_newton_large<FORM_A>, k_newton_small<FORM_A>, step);
+        launch("newton_b", k_newton_large<FORM_B>, k_newton_small<FORM_B>, step);
         deal(C, all);
-        if (k + 1 < S.steps) launch("newton_x", k_newton<TILE, SUB, FORM_X>, step);
-        else launch("newton_last", k_newton<TILE, SUB, FORM_LAST>, step);
+        if (k + 1 < S.steps) launch("newton_x", k_newton_large<FORM_X>, k_newton_small<FORM_X>, step);
+        else launch("newton_last", k_newton_large<FORM_LAST>, k_newton_small<FORM_LAST>, step);
     }
 }
 
@@ -441,8 +634,7 @@ void run_newton(gsplit_ctx *ctx, int64_t n_tensors, const Settings &S, void *wor
             GsTimeScope ts(ctx, "newton_start", -1, st);
             hipLaunchKernelGGL(S.update ? k_newton_start<true> : k_newton_start<false>, dim3(C.first[n]), dim3(NT), 0, st, C, S.mom, S.eps);
         }
-        if (tile == 128) steps<128, 1>(ctx, C, S, st);
-        else steps<64, 2>(ctx, C, S, st);
+        steps(ctx, C, S, tile, st);
     });
 }
 
