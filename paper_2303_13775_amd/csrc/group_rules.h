@@ -23,10 +23,21 @@ inline int64_t group_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // tiles of rows of all groups, at most: every group that has rows leaves one of its tiles short
 inline int64_t group_row_tiles(int64_t n_rows, int n_groups, int rows) { return n_rows / rows + std::min<int64_t>(n_groups, n_rows); }
 
-// -- weight gradients: the rows of a group are taken in chunks where one group's tiles do not fill the chip --
-inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int n_cu) {
-    if (tiles_of_a_group >= n_cu) return std::max<int64_t>(n_rows, 1);
-    const int64_t want = group_ceil(2 * n_cu, tiles_of_a_group);        // chunks of all rows
+// bfloat16 rows of whole granules: tiles of 256 x 256 where they are enough for the chip
+inline bool group_core_rows(int64_t n_rows, int n_groups, int64_t k, int64_t n, int n_cu) {
+    return group_ceil(n_rows, 256) * group_ceil(n, 256) >= n_cu / 2 && k >= 128 && n >= 128 && n_rows >= 64 * (int64_t)n_groups;
+}
+inline bool group_core_weights(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, int n_cu) {
+    return n_in >= 128 && n_out >= 128 && n_rows >= 64 * (int64_t)n_groups && group_ceil(n_in, 256) * group_ceil(n_out, 256) * group_ceil(n_rows, 256) >= n_cu / 2;
+}
+
+// -- weight gradients: tiles of 128 or of 64 --
+inline bool group_weights_large(int64_t n_in, int64_t n_out) { return n_in > 64 && n_out > 64 && n_in * n_out >= 1 << 18; }
+
+// The rows of a group are taken in chunks where one group's tiles do not fill the chip: as many chunks of all rows as give `workgroups`
+inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int64_t workgroups) {
+    const int64_t want = group_ceil(workgroups, tiles_of_a_group);
+    if (want <= 1) return std::max<int64_t>(n_rows, 1);
     return std::max<int64_t>(256, group_ceil(group_ceil(n_rows, want), 64) * 64);
 }
 // slabs: the chunks of those groups that have more than one

@@ -20,6 +20,7 @@ namespace {
 
 #include "gemm_common.h"
 #include "split_parts.h"
+#include "tile_core.h"
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -578,6 +579,8 @@ __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
     }
 }
 
+#include "grouped_core.h"
+
 // -- launches ---------------------------------------------------------------------------------
 
 constexpr int64_t MOST_BLOCKS = 1 << 22;        // (a launch has less than 2^32 threads; workgroups go round)
@@ -589,8 +592,22 @@ void launch_rows(RowsArgs A, hipStream_t st) {
     A.tiles_n = (int32_t)group_ceil(A.N, TL::BN);
     hipLaunchKernelGGL((k_grouped_rows<T, TL, TRANSPOSED>), dim3(blocks(A.tiles_m * A.tiles_n)), dim3(NT), 0, st, A);
 }
+// rows that start at multiples of 16 bytes, and are a whole number of them
+bool in_granules(std::initializer_list<const void *> p, std::initializer_list<int64_t> widths) {
+    for (const void *x : p)
+        if (!aligned16(x)) return false;
+    for (int64_t n : widths)
+        if (n % 8) return false;
+    return true;
+}
 template <bool TRANSPOSED>
-void launch_rows(const gsplit_ctx *ctx, int32_t dtype, const RowsArgs &A, hipStream_t st) {
+void launch_rows(const gsplit_ctx *ctx, int32_t dtype, RowsArgs A, hipStream_t st) {
+    if (dtype == GSPLIT_BF16 && in_granules({A.a, A.w, A.c}, {A.K, A.N, A.lda, A.ldc}) && group_core_rows(A.list.n, A.G, A.K, A.N, ctx->n_cu)) {
+        A.tiles_m = group_row_tiles(A.list.n, A.G, CORE_TILE);
+        A.tiles_n = (int32_t)group_ceil(A.N, CORE_TILE);
+        hipLaunchKernelGGL(k_grouped_rows_core<TRANSPOSED>, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(CT), 0, st, A);
+        return;
+    }
     const bool large = group_row_tiles(A.list.n, A.G, 128) * group_ceil(A.N, 128) >= ctx->n_cu;
     if (dtype == GSPLIT_F32) {
         if (large) launch_rows<float, Tile<128, 128>, TRANSPOSED>(A, st);
@@ -601,11 +618,15 @@ void launch_rows(const gsplit_ctx *ctx, int32_t dtype, const RowsArgs &A, hipStr
     }
 }
 
-bool weights_large(int32_t n_in, int32_t n_out) { return n_in > 64 && n_out > 64 && (int64_t)n_in * n_out >= 1 << 18; }
-int weights_tile(int32_t n_in, int32_t n_out) { return weights_large(n_in, n_out) ? 128 : 64; }
-int64_t weights_chunk(int n_cu, int64_t n_rows, int32_t n_in, int32_t n_out) {
-    const int t = weights_tile(n_in, n_out);
-    return group_chunk(n_rows, group_ceil(n_in, t) * group_ceil(n_out, t), n_cu);
+// How the weight gradients are formed
+struct WeightForm { bool core; int tile; int64_t chunk, slabs; };
+WeightForm weight_form(int n_cu, int64_t n_rows, int32_t n_groups, int32_t n_in, int32_t n_out, bool granules) {
+    WeightForm f;
+    f.core = granules && group_core_weights(n_rows, n_groups, n_in, n_out, n_cu);
+    f.tile = f.core ? CORE_TILE : group_weights_large(n_in, n_out) ? 128 : 64;
+    f.chunk = group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu : 2 * n_cu);
+    f.slabs = group_slabs(n_rows, f.chunk);
+    return f;
 }
 
 }  // namespace
@@ -631,7 +652,10 @@ extern "C" int64_t gsplit_grouped_linear_work(gsplit_ctx *ctx, const gsplit_grou
     if (const char *e = op_check_grouped(c, n_rows)) {
         try { return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_work: ") + e); } catch (...) { return GSPLIT_ENOMEM; }
     }
-    const int64_t slabs = group_slabs(n_rows, weights_chunk(ctx->n_cu, n_rows, c->n_in, c->n_out));
+    // (of the form that needs more: which one it is depends on addresses too)
+    const bool granules = c->dtype == GSPLIT_BF16 && c->n_in % 8 == 0 && c->n_out % 8 == 0;
+    const int64_t slabs = std::max(weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out, granules).slabs,
+                                   weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out, false).slabs);
     return slabs * ((int64_t)c->n_in + 1) * c->n_out * (int64_t)sizeof(float);
 }
 
@@ -644,11 +668,11 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
     return gs_call(ctx, st, [&] {
         const char *e = op_check_grouped_bwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_dy, dy_stride, d_dx, dx_stride, d_dw,
                                              d_dbias, d_work);
-        int64_t chunk = 1, slabs = 0;
+        WeightForm f{};
         if (!e && d_dw) {
-            chunk = weights_chunk(ctx->n_cu, n_rows, c->n_in, c->n_out);
-            slabs = group_slabs(n_rows, chunk);
-            if (slabs && !d_work) e = "NULL d_work";
+            f = weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out,
+                            c->dtype == GSPLIT_BF16 && in_granules({d_x, d_dy, d_dw, d_dbias}, {c->n_in, c->n_out, x_stride, dy_stride}));
+            if (f.slabs && !d_work) e = "NULL d_work";
         }
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_bwd: ") + e);
         const RowList list{d_rows, (int32_t)n_rows};
@@ -658,22 +682,22 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
                                                       c->n_groups, d_group_ptr, list, 0, 0}, st);
         }
         if (d_dw) {
-            const int t = weights_tile(c->n_in, c->n_out);
-            WeightArgs A{d_x, d_dy, (uint32_t)x_stride, (uint32_t)dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)chunk,
-                         n_rows / chunk + c->n_groups, (int32_t)group_ceil(c->n_in, t), (int32_t)group_ceil(c->n_out, t), d_dw, d_dbias,
-                         (float *)d_work, slabs};
+            WeightArgs A{d_x, d_dy, (uint32_t)x_stride, (uint32_t)dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)f.chunk,
+                         n_rows / f.chunk + c->n_groups, (int32_t)group_ceil(c->n_in, f.tile), (int32_t)group_ceil(c->n_out, f.tile), d_dw, d_dbias,
+                         (float *)d_work, f.slabs};
             const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));
             {
                 GsTimeScope ts(ctx, "grouped_dw", -1, st);
-                const auto kernel = c->dtype == GSPLIT_F32 ? t == 128 ? k_grouped_weights<float, Tile<128, 128>> : k_grouped_weights<float, Tile<64, 64>>
-                                                           : t == 128 ? k_grouped_weights<uint16_t, Tile<128, 128>> : k_grouped_weights<uint16_t, Tile<64, 64>>;
-                hipLaunchKernelGGL(kernel, grid, dim3(NT), 0, st, A);
+                const auto kernel = f.core ? k_grouped_weights_core
+                                    : c->dtype == GSPLIT_F32 ? f.tile == 128 ? k_grouped_weights<float, Tile<128, 128>> : k_grouped_weights<float, Tile<64, 64>>
+                                    : f.tile == 128 ? k_grouped_weights<uint16_t, Tile<128, 128>> : k_grouped_weights<uint16_t, Tile<64, 64>>;
+                hipLaunchKernelGGL(kernel, grid, dim3(f.core ? CT : NT), 0, st, A);
             }
-            if (slabs) {
+            if (f.slabs) {
                 GsTimeScope ts(ctx, "grouped_dw_sum", -1, st);
                 const int64_t words = ((int64_t)c->n_in + 1) * c->n_out;
                 hipLaunchKernelGGL(k_grouped_weights_sum, dim3((unsigned)std::min<int64_t>(group_ceil(words, NT), 1024),
-                                                               (unsigned)std::min<int64_t>(c->n_groups, n_rows / chunk)), dim3(NT), 0, st, A);
+                                                               (unsigned)std::min<int64_t>(c->n_groups, n_rows / f.chunk)), dim3(NT), 0, st, A);
             }
         }
         return (int)GSPLIT_OK;

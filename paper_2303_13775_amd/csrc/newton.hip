@@ -476,7 +476,7 @@ __global__ __launch_bounds__(NT, 2) void k_newton_small(Call C, Step S) {
     const int half_ = lane >> 5, l32 = lane & 31, wm = (wave & 1) * 32, wn = (wave >> 1) * 32;
     floatx16 acc[1][1], low = zero16();
     acc[0][0] = zero16();
-    const int T = F.k / (32 * SUB);
+    const int T = F.k / (32 * SUB), base_q = across_base<16>(HALF, wn / 4);
     fetch(0, lds[0]);
     for (int t = 0; t < T; ++t) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(NT, 2) void k_newton_small(Call C, Step S) {
                 for (int q = 0; q < 2; ++q) {
                     const int g = 4 * q + 2 * h + half_;
                     fp[u][h][q] = __builtin_bit_cast(halfx8, now[u * TILE * 8 + along_at(wm + l32, g)]);
-                    if constexpr (ACROSS) fq[u][h][q] = __builtin_bit_cast(halfx8, across_fragment<16>(now + HALF, 2 * u + h, wn / 4 + 4 * q));
+                    if constexpr (ACROSS) fq[u][h][q] = __builtin_bit_cast(halfx8, across_fragment<16>(now, base_q, 2 * u + h, 4 * q));
                     else fq[u][h][q] = __builtin_bit_cast(halfx8, now[HALF + u * TILE * 8 + along_at(wn + l32, g)]);
                 }
         if (t + 1 < T) fetch(t + 1, lds[(t + 1) & 1]);
@@ -543,17 +543,18 @@ __global__ __launch_bounds__(NT, 2) void k_newton_large(Call C, Step S) {
 #pragma unroll
         for (int b = 0; b < MI; ++b) acc[a][b] = zero16();
     struct Frag { halfx8 p[MI][2], q[MI][2]; };
+    const int base_p = along_base(0, wm), base_q = ACROSS ? across_base<32>(HALF, wn / 4) : along_base(HALF, wn);
     core_contract<2, Frag>(F.k / 32, lds, fetch,
         [&](Frag &f, const core_u32x4 *now, int h) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int g = 4 * q + 2 * h + half_;
+                // (the lo of a row's 32 columns: four granules behind the hi)
 #pragma unroll
-                for (int a = 0; a < MI; ++a) f.p[a][q] = __builtin_bit_cast(halfx8, now[along_at(wm + 32 * a + l32, g)]);
+                for (int a = 0; a < MI; ++a) f.p[a][q] = __builtin_bit_cast(halfx8, along_fragment(now, base_p, 2 * q + h, a));
 #pragma unroll
                 for (int b = 0; b < MI; ++b) {
-                    if constexpr (ACROSS) f.q[b][q] = __builtin_bit_cast(halfx8, across_fragment<32>(now + HALF, h, wn / 4 + 8 * b + 4 * q));
-                    else f.q[b][q] = __builtin_bit_cast(halfx8, now[HALF + along_at(wn + 32 * b + l32, g)]);
+                    if constexpr (ACROSS) f.q[b][q] = __builtin_bit_cast(halfx8, across_fragment<32>(now, base_q, h, 8 * b + 4 * q));
+                    else f.q[b][q] = __builtin_bit_cast(halfx8, along_fragment(now, base_q, 2 * q + h, b));
                 }
             }
         },

@@ -154,6 +154,25 @@ def test_large_products(ctx, rows, groups, n_in, n_out, kw, dtype):
     _case(ctx, rows, groups, n_in, n_out, dtype, **kw)
 
 
+# bfloat16 rows of whole granules, enough for the large tiles: edges of the rows, of the contraction, of the columns; groups of a few rows
+@pytest.mark.parametrize("rows, groups, n_in, n_out, kw", [
+    (17_000, 5, 264, 520, dict(skew=1.0, left_out=0.1, pad=8, offset=8)), (33_000, 1, 128, 1000, dict(listed=False)), (20_000, 300, 512, 256, dict(skew=2.0)),
+    (35_000, 40, 136, 1288, dict(skew=1.0, pad=16, bias=False)), (16_500, 2, 1000, 504, dict(empty=(0,))), (40_000, 7, 392, 128, dict(left_out=0.5))])
+def test_large_tiles(ctx, rows, groups, n_in, n_out, kw):
+    _case(ctx, rows, groups, n_in, n_out, BF16, **kw)
+
+
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+def test_large_tiles_keep_values_that_are_not_finite_where_they_belong(ctx, bad):
+    rows, n_in, n_out = 17_000, 264, 520
+
+    def values(x, w, dy):
+        x[3, 1], x[rows - 1, n_in - 1] = bad, bad
+        w[1, n_in - 1, n_out - 2], w[0, 0, 0] = bad, bad
+        dy[rows - 2, 5], dy[4, n_out - 1] = bad, bad
+    _case(ctx, rows, 3, n_in, n_out, BF16, values=values)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_groups_without_rows_and_no_rows_at_all(ctx, dtype):
     _case(ctx, 50, 6, 40, 24, dtype, empty=(0, 2, 3, 5))
