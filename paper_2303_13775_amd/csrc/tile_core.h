@@ -14,9 +14,12 @@ typedef short core_s16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int core_wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// 64 lanes fetch 16 bytes each into 1 KB of LDS side by side
+// 64 lanes fetch 16 bytes each into 1 KB of LDS side by side.  (Not the compiler's built-in function: it has every transposed read of
+// LDS wait for all fetches on their way, whatever place they write, which left none of them in flight behind the matrix instructions.
+// Nothing here waits for a fetch but core_landed.)
 __device__ __forceinline__ void core_fetch(const void *from, core_u32x4 *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
 }
 
 // Operand rows of 128 bytes a stage, eight granules of 16 each.  Granule p of row r of LDS holds granule p ^ (r / 2) % 8: sixteen rows of
@@ -54,6 +57,7 @@ __device__ __forceinline__ core_u32x4 across_fragment(const core_u32x4 *lds, int
 }
 
 // STEPS steps a stage.  fetch(t, lds): stage t of both operands into lds; Frag read(lds, s); multiply(frag).
+// Waits until this wave's fetches have landed, and for the other waves' to have.
 __device__ __forceinline__ void core_landed() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
