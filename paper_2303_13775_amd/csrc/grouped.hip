@@ -296,41 +296,56 @@ struct Sums {
     }
 };
 
-// Which rows a tile takes: its group, the place of its first row among the sorted ones, how many.  Tiles are numbered group by
-// group; every wave works it out for itself, 64 groups at a time.  Offsets that make no sense are held inside 0 .. n_rows.
-struct Spot { int g, first, rows, chunk, chunks, slab; };
+// Which rows a tile takes: its group, the place of its first row among the sorted ones, how many.  Tiles of rows are numbered group by
+// group, `across` of them side by side; every wave works it out for itself, 64 groups at a time.  Offsets that make no sense are held
+// inside 0 .. n_rows.
+struct Spot { int g, first, rows, chunks, slab, side; };
 template <bool EMPTY_TOO>
-__device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G, int n_rows, int per, int j, Spot &s) {
+__device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G, int n_rows, int per, int64_t block, int64_t across, Spot &s) {
     const int lane = threadIdx.x & 63;
-    int slab = 0;
-    for (int base = 0; base < G; base += 64) {
+    int lo, hi, tiles, sum, own_slabs, slabs;
+    const auto scan = [&](int base) __attribute__((always_inline)) {
         const int g = base + lane;
-        const int lo = min(max(ptr[min(g, G)], 0), n_rows), hi = min(max(ptr[min(g + 1, G)], lo), n_rows);
-        int tiles = (int)(((int64_t)(hi - lo) + per - 1) / per);
+        lo = min(max(ptr[min(g, G)], 0), n_rows); hi = min(max(ptr[min(g + 1, G)], lo), n_rows);
+        tiles = (int)(((int64_t)(hi - lo) + per - 1) / per);
         if (EMPTY_TOO) tiles = max(tiles, 1);
         if (g >= G) tiles = 0;
-        int sum = tiles, slabs = tiles > 1 ? tiles : 0;
-        const int own_slabs = slabs;
+        sum = tiles;
+        slabs = own_slabs = tiles > 1 ? tiles : 0;
         for (int o = 1; o < 64; o <<= 1) {
-            const int up = __shfl_up(sum, o), up2 = __shfl_up(slabs, o);
+            const int up = __shfl_up(sum, o), up2 = EMPTY_TOO ? __shfl_up(slabs, o) : 0;
             if (lane >= o) { sum += up; slabs += up2; }
         }
-        const int all = __builtin_amdgcn_readlane(sum, 63);
-        if (j < all) {
+    };
+    int all = 0;
+    for (int base = (G - 1) / 64 * 64; base >= 0; base -= 64) {         // (the first groups last: they are what the search begins with)
+        scan(base);
+        all += __builtin_amdgcn_readlane(sum, 63);
+    }
+    // Workgroups are dealt round-robin to the eight XCDs: consecutive tiles (the same rows, the same matrix) go to one of them, for its
+    // L2, an eighth of the tiles there are each (not of those there may be, or the last XCDs have less to do)
+    const int64_t total = all * across, each = (total + 7) / 8, x = (block & 7) * each + (block >> 3);
+    if (block >> 3 >= each || x >= total) return false;
+    int j = (int)(x / across), slab = 0;
+    s.side = (int)(x - j * across);
+    for (int base = 0;;) {
+        const int n = __builtin_amdgcn_readlane(sum, 63);
+        if (j < n) {
             const int l = __builtin_ctzll(__ballot(sum > j));
             const int c = j - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(tiles, l));
             s.g = base + l;
-            s.chunk = c;
             s.chunks = __builtin_amdgcn_readlane(tiles, l);
             s.first = __builtin_amdgcn_readlane(lo, l) + c * per;
             s.rows = min(per, __builtin_amdgcn_readlane(hi, l) - s.first);
             s.slab = slab + __builtin_amdgcn_readlane(slabs, l) - __builtin_amdgcn_readlane(own_slabs, l) + c;
             return true;
         }
-        j -= all;
+        j -= n;
         slab += __builtin_amdgcn_readlane(slabs, 63);
+        base += 64;
+        if (base >= G) return false;
+        scan(base);
     }
-    return false;
 }
 
 // The list of rows; a number outside the rows reads row 0 and is not written
@@ -345,13 +360,6 @@ struct RowList {
 
 // where row r of a matrix starts: one multiplication (strides are below 2^31)
 __device__ __forceinline__ uint64_t row_at(int r, uint32_t ld) { return (uint64_t)(uint32_t)r * ld; }
-
-// Which tile a workgroup takes: workgroups are dealt round-robin to the eight XCDs, and consecutive tiles (the same rows, the same
-// matrix) belong into the L2 of one
-__device__ __forceinline__ int64_t tile_number(int64_t block, int64_t total) {
-    const int64_t per = (total + 7) / 8;
-    return (block & 7) * per + (block >> 3);
-}
 
 struct RowsArgs {
     const void *a, *w;
@@ -387,12 +395,11 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
     __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
     __shared__ int s_row[BM];
     __shared__ __attribute__((aligned(16))) float s_bias[BN];
-    const int64_t total = A.tiles_m * A.tiles_n, room = (total + 7) / 8 * 8;
+    const int64_t room = (A.tiles_m * A.tiles_n + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
-        const int64_t x = tile_number(block, total);
         Spot s;
-        if (x >= total || !find_spot<false>(A.ptr, A.G, A.list.n, BM, (int)(x / A.tiles_n), s)) continue;
-        const int n0 = (int)(x % A.tiles_n) * BN;
+        if (!find_spot<false>(A.ptr, A.G, A.list.n, BM, block, A.tiles_n, s)) continue;
+        const int n0 = s.side * BN;
         if (threadIdx.x < BM) s_row[threadIdx.x] = (int)threadIdx.x < s.rows ? A.list.at(s.first + threadIdx.x) : -1;
         if (threadIdx.x < BN) s_bias[threadIdx.x] = A.bias && n0 + (int)threadIdx.x < A.N ? A.bias[(int64_t)s.g * A.N + n0 + threadIdx.x] : 0.f;
         if (!TRANSPOSED && n0 + BN > A.N) clear_rows<T, BN>(s_b);
@@ -461,14 +468,13 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
     constexpr int BM = TL::BM, BN = TL::BN, KG = Kind<T>::KG, P = Kind<T>::PLANES;
     __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
     __shared__ double s_sum[KG][BN];
-    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, total = A.items * tiles, room = (total + 7) / 8 * 8;
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
-        const int64_t x = tile_number(block, total);
         Spot s;
-        if (x >= total || !find_spot<true>(A.ptr, A.G, A.list.n, A.per, (int)(x / tiles), s)) continue;
+        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
         const bool whole = s.chunks == 1;
         if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
-        const int m0 = (int)(x % tiles / A.tiles_n) * BM, n0 = (int)(x % A.tiles_n) * BN;
+        const int m0 = s.side / A.tiles_n * BM, n0 = s.side % A.tiles_n * BN;
         const T *xs = (const T *)A.x, *dys = (const T *)A.dy;
         const auto x_row = [&](int k) { return xs + row_at(max(A.list.at(s.first + k), 0), A.ldx); };
         const auto dy_row = [&](int k) { return dys + row_at(max(A.list.at(s.first + k), 0), A.lddy); };

@@ -42,12 +42,11 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     __shared__ int s_row[T];
     __shared__ __attribute__((aligned(16))) float s_bias[T];
     const int lane = threadIdx.x & 63, wave = core_wave(), half = lane >> 5, l32 = lane & 31, wm = core_wm(), wn = core_wn();
-    const int64_t total = A.tiles_m * A.tiles_n, room = (total + 7) / 8 * 8;
+    const int64_t room = (A.tiles_m * A.tiles_n + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
-        const int64_t x = tile_number(block, total);
         Spot s;
-        if (x >= total || !find_spot<false>(A.ptr, A.G, A.list.n, T, (int)(x / A.tiles_n), s)) continue;
-        const int n0 = (int)(x % A.tiles_n) * T;
+        if (!find_spot<false>(A.ptr, A.G, A.list.n, T, block, A.tiles_n, s)) continue;
+        const int n0 = s.side * T;
         if (threadIdx.x < T) {
             const int t = threadIdx.x;
             s_row[t] = t < s.rows ? A.list.at(s.first + t) : -1;
@@ -148,14 +147,13 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     constexpr int T = CORE_TILE;
     __shared__ __attribute__((aligned(16))) core_u32x4 lds[2][2 * CORE_HALF];
     const int lane = threadIdx.x & 63, wave = core_wave(), half = lane >> 5, l32 = lane & 31, wm = core_wm(), wn = core_wn();
-    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, total = A.items * tiles, room = (total + 7) / 8 * 8;
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
-        const int64_t x = tile_number(block, total);
         Spot s;
-        if (x >= total || !find_spot<true>(A.ptr, A.G, A.list.n, A.per, (int)(x / tiles), s)) continue;
+        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
         const bool whole = s.chunks == 1;
         if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
-        const int m0 = (int)(x % tiles / A.tiles_n) * T, n0 = (int)(x % A.tiles_n) * T;
+        const int m0 = s.side / A.tiles_n * T, n0 = s.side % A.tiles_n * T;
         // a lane holds the number of a row of the next stage
         int next = 0;
         const auto look_up = [&](int t) __attribute__((always_inline)) {
