@@ -570,6 +570,211 @@ __global__ __launch_bounds__(NT, 2) void k_newton_large(Call C, Step S) {
     finish<MI, FORM>(C, s, part.i, S, acc, &lds[0][0] + wave * 64 * 16, m0 + wm, n0 + wn, part.ti != part.tj);
 }
 
+// -- small matrices: all steps of one by one workgroup --------------------------------------------
+
+// Sixteen waves form a block of 16 x 16 of A and of B each, and up to ONE_BLOCKS of X; what bounds this is the way through LDS and the
+// barriers, some 0.3 us a product.
+// The matrices lie in LDS, rows of granules: 32 columns are 4 granules of hi and 4 of lo.  Granule p of row r holds granule
+// p ^ (4 (r % 4) + r / 4 % 4): sixteen rows of one granule column lie in sixteen groups of banks, and so do the four rows of four
+// granules that are read transposed.
+constexpr int ONE_ROWS = 64, ONE_NT = 1024, ONE_BLOCKS = NEWTON_ONE_N / 64;
+__device__ __forceinline__ int one_turn(int r) { return 4 * (r & 3) + (r >> 2 & 3); }
+typedef float floatx4m __attribute__((ext_vector_type(4)));
+// 16 rows of p from m0 on times 16 columns from n0 on: rows of q, or columns (ACROSS).  A lane gets four columns of one row.
+template <bool ACROSS>
+__device__ __forceinline__ floatx4m one_block(const core_u32x4 *p, const core_u32x4 *q, int row_p, int row_q, int m0, int n0, int k) {
+    const int lane = threadIdx.x & 63, quarter = lane >> 4, rp = m0 + (lane & 15), rq = n0 + (lane & 15);
+    floatx4m acc{0.f, 0.f, 0.f, 0.f}, low = acc;
+#pragma unroll 2
+    for (int h = 0; h < k / 32; ++h) {          // 32 columns of p: four granules of hi, four of lo
+        halfx8 fp[2], fq[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int g = h * 8 + 4 * x + quarter;
+            fp[x] = __builtin_bit_cast(halfx8, p[rp * row_p + (g ^ one_turn(rp))]);
+            if constexpr (ACROSS) {
+                // eight rows of 16 columns, one a lane (see across_fragment)
+                const int r = 32 * h + 8 * quarter + ((lane & 15) >> 2), c = n0 / 32 * 8 + n0 / 16 % 2 * 2 + 4 * x + (lane >> 1 & 1);
+                typedef __attribute__((address_space(3))) core_s16x4 *P;
+                const auto at = [&](int row) { return (P)((__attribute__((address_space(3))) const core_u32x2 *)q + 2 * (row * row_q + (c ^ one_turn(row))) + (lane & 1)); };
+                const core_u32x2 a = __builtin_bit_cast(core_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r)));
+                const core_u32x2 b = __builtin_bit_cast(core_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(r + 4)));
+                fq[x] = __builtin_bit_cast(halfx8, core_u32x4{a[0], a[1], b[0], b[1]});
+            } else {
+                fq[x] = __builtin_bit_cast(halfx8, q[rq * row_q + (g ^ one_turn(rq))]);
+            }
+        }
+        low = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[1], fp[1], low, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[0], fp[0], acc, 0, 0, 0);
+        low = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[1], fp[0], low, 0, 0, 0);
+        low = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[0], fp[1], low, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += low[j];
+    return acc;
+}
+__device__ __forceinline__ halfx4 *one_pair(core_u32x4 *m, int row, int r, int c, int lo) {
+    return (halfx4 *)(m + r * row + ((c / 32 * 8 + lo * 4 + c % 32 / 8) ^ one_turn(r))) + (c / 4 & 1);
+}
+
+// A matrix of at most 64 x NEWTON_ONE_N (or its transpose): momentum, norm, steps and result; as above otherwise
+template <bool MOMENTUM>
+__global__ __launch_bounds__(ONE_NT) void k_newton_one(Call C, Momentum M, double eps, Step S, int steps) {
+    extern __shared__ __attribute__((aligned(16))) core_u32x4 one_lds[];          // X [64 x np], A and B [64 x 64]
+    __shared__ double s_sum[ONE_NT / 64];
+    const int k = stack_of(C, blockIdx.x);
+    const Stack &s = C.s[k];
+    const int i = blockIdx.x - C.first[k], lane = threadIdx.x & 63, wave = core_wave();
+    const int row_x = s.np / 4, row_a = ONE_ROWS / 4;
+    core_u32x4 *const X = one_lds, *const A = X + ONE_ROWS * row_x, *const B = A + ONE_ROWS * row_a;
+    const int64_t base = (int64_t)i * s.rows * s.cols;
+    // four of the matrix' own columns a thread
+    const int quads = (s.cols + 3) / 4, items = s.rows * quads;
+    const auto load = [&](int x, bool update, int &r, int &c, float (&u)[4]) __attribute__((always_inline)) {
+        r = x / quads; c = x % quads * 4;
+        const int n = min(4, s.cols - c);
+        const int64_t at = base + (int64_t)r * s.cols + c;
+        float m[4] = {};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) u[q] = 0.f;
+        if (n == 4) {
+            load4(s, at, u);
+            if (MOMENTUM) {
+                floatx4 f = *(const floatx4_any *)(s.mom + at);
+                if (update) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) f[q] = M.keep * f[q] + M.take * u[q];
+                    *(floatx4_any *)(s.mom + at) = f;
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) m[q] = f[q];
+            }
+        } else {
+            for (int q = 0; q < n; ++q) {
+                u[q] = value(s.g, at + q, s.half_g);
+                if (MOMENTUM) {
+                    m[q] = s.mom[at + q];
+                    if (update) s.mom[at + q] = m[q] = M.keep * m[q] + M.take * u[q];
+                }
+            }
+        }
+        if (MOMENTUM)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) u[q] = mixed(M, m[q], u[q]);
+    };
+    constexpr int KEPT = 4;             // items that a thread keeps; more are read again
+    float kept[KEPT][4];
+    double sum = 0.0;
+    const auto add = [&](const float (&u)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum = fma((double)u[q], (double)u[q], sum);
+    };
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j) {
+        int r, c;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) kept[j][q] = 0.f;
+        if (j * ONE_NT + (int)threadIdx.x < items) load(j * ONE_NT + threadIdx.x, true, r, c, kept[j]);
+        add(kept[j]);
+    }
+    for (int x = KEPT * ONE_NT + threadIdx.x; x < items; x += ONE_NT) {
+        int r, c;
+        float u[4];
+        load(x, true, r, c, u);
+        add(u);
+    }
+    for (int x = threadIdx.x; x < ONE_ROWS * row_x; x += ONE_NT) X[x] = core_u32x4{0u, 0u, 0u, 0u};
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    sum = s_sum[0];
+    for (int w = 1; w < ONE_NT / 64; ++w) sum += s_sum[w];
+    const double norm = sqrt(sum) + eps;
+    const double factor = norm < INFINITY ? norm > 0.0 ? (double)SCALE_X / norm : 0.0 : NAN;
+    const auto place_x = [&](int r, int c, const float (&u)[4]) __attribute__((always_inline)) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)(u[q] * factor);
+        if (!s.tall) {
+            halfx4 hi, lo;
+            split4(v, hi, lo);
+            *one_pair(X, row_x, r, c, 0) = hi;
+            *one_pair(X, row_x, r, c, 1) = lo;
+        } else {                        // the transpose: a value by itself
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (c + q >= s.cols) continue;
+                const half hi = (half)v[q];
+                ((half *)one_pair(X, row_x, c + q, r & ~3, 0))[r & 3] = hi;
+                ((half *)one_pair(X, row_x, c + q, r & ~3, 1))[r & 3] = (half)(v[q] - (float)hi);
+            }
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < KEPT; ++j) {
+        const int x = j * ONE_NT + threadIdx.x;
+        if (x < items) place_x(x / quads, x % quads * 4, kept[j]);
+    }
+    for (int x = KEPT * ONE_NT + threadIdx.x; x < items; x += ONE_NT) {
+        int r, c;
+        float u[4];
+        load(x, false, r, c, u);
+        place_x(r, c, u);
+    }
+    __syncthreads();
+    float keep = 0.f, lr = 0.f;
+    rates(S, keep, lr);
+    const int m0 = (wave & 3) * 16, n0 = (wave >> 2) * 16, r = lane & 15, c = 4 * (lane >> 4);
+    const auto put = [&](core_u32x4 *m, int row, int r, int c, const float (&v)[4]) __attribute__((always_inline)) {
+        halfx4 hi, lo;
+        split4(v, hi, lo);
+        *one_pair(m, row, r, c, 0) = hi;
+        *one_pair(m, row, r, c, 1) = lo;
+    };
+    for (int step = 0; step < steps; ++step) {
+        floatx4m acc = one_block<false>(X, X, row_x, row_x, m0, n0, s.np);
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = acc[j] * (SCALE_A / (SCALE_X * SCALE_X));
+        put(A, row_a, m0 + r, n0 + c, v);
+        __syncthreads();
+        acc = one_block<false>(A, A, row_a, row_a, m0, n0, ONE_ROWS);
+        const halfx4 hi = *one_pair(A, row_a, m0 + r, n0 + c, 0), lo = *one_pair(A, row_a, m0 + r, n0 + c, 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[j] = S.c * (SCALE_B / (SCALE_A * SCALE_A)) * acc[j] + S.b * (SCALE_B / SCALE_A) * ((float)hi[j] + (float)lo[j])
+                   + (m0 + r == n0 + c + j ? S.a * SCALE_B : 0.f);
+        put(B, row_a, m0 + r, n0 + c, v);
+        __syncthreads();
+        // columns n0, n0 + 64 .. of X, which stay in registers until all waves have read theirs
+        floatx4m next[ONE_BLOCKS];
+#pragma unroll
+        for (int b = 0; b < ONE_BLOCKS; ++b)
+            if (64 * b < s.np) next[b] = one_block<true>(B, X, row_a, row_x, m0, n0 + 64 * b, ONE_ROWS);
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < ONE_BLOCKS; ++b) {
+            if (64 * b >= s.np) break;
+            int row = m0 + r, col = n0 + 64 * b + c;
+            if (step + 1 < steps) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = next[b][j] * (1.f / SCALE_B);
+                put(X, row_x, row, col, v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = next[b][j] * (1.f / (SCALE_B * SCALE_X));
+                if (s.tall) {
+                    transpose4(v);
+                    const int t = row & ~3;
+                    row = col + (lane & 3); col = t;
+                }
+                if (row < s.rows && col < s.cols) write_result(s, base + (int64_t)row * s.cols + col, v, s.cols - col, S.update, keep, lr * s.scale);
+            }
+        }
+        __syncthreads();
+    }
+}
+
 // -- launches ---------------------------------------------------------------------------------
 
 struct Settings {
@@ -623,7 +828,17 @@ void run_newton(gsplit_ctx *ctx, int64_t n_tensors, const Settings &S, void *wor
             s.count = (int32_t)z.count; s.rows = z.rows; s.cols = z.cols; s.m = z.m; s.n = z.n; s.mp = z.mp; s.np = z.np;
             s.tall = z.rows > z.cols;
             fill(s, in[k].tensor, in[k].first * z.rows * z.cols);
-            at += newton_words(z);
+            at += newton_words(z, tile);
+        }
+        if (tile == NEWTON_ONE) {
+            int np = 0;
+            for (int k = 0; k < n; ++k) np = std::max(np, C.s[k].np);
+            deal(C, [](const NewtonSize &z) { return z.count; });
+            const Step step{S.a, S.b, S.c, 0, S.lr, S.keep, S.decay, S.d_lr, S.update};
+            GsTimeScope ts(ctx, "newton_one", -1, st);
+            hipLaunchKernelGGL(S.update ? k_newton_one<true> : k_newton_one<false>, dim3(C.first[n]), dim3(ONE_NT), (np + 2 * 64) * 64 * 4, st, C, S.mom,
+                               S.eps, step, S.steps);
+            return;
         }
         deal(C, [](const NewtonSize &z) { return z.count * newton_slots(z); });
         {
@@ -645,9 +860,9 @@ template <class Tensor> Shape shape_of(const Tensor &t) { return {t.count, t.row
 template <class Tensor>
 int64_t work_bytes(const Tensor *t, int64_t n_tensors) {
     int64_t most = 0;
-    newton_groups(n_tensors, [&](int64_t i) { return shape_of(t[i]); }, [&](const NewtonStack *in, int n, int) {
+    newton_groups(n_tensors, [&](int64_t i) { return shape_of(t[i]); }, [&](const NewtonStack *in, int n, int tile) {
         int64_t words = 0;
-        for (int k = 0; k < n; ++k) words += newton_words(in[k].size);
+        for (int k = 0; k < n; ++k) words += newton_words(in[k].size, tile);
         most = std::max(most, words);
     });
     return most * 16;

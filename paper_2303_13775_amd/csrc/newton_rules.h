@@ -6,6 +6,8 @@
 #include <cstdint>
 
 constexpr int NEWTON_TILE = 128;                // the large tile; the small one is 64
+constexpr int NEWTON_ONE = 1;                   // (not a tile:) the kernel that takes a matrix in LDS, at most 64 x NEWTON_ONE_N, padded to 64
+constexpr int64_t NEWTON_ONE_N = 384;
 constexpr int NEWTON_STACKS = 24;               // of a launch: they travel in its arguments
 constexpr int64_t NEWTON_CHUNK = 16384;         // elements whose squares a workgroup adds up
 
@@ -18,13 +20,15 @@ struct NewtonSize {
 inline int32_t newton_pad(int64_t x, int tile) { return (int32_t)((x + tile - 1) / tile * tile); }
 inline NewtonSize newton_size(int64_t count, int32_t rows, int32_t cols, int tile) {
     const int32_t m = std::min(rows, cols), n = std::max(rows, cols);
-    return {count, rows, cols, m, n, newton_pad(m, tile), newton_pad(n, tile)};
+    const int pad = tile == NEWTON_ONE ? 64 : tile;
+    return {count, rows, cols, m, n, newton_pad(m, pad), newton_pad(n, pad)};
 }
 // 16-byte words of the working memory: X, twice; A and B; the sums of squares.  A value is two halves.
 inline int64_t newton_words_x(const NewtonSize &s) { return (int64_t)s.mp * s.np / 4; }         // of one X
 inline int64_t newton_words_a(const NewtonSize &s) { return (int64_t)s.mp * s.mp / 4; }         // of one A
 inline int64_t newton_slots(const NewtonSize &s) { return ((int64_t)s.rows * s.cols + NEWTON_CHUNK - 1) / NEWTON_CHUNK; }
-inline int64_t newton_words(const NewtonSize &s) {
+inline int64_t newton_words(const NewtonSize &s, int tile) {
+    if (tile == NEWTON_ONE) return 0;
     return s.count * (2 * newton_words_x(s) + 2 * newton_words_a(s) + (newton_slots(s) + 1) / 2);
 }
 // tiles of X, of the lower triangle of A
@@ -36,28 +40,38 @@ inline bool newton_large(int64_t tiles_of_a) { return tiles_of_a >= 256; }
 // A launch takes stacks up to this many padded elements, so that working memory stays in proportion
 constexpr int64_t NEWTON_LAUNCH = 1 << 27;
 
-// Deals the stacks to launches: group(stacks, n) for each.  size(i): (count, rows, cols) of stack i
+// Matrices that one workgroup each takes through all steps (one launch).  By itself a small matrix is done sooner that way; in front of
+// launches for larger ones few of them would only add theirs.
+inline bool newton_one(int64_t rows, int64_t cols) { return std::min(rows, cols) <= 64 && std::max(rows, cols) <= NEWTON_ONE_N; }
+inline bool newton_ones(int64_t small, int64_t others) { return others == 0 || small >= 256; }
+
+// Deals the stacks to launches: group(stacks, n, tile) for each.  size(i): (count, rows, cols) of stack i
 struct NewtonStack { int64_t tensor, first; NewtonSize size; };         // matrices first .. first + size.count - 1 of a tensor
 template <class Size, class Group>
 void newton_groups(int64_t n_tensors, Size size, Group group) {
-    int64_t tiles = 0;
+    int64_t tiles = 0, small = 0, others = 0;
     for (int64_t i = 0; i < n_tensors; ++i) {
         const auto s = size(i);
-        if (std::min(s.rows, s.cols) > 64) tiles += s.count * newton_tiles_a(newton_size(s.count, s.rows, s.cols, NEWTON_TILE), NEWTON_TILE);
+        if (s.count == 0 || s.rows == 0 || s.cols == 0) continue;
+        if (std::min(s.rows, s.cols) > 64) {
+            const int64_t t = newton_pad(std::min(s.rows, s.cols), 128) / 128;
+            tiles += s.count * (t * (t + 1) / 2);
+        }
+        (newton_one(s.rows, s.cols) ? small : others) += s.count;
     }
-    const bool large = newton_large(tiles);
-    for (int pass = 0; pass < 2; ++pass) {              // those of the large tile, then the others
-        const int tile = pass == 0 ? NEWTON_TILE : 64;
-        if (pass == 0 && !large) continue;
+    const bool large = newton_large(tiles), ones = newton_ones(small, others);
+    const auto tile_of = [&](int32_t rows, int32_t cols) {
+        return ones && newton_one(rows, cols) ? NEWTON_ONE : large && std::min(rows, cols) > 64 ? NEWTON_TILE : 64;
+    };
+    for (const int tile : {NEWTON_TILE, 64, NEWTON_ONE}) {
         NewtonStack in[NEWTON_STACKS];
         int n = 0;
         int64_t room = NEWTON_LAUNCH;
         for (int64_t i = 0; i < n_tensors; ++i) {
             const auto s = size(i);
-            if ((large && std::min(s.rows, s.cols) > 64) != (tile == NEWTON_TILE)) continue;
+            if (s.rows == 0 || s.cols == 0 || tile_of(s.rows, s.cols) != tile) continue;
             for (int64_t first = 0; first < s.count;) {
                 NewtonSize one = newton_size(1, s.rows, s.cols, tile);
-                if (one.m == 0) break;
                 const int64_t each = (int64_t)one.mp * one.np;
                 int64_t take = std::min<int64_t>(s.count - first, room / each);
                 if (n == NEWTON_STACKS || (take == 0 && n > 0)) {

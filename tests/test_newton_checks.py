@@ -31,7 +31,7 @@ extern "C" int64_t groups(const gsplit_matrix_tensor *t, int64_t n, int64_t *out
                   [&](const NewtonStack *in, int k, int tile) {
         for (int j = 0; j < k; ++j, ++at)
             if (at < room) {
-                const int64_t row[8] = {launch, tile, in[j].tensor, in[j].first, in[j].size.count, in[j].size.mp, in[j].size.np, newton_words(in[j].size)};
+                const int64_t row[8] = {launch, tile, in[j].tensor, in[j].first, in[j].size.count, in[j].size.mp, in[j].size.np, newton_words(in[j].size, tile)};
                 for (int x = 0; x < 8; ++x) out[8 * at + x] = row[x];
             }
         ++launch;
@@ -154,8 +154,9 @@ def test_every_matrix_is_in_one_launch():
             c, r, q = shapes[i]
             tiles.add(tile)
             m, w = min(r, q), max(r, q)
-            assert count >= 1 and mp % tile == 0 and np_ % tile == 0 and m <= mp < m + tile and w <= np_ < w + tile
-            assert words >= count * (mp * np_ // 2 + mp * mp // 2 + -(-r * q // 16384) // 2)
+            pad = 64 if tile == 1 else tile
+            assert count >= 1 and mp % pad == 0 and np_ % pad == 0 and m <= mp < m + pad and w <= np_ < w + pad
+            assert (words == 0 and m <= 64 and w <= 384) if tile == 1 else words >= count * (mp * np_ // 2 + mp * mp // 2 + -(-r * q // 16384) // 2)
             covered[i] += range(first, first + count)
         for i, (c, r, q) in enumerate(shapes):
             assert covered[i] == (list(range(c)) if r and q else [])
@@ -164,4 +165,4 @@ def test_every_matrix_is_in_one_launch():
             assert 1 <= len(own) <= 24 and len(set(own[:, 1])) == 1
             assert (own[:, 4] * own[:, 5] * own[:, 6]).sum() <= 1 << 27 or (len(own) == 1 and own[0, 4] == 1)
         assert B.load_library().gsplit_orthogonalize_work(t, len(shapes)) == 16 * max([0] + [int(rows[rows[:, 0] == l, 7].sum()) for l in set(rows[:, 0])])
-    assert tiles == {64, 128}
+    assert tiles == {1, 64, 128}
