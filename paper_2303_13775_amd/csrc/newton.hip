@@ -65,10 +65,10 @@ struct Call {
 };
 static_assert(sizeof(Call) <= 4096 - 256, "kernel arguments");
 
-__device__ __forceinline__ int stack_of(const Call &C, int block) {
-    int k = 0;
-    while (k + 1 < C.n && C.first[k + 1] <= block) ++k;
-    return k;
+__device__ __forceinline__ int stack_of(const Call &C, int block) {      // (a lane a stack: a loop would wait for each)
+    const int lane = threadIdx.x & 63;
+    const bool before = lane + 1 < C.n && C.first[min(lane + 1, NEWTON_STACKS)] <= block;
+    return __builtin_amdgcn_readfirstlane((int)__popcll(__ballot(before)));
 }
 
 // -- the matrix to be orthogonalised ------------------------------------------------------------
@@ -83,9 +83,11 @@ __device__ __forceinline__ float value(const void *p, int64_t i, bool half_type)
 __device__ __forceinline__ void load4(const Stack &s, int64_t at, float (&g)[4]) {
     if (s.half_g) {
         const bf16x4 q = *(const bf16x4_any *)((const bf16 *)s.g + at);
+#pragma unroll
         for (int k = 0; k < 4; ++k) g[k] = (float)q[k];
     } else {
         const floatx4 q = *(const floatx4_any *)((const float *)s.g + at);
+#pragma unroll
         for (int k = 0; k < 4; ++k) g[k] = q[k];
     }
 }
@@ -94,30 +96,47 @@ __device__ __forceinline__ void load4(const Stack &s, int64_t at, float (&g)[4])
 template <bool MOMENTUM>
 __global__ __launch_bounds__(NT) void k_newton_sums(Call C, Momentum M) {
     __shared__ double s_sum[NT / 64];
-    const Stack &s = C.s[stack_of(C, blockIdx.x)];
-    const int64_t size = (int64_t)s.rows * s.cols, slots = (size + NEWTON_CHUNK - 1) / NEWTON_CHUNK;
-    const int64_t item = blockIdx.x - C.first[stack_of(C, blockIdx.x)];
-    const int64_t lo = item % slots * NEWTON_CHUNK, hi = min(lo + NEWTON_CHUNK, size), base = item / slots * size;
+    const int k = stack_of(C, blockIdx.x);
+    const Stack &s = C.s[k];
+    const int64_t size = (int64_t)s.rows * s.cols, chunk = newton_chunk(size), slots = (size + chunk - 1) / chunk;
+    const int item = blockIdx.x - C.first[k];
+    const int64_t lo = item % slots * chunk, hi = min(lo + chunk, size), base = item / slots * size;
     double sum = 0.0;
-    for (int64_t i = lo + threadIdx.x * 4; i < hi; i += NT * 4) {
-        float g[4] = {}, m[4] = {};
-        const int n = (int)min<int64_t>(4, hi - i);
-        if (n == 4) {
-            load4(s, base + i, g);
-            if (MOMENTUM) {
-                floatx4 q = *(const floatx4_any *)(s.mom + base + i);
-                for (int k = 0; k < 4; ++k) q[k] = m[k] = M.keep * q[k] + M.take * g[k];
-                *(floatx4_any *)(s.mom + base + i) = q;
-            }
-        } else {
-            for (int k = 0; k < n; ++k) {
-                g[k] = value(s.g, base + i + k, s.half_g);
-                if (MOMENTUM) s.mom[base + i + k] = m[k] = M.keep * s.mom[base + i + k] + M.take * g[k];
+    constexpr int DEEP = 4;             // pieces of four that a thread has in flight
+    for (int64_t at = lo + threadIdx.x * 4; at < hi; at += NT * 4 * DEEP) {
+        float g[DEEP][4] = {}, m[DEEP][4] = {};
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            const int64_t i = at + d * NT * 4;
+            const int n = (int)min<int64_t>(4, hi - i);
+            if (n >= 4) {
+                load4(s, base + i, g[d]);
+                if (MOMENTUM) {
+                    const floatx4 q = *(const floatx4_any *)(s.mom + base + i);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) m[d][x] = q[x];
+                }
+            } else {
+                for (int x = 0; x < n; ++x) {
+                    g[d][x] = value(s.g, base + i + x, s.half_g);
+                    if (MOMENTUM) m[d][x] = s.mom[base + i + x];
+                }
             }
         }
-        for (int k = 0; k < 4; ++k) {
-            const double u = MOMENTUM ? mixed(M, m[k], g[k]) : g[k];
-            sum = fma(u, u, sum);
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            const int64_t i = at + d * NT * 4;
+            const int n = (int)min<int64_t>(4, hi - i);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (MOMENTUM) m[d][x] = M.keep * m[d][x] + M.take * g[d][x];
+                const double u = MOMENTUM ? mixed(M, m[d][x], g[d][x]) : g[d][x];
+                sum = fma(u, u, sum);
+            }
+            if (!MOMENTUM) continue;
+            if (n >= 4) *(floatx4_any *)(s.mom + base + i) = floatx4{m[d][0], m[d][1], m[d][2], m[d][3]};
+            else
+                for (int x = 0; x < n; ++x) s.mom[base + i + x] = m[d][x];
         }
     }
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
@@ -164,32 +183,40 @@ __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double 
     const int rp = s.tall ? s.np : s.mp, cp = s.tall ? s.mp : s.np;
     const int tiles = rp / 64 * (cp / 64), item = blockIdx.x - C.first[k], i = item / tiles, tile = item % tiles;
     const int r0 = tile / (cp / 64) * 64, c0 = tile % (cp / 64) * 64;
-    const int slots = (int)((size + NEWTON_CHUNK - 1) / NEWTON_CHUNK);
-    const int c = threadIdx.x % 16 * 4, n = min(max(s.cols - c0 - c, 0), 4);
-    float u[4][4] = {};
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int r = r0 + (int)threadIdx.x / 16 + 16 * x;
-        const int64_t at = i * size + (int64_t)r * s.cols + c0 + c;
-        if (r >= s.rows) continue;
-        float m[4] = {};
-        if (n == 4) {
-            load4(s, at, u[x]);
-            if (MOMENTUM) {
-                const floatx4 q = *(const floatx4_any *)(s.mom + at);
-                for (int q4 = 0; q4 < 4; ++q4) m[q4] = q[q4];
-            }
-        } else {
-            for (int q = 0; q < n; ++q) {
-                u[x][q] = value(s.g, at + q, s.half_g);
-                if (MOMENTUM) m[q] = s.mom[at + q];
-            }
-        }
-        if (MOMENTUM)
-            for (int q = 0; q < 4; ++q) u[x][q] = mixed(M, m[q], u[x][q]);
-    }
+    const int64_t chunk = newton_chunk(size);
+    const int slots = (int)((size + chunk - 1) / chunk);
     double sum = 0.0;
     for (int j = threadIdx.x; j < slots; j += NT) sum += C.sums(s)[(int64_t)i * slots + j];
+    const int c = threadIdx.x % 16 * 4, n = min(max(s.cols - c0 - c, 0), 4);
+    float u[4][4] = {}, m[4][4] = {};
+    if (r0 + 64 <= s.rows && c0 + 64 <= s.cols) {           // (no branch around a load in the tiles that lie inside: each would be waited for)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) load4(s, i * size + (int64_t)(r0 + (int)threadIdx.x / 16 + 16 * x) * s.cols + c0 + c, u[x]);
+        if (MOMENTUM)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const floatx4 q = *(const floatx4_any *)(s.mom + i * size + (int64_t)(r0 + (int)threadIdx.x / 16 + 16 * x) * s.cols + c0 + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) m[x][k] = q[k];
+            }
+    } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int r = r0 + (int)threadIdx.x / 16 + 16 * x;
+            const int64_t at = i * size + (int64_t)r * s.cols + c0 + c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (r < s.rows && k < n) {
+                    u[x][k] = value(s.g, at + k, s.half_g);
+                    if (MOMENTUM) m[x][k] = s.mom[at + k];
+                }
+        }
+    }
+    if (MOMENTUM)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[x][k] = mixed(M, m[x][k], u[x][k]);
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
     if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();

@@ -9,7 +9,6 @@ constexpr int NEWTON_TILE = 128;                // the large tile; the small one
 constexpr int NEWTON_ONE = 1;                   // (not a tile:) the kernel that takes a matrix in LDS, at most 64 x NEWTON_ONE_N, padded to 64
 constexpr int64_t NEWTON_ONE_N = 384;
 constexpr int NEWTON_STACKS = 24;               // of a launch: they travel in its arguments
-constexpr int64_t NEWTON_CHUNK = 16384;         // elements whose squares a workgroup adds up
 
 // A stack of `count` matrices rows x cols, or a run of one's matrices.  The steps work on m x n with m <= n (the transpose of a tall
 // matrix), padded with zeros to multiples of the tile.
@@ -26,7 +25,15 @@ inline NewtonSize newton_size(int64_t count, int32_t rows, int32_t cols, int til
 // 16-byte words of the working memory: X, twice; A and B; the sums of squares.  A value is two halves.
 inline int64_t newton_words_x(const NewtonSize &s) { return (int64_t)s.mp * s.np / 4; }         // of one X
 inline int64_t newton_words_a(const NewtonSize &s) { return (int64_t)s.mp * s.mp / 4; }         // of one A
-inline int64_t newton_slots(const NewtonSize &s) { return ((int64_t)s.rows * s.cols + NEWTON_CHUNK - 1) / NEWTON_CHUNK; }
+// elements whose squares a workgroup adds up: a thread's four pieces of four, or a 1024th of the matrix
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int64_t newton_chunk(int64_t size) { return size <= 4096 * 1024 ? 4096 : (size / 1024 + 4095) / 4096 * 4096; }
+inline int64_t newton_slots(const NewtonSize &s) {
+    const int64_t size = (int64_t)s.rows * s.cols, chunk = newton_chunk(size);
+    return (size + chunk - 1) / chunk;
+}
 inline int64_t newton_words(const NewtonSize &s, int tile) {
     if (tile == NEWTON_ONE) return 0;
     return s.count * (2 * newton_words_x(s) + 2 * newton_words_a(s) + (newton_slots(s) + 1) / 2);

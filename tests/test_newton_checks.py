@@ -156,7 +156,7 @@ def test_every_matrix_is_in_one_launch():
             m, w = min(r, q), max(r, q)
             pad = 64 if tile == 1 else tile
             assert count >= 1 and mp % pad == 0 and np_ % pad == 0 and m <= mp < m + pad and w <= np_ < w + pad
-            assert (words == 0 and m <= 64 and w <= 384) if tile == 1 else words >= count * (mp * np_ // 2 + mp * mp // 2 + -(-r * q // 16384) // 2)
+            assert (words == 0 and m <= 64 and w <= 384) if tile == 1 else words >= count * (mp * np_ // 2 + mp * mp // 2 + -(-r * q // max(4096, -(-(r * q // 1024) // 4096) * 4096)) // 2)
             covered[i] += range(first, first + count)
         for i, (c, r, q) in enumerate(shapes):
             assert covered[i] == (list(range(c)) if r and q else [])
