@@ -31,6 +31,19 @@ inline bool group_core_weights(int64_t n_rows, int n_groups, int64_t n_in, int64
     return n_in >= 128 && n_out >= 128 && n_rows >= 64 * (int64_t)n_groups && group_ceil(n_in, 256) * group_ceil(n_out, 256) * group_ceil(n_rows, 256) >= n_cu / 2;
 }
 
+// Few rows: workgroups of 32 x 32 without a loop of barriers, against tiles of 64 (us, y / dx, few / tiles).  Where groups have few rows
+// (float 64 rows of 8 groups, 2048 x 2048: 31 / 73, 30 / 52; 2048 of 64, 512 x 512: 29 / 48, 33 / 43; 512 of 8, 1024 x 1024: 27 / 41,
+// 31 / 29; bfloat16 64 of 8: 17 / 24, 16 / 21; 2048 of 64: 15 / 16, 16 / 15; 512 of 8: 14 / 13.5, 14 / 10), and forward where few tiles
+// leave compute units to the longer way (float 1024 x 256 x 172 of 16 5.9 / 9.7, 4096 of 16 10.5 / 10.1, 8192 of 16 22 / 16).
+inline bool group_few_rows(int64_t n_rows, int n_groups, int64_t n, bool is_float, bool transposed, int n_cu) {
+    const int64_t a_group = n_rows / std::max<int64_t>(1, std::min<int64_t>(n_groups, n_rows));
+    return a_group <= (is_float ? 48 : 32) || (is_float && !transposed && group_row_tiles(n_rows, n_groups, 32) * group_ceil(n, 32) <= 3 * n_cu);
+}
+// The weight gradients of few rows: a group's rows in one go, as long as that is short
+inline bool group_few_weights(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, int n_cu) {
+    return n_rows <= 4096 && n_rows <= 512 * (int64_t)n_groups && n_groups * group_ceil(n_in, 32) * group_ceil(n_out, 32) <= 4 * n_cu;
+}
+
 // -- weight gradients: tiles of 128 or of 64 --
 inline bool group_weights_large(int64_t n_in, int64_t n_out) { return n_in > 64 && n_out > 64 && n_in * n_out >= 1 << 18; }
 
@@ -41,4 +54,4 @@ inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int64_t wor
     return std::max<int64_t>(256, group_ceil(group_ceil(n_rows, want), 64) * 64);
 }
 // slabs: the chunks of those groups that have more than one
-inline int64_t group_slabs(int64_t n_rows, int64_t chunk) { return 2 * (n_rows / chunk); }
+inline int64_t group_slabs(int64_t n_rows, int64_t chunk) { return n_rows > chunk ? 2 * (n_rows / chunk) : 0; }

@@ -586,6 +586,7 @@ __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
 }
 
 #include "grouped_core.h"
+#include "grouped_few.h"
 
 // -- launches ---------------------------------------------------------------------------------
 
@@ -614,6 +615,13 @@ void launch_rows(const gsplit_ctx *ctx, int32_t dtype, RowsArgs A, hipStream_t s
         hipLaunchKernelGGL(k_grouped_rows_core<TRANSPOSED>, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(CT), 0, st, A);
         return;
     }
+    if (group_few_rows(A.list.n, A.G, A.N, dtype == GSPLIT_F32, TRANSPOSED, ctx->n_cu)) {
+        A.tiles_m = group_row_tiles(A.list.n, A.G, 32);
+        A.tiles_n = (int32_t)group_ceil(A.N, 32);
+        const auto kernel = dtype == GSPLIT_F32 ? k_grouped_rows_few<float, TRANSPOSED> : k_grouped_rows_few<uint16_t, TRANSPOSED>;
+        hipLaunchKernelGGL(kernel, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(NT), 0, st, A);
+        return;
+    }
     const bool large = group_row_tiles(A.list.n, A.G, 128) * group_ceil(A.N, 128) >= ctx->n_cu;
     if (dtype == GSPLIT_F32) {
         if (large) launch_rows<float, Tile<128, 128>, TRANSPOSED>(A, st);
@@ -629,8 +637,8 @@ struct WeightForm { bool core; int tile; int64_t chunk, slabs; };
 WeightForm weight_form(int n_cu, int64_t n_rows, int32_t n_groups, int32_t n_in, int32_t n_out, bool granules) {
     WeightForm f;
     f.core = granules && group_core_weights(n_rows, n_groups, n_in, n_out, n_cu);
-    f.tile = f.core ? CORE_TILE : group_weights_large(n_in, n_out) ? 128 : 64;
-    f.chunk = group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu : 2 * n_cu);
+    f.tile = f.core ? CORE_TILE : group_few_weights(n_rows, n_groups, n_in, n_out, n_cu) ? 32 : group_weights_large(n_in, n_out) ? 128 : 64;
+    f.chunk = f.tile == 32 ? std::max<int64_t>(n_rows, 1) : group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu : 2 * n_cu);
     f.slabs = group_slabs(n_rows, f.chunk);
     return f;
 }
@@ -695,6 +703,7 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
             {
                 GsTimeScope ts(ctx, "grouped_dw", -1, st);
                 const auto kernel = f.core ? k_grouped_weights_core
+                                    : f.tile == 32 ? c->dtype == GSPLIT_F32 ? k_grouped_weights_few<float> : k_grouped_weights_few<uint16_t>
                                     : c->dtype == GSPLIT_F32 ? f.tile == 128 ? k_grouped_weights<float, Tile<128, 128>> : k_grouped_weights<float, Tile<64, 64>>
                                     : f.tile == 128 ? k_grouped_weights<uint16_t, Tile<128, 128>> : k_grouped_weights<uint16_t, Tile<64, 64>>;
                 hipLaunchKernelGGL(kernel, grid, dim3(f.core ? CT : NT), 0, st, A);
