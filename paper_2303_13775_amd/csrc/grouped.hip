@@ -559,29 +559,61 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
 
 // the slabs of every group that has several, added up in their order: blockIdx.y counts those groups
 __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
-    const int64_t words = (int64_t)A.K * A.N, all = words + (A.db ? A.N : 0);
-    // the blockIdx.y-th group of several chunks
-    int g = 0, slab = 0, chunks = 0, seen = -1;
-    for (; g < A.G; ++g) {
-        const int lo = min(max(A.ptr[g], 0), A.list.n), hi = min(max(A.ptr[g + 1], lo), A.list.n);
-        chunks = (int)(((int64_t)(hi - lo) + A.per - 1) / A.per);
-        if (chunks > 1 && ++seen == (int)blockIdx.y) break;
-        slab += chunks > 1 ? chunks : 0;
-    }
-    if (g == A.G || slab + chunks > A.slabs) return;
-    const float *part = A.slab + slab * (words + A.N);
-    for (int64_t i = blockIdx.x * (int64_t)NT + threadIdx.x; i < all; i += (int64_t)gridDim.x * NT) {
-        float sum = 0.f;
-        int c = 0;
-        for (; c + 8 <= chunks; c += 8) {
-            float v[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = part[(c + q) * (words + A.N) + i];
-            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    const int64_t words = (int64_t)A.K * A.N, all = words + (A.db ? A.N : 0), each = words + A.N;
+    // the blockIdx.y-th group of several chunks, a lane a group
+    const int lane = threadIdx.x & 63;
+    int g = -1, slab = 0, chunks = 0, left = blockIdx.y;
+    for (int base = 0; base < A.G && g < 0; base += 64) {
+        const int x = base + lane;
+        const int lo = min(max(A.ptr[min(x, A.G)], 0), A.list.n), hi = min(max(A.ptr[min(x + 1, A.G)], lo), A.list.n);
+        const int n = x < A.G ? (int)(((int64_t)(hi - lo) + A.per - 1) / A.per) : 0, own = n > 1 ? n : 0;
+        int sum = own;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(sum, o);
+            if (lane >= o) sum += up;
         }
-        for (; c < chunks; ++c) sum += part[c * (words + A.N) + i];
-        if (i < words) A.dw[g * words + i] = sum;
-        else A.db[(int64_t)g * A.N + (i - words)] = sum;
+        uint64_t several = __ballot(own > 0);
+        const int found = __popcll(several);
+        if (left < found) {
+            for (; left > 0; --left) several &= several - 1;
+            const int l = __builtin_ctzll(several);
+            g = base + l;
+            chunks = __builtin_amdgcn_readlane(own, l);
+            slab += __builtin_amdgcn_readlane(sum, l) - chunks;
+        } else {
+            left -= found;
+            slab += __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+    if (g < 0 || slab + chunks > A.slabs) return;
+    const float *part = A.slab + slab * each;
+    float *const dw = A.dw + g * words, *const db = A.db ? A.db + (int64_t)g * A.N : nullptr;
+    // four words a thread (the last ones, and those of rows that are no multiple of four, by themselves)
+    const int64_t quads = words / 4, items = quads + (all - quads * 4);
+    for (int64_t x = blockIdx.x * (int64_t)NT + threadIdx.x; x < items; x += (int64_t)gridDim.x * NT) {
+        if (x < quads) {
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const auto add = [&](const u32x4 &q) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] += __uint_as_float(q[k]);
+            };
+            int c = 0;
+            for (; c + 4 <= chunks; c += 4) {
+                u32x4 q[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[k] = *(const u32x4_any *)(part + (c + k) * each + 4 * x);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) add(q[k]);
+            }
+            for (; c < chunks; ++c) add(*(const u32x4_any *)(part + c * each + 4 * x));
+            store4(dw + 4 * x, sum, 4);
+        } else {
+            const int64_t i = quads * 4 + (x - quads);
+            float sum = 0.f;
+            for (int c = 0; c < chunks; ++c) sum += part[c * each + i];
+            if (i < words) dw[i] = sum;
+            else db[i - words] = sum;
+        }
     }
 }
 
@@ -710,8 +742,8 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
             }
             if (f.slabs) {
                 GsTimeScope ts(ctx, "grouped_dw_sum", -1, st);
-                const int64_t words = ((int64_t)c->n_in + 1) * c->n_out;
-                hipLaunchKernelGGL(k_grouped_weights_sum, dim3((unsigned)std::min<int64_t>(group_ceil(words, NT), 1024),
+                const int64_t quads = (int64_t)c->n_in * c->n_out / 4 + c->n_out + 4;
+                hipLaunchKernelGGL(k_grouped_weights_sum, dim3((unsigned)std::min<int64_t>(group_ceil(quads, NT), 1024),
                                                                (unsigned)std::min<int64_t>(c->n_groups, n_rows / f.chunk)), dim3(NT), 0, st, A);
             }
         }
