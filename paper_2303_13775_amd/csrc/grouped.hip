@@ -121,15 +121,15 @@ struct Along {
 };
 
 // An operand with the contraction across its rows: element (i, k) at row(k)[i], i < cols; of these the ones from `first` on.  A thread
-// takes W columns of the eight rows of a granule.
-template <class T, int ROWS>
+// takes W columns of the eight rows of a granule; THREADS of them fetch the operand.
+template <class T, int ROWS, int THREADS = NT>
 struct Across {
-    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, W = ROWS * KG / NT, WORDS = W * (int)sizeof(T) / 4;
-    static_assert(W * NT == ROWS * KG && (WORDS == 1 || WORDS == 2), "one item a thread");
+    static constexpr int KG = Kind<T>::KG, KT = Kind<T>::KT, W = ROWS * KG / THREADS, WORDS = W * (int)sizeof(T) / 4;
+    static_assert(W * THREADS == ROWS * KG && (WORDS == 1 || WORDS == 2 || WORDS == 4), "one item a thread");
     int cols, col, base;            // this thread's first column; LDS row of it
     uint32_t r[8][WORDS];
 
-    static __device__ __forceinline__ int granule() { return (int)threadIdx.x / (ROWS / W); }
+    static __device__ __forceinline__ int granule() { return (int)threadIdx.x % THREADS / (ROWS / W); }
     __device__ __forceinline__ void init(int n_cols, int first) {
         cols = n_cols;
         const int want = first + (int)threadIdx.x % (ROWS / W) * W;
@@ -155,6 +155,10 @@ struct Across {
                 const T *p = row(j) + col;
                 if constexpr (WORDS == 1) {
                     r[j][0] = *(const u32_any *)p;
+                } else if constexpr (WORDS == 4) {
+                    const u32x4 a = *(const u32x4_any *)p;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) r[j][w] = a[w];
                 } else {
                     const u32x2 a = *(const u32x2_any *)p;
                     r[j][0] = a[0]; r[j][1] = a[1];
@@ -324,10 +328,19 @@ __device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G
     }
     // Workgroups are dealt round-robin to the eight XCDs: consecutive tiles (the same rows, the same matrix) go to one of them, for its
     // L2, an eighth of the tiles there are each (not of those there may be, or the last XCDs have less to do)
-    const int64_t total = all * across, each = (total + 7) / 8, x = (block & 7) * each + (block >> 3);
-    if (block >> 3 >= each || x >= total) return false;
-    int j = (int)(x / across), slab = 0;
-    s.side = (int)(x - j * across);
+    int j, slab = 0;
+    if (EMPTY_TOO && all >= 16) {
+        // (chunks of rows are of all lengths, and the long ones lie side by side: each in turn to another XCD)
+        const int q = (int)((block >> 3) / across);
+        j = q * 8 + (int)(block & 7);
+        s.side = (int)((block >> 3) - q * across);
+        if (j >= all) return false;
+    } else {
+        const int64_t total = all * across, each = (total + 7) / 8, x = (block & 7) * each + (block >> 3);
+        if (block >> 3 >= each || x >= total) return false;
+        j = (int)(x / across);
+        s.side = (int)(x - j * across);
+    }
     for (int base = 0;;) {
         const int n = __builtin_amdgcn_readlane(sum, 63);
         if (j < n) {
@@ -455,7 +468,7 @@ struct WeightArgs {
     const int32_t *ptr;
     RowList list;
     int32_t per;                // rows of a chunk
-    int64_t items;              // chunks, at most
+    int64_t items;              // chunks, at most (a multiple of 8)
     int32_t tiles_m, tiles_n;
     float *dw, *db;
     float *slab;                // [slabs x (K + 1) x N]: the chunks' gradients of W, then of b
@@ -468,6 +481,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
     constexpr int BM = TL::BM, BN = TL::BN, KG = Kind<T>::KG, P = Kind<T>::PLANES;
     __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
     __shared__ double s_sum[KG][BN];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
     for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
         Spot s;
@@ -478,17 +492,21 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         const T *xs = (const T *)A.x, *dys = (const T *)A.dy;
         const auto x_row = [&](int k) { return xs + row_at(max(A.list.at(s.first + k), 0), A.ldx); };
         const auto dy_row = [&](int k) { return dys + row_at(max(A.list.at(s.first + k), 0), A.lddy); };
-        Across<T, BM> la;
-        Across<T, BN> lb;
-        la.init(A.K, m0);
-        lb.init(A.N, n0);
+        // two waves fetch x, two dy: sixteen bytes a load
+        static_assert(BM == BN, "one operand is like the other");
+        typedef Across<T, BM, NT / 2> Half;
+        Half l;
+        const bool is_dy = wave >= 2;
+        l.init(is_dy ? A.N : A.K, is_dy ? n0 : m0);
+        const T *const from = is_dy ? dys : xs;
+        const uint32_t ld = is_dy ? A.lddy : A.ldx;
+        uint4 *const to = is_dy ? s_b : s_a;
         // the rows of the next tile are looked up a tile ahead: their loads would wait for the list's
         int next[8];
-        static_assert(BM == BN, "both operands' granules hold the same rows");
         const auto look_up = [&](int t) __attribute__((always_inline)) {
             int place[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) place[j] = s.first + min(t * Kind<T>::KT + Kind<T>::k_of(la.granule(), j), s.rows - 1);
+            for (int j = 0; j < 8; ++j) place[j] = s.first + min(t * Kind<T>::KT + Kind<T>::k_of(l.granule(), j), s.rows - 1);
             if (A.list.rows) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) next[j] = A.list.rows[place[j]];
@@ -500,13 +518,12 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         const auto load = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) next[j] = (uint32_t)next[j] < (uint32_t)A.list.n ? next[j] : 0;
-            la.load([&](int j) { return xs + row_at(next[j], A.ldx); });
-            lb.load([&](int j) { return dys + row_at(next[j], A.lddy); });
+            l.load([&](int j) { return from + row_at(next[j], ld); });
             look_up(t + 1);
         };
         Sums<T, TL> sums;
         sums.clear();
-        double col[Across<T, BN>::W] = {};
+        double col[Half::W] = {};
         const bool bias = A.db && m0 == 0;
         if (m0 + BM > A.K) clear_rows<T, BM>(s_a);
         if (n0 + BN > A.N) clear_rows<T, BN>(s_b);
@@ -514,16 +531,14 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         const int KT = (s.rows + Kind<T>::KT - 1) / Kind<T>::KT;
         if (KT > 0) { look_up(0); load(0); }
         for (int t = 0; t < KT; ++t) {
-            la.cut(t, s.rows);
-            lb.cut(t, s.rows);
-            la.store(s_a);
-            lb.store(s_b);
-            if (bias) {
+            l.cut(t, s.rows);
+            l.store(to);
+            if (bias && is_dy) {
 #pragma unroll
-                for (int c = 0; c < Across<T, BN>::W; ++c) {
+                for (int c = 0; c < Half::W; ++c) {
                     float f = 0.f, h = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) { f += lb.at(j, c); h += lb.at(j + 1, c); }
+                    for (int j = 0; j < 8; j += 2) { f += l.at(j, c); h += l.at(j + 1, c); }
                     col[c] += (double)f + (double)h;
                 }
             }
@@ -541,11 +556,11 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
             if (m < A.K && n < A.N) store4(out + (int64_t)m * A.N + n, v, A.N - n);
         });
         if (bias) {
-            constexpr int W = Across<T, BN>::W;
-            const int g = lb.granule();
+            if (is_dy) {
 #pragma unroll
-            for (int c = 0; c < W; ++c)
-                if (lb.base + c >= 0 && lb.base + c < BN) s_sum[g][lb.base + c] = col[c];
+                for (int c = 0; c < Half::W; ++c)
+                    if (l.base + c >= 0 && l.base + c < BN) s_sum[l.granule()][l.base + c] = col[c];
+            }
             __syncthreads();
             for (int j = threadIdx.x; j < BN && n0 + j < A.N; j += NT) {
                 double sum = 0.0;
@@ -670,7 +685,7 @@ WeightForm weight_form(int n_cu, int64_t n_rows, int32_t n_groups, int32_t n_in,
     WeightForm f;
     f.core = granules && group_core_weights(n_rows, n_groups, n_in, n_out, n_cu);
     f.tile = f.core ? CORE_TILE : group_few_weights(n_rows, n_groups, n_in, n_out, n_cu) ? 32 : group_weights_large(n_in, n_out) ? 128 : 64;
-    f.chunk = f.tile == 32 ? std::max<int64_t>(n_rows, 1) : group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu : 2 * n_cu);
+    f.chunk = f.tile == 32 ? std::max<int64_t>(n_rows, 1) : group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu / 2 : 4 * n_cu);
     f.slabs = group_slabs(n_rows, f.chunk);
     return f;
 }
@@ -729,7 +744,7 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
         }
         if (d_dw) {
             WeightArgs A{d_x, d_dy, (uint32_t)x_stride, (uint32_t)dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)f.chunk,
-                         n_rows / f.chunk + c->n_groups, (int32_t)group_ceil(c->n_in, f.tile), (int32_t)group_ceil(c->n_out, f.tile), d_dw, d_dbias,
+                         group_ceil(n_rows / f.chunk + c->n_groups, 8) * 8, (int32_t)group_ceil(c->n_in, f.tile), (int32_t)group_ceil(c->n_out, f.tile), d_dw, d_dbias,
                          (float *)d_work, f.slabs};
             const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));
             {
