@@ -23,12 +23,16 @@ inline int64_t group_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // tiles of rows of all groups, at most: every group that has rows leaves one of its tiles short
 inline int64_t group_row_tiles(int64_t n_rows, int n_groups, int rows) { return n_rows / rows + std::min<int64_t>(n_groups, n_rows); }
 
-// bfloat16 rows of whole granules: tiles of 256 x 256 where they are enough for the chip
+// bfloat16 rows of whole granules (16 bytes): tiles of 256 x 256 that go straight into LDS, against tiles of 128 or 64 through registers
+// (us, y / dx / dW).  16384 rows of 16 groups 512 x 512 22 / 22 / 37 and 31 / 26 / 53; 8192 of 8 1024 x 1024 34 / 34 / 53 and 50 / 42 / 79; 4096 of 2
+// 2048 x 2048 56 / 55 / 81 and 85 / 69 / 108; 32768 of 128 512 x 512 41 / 41 / 76 and 50 / 43 / 97; but 8192 of 8 512 x 512 21 / 20 / 33 and
+// 19 / 18 / 37, 65536 of 8 128 x 128 21 / 21 / 34 and 18 / 17 / 41.
 inline bool group_core_rows(int64_t n_rows, int n_groups, int64_t k, int64_t n, int n_cu) {
-    return group_ceil(n_rows, 256) * group_ceil(n, 256) >= n_cu / 2 && k >= 128 && n >= 128 && n_rows >= 64 * (int64_t)n_groups;
+    return k >= 128 && n > 128 && n_rows >= 64 * (int64_t)n_groups && group_ceil(n_rows, 256) * group_ceil(n, 256) >= n_cu / 2;
 }
 inline bool group_core_weights(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, int n_cu) {
-    return n_in >= 128 && n_out >= 128 && n_rows >= 64 * (int64_t)n_groups && group_ceil(n_in, 256) * group_ceil(n_out, 256) * group_ceil(n_rows, 256) >= n_cu / 2;
+    return n_in >= 128 && n_out >= 128 && n_rows >= 64 * (int64_t)n_groups &&
+           group_ceil(n_in, 256) * group_ceil(n_out, 256) * group_ceil(n_rows, 256) >= n_cu / 2;
 }
 
 // Few rows: workgroups of 32 x 32 without a loop of barriers, against tiles of 64 (us, y / dx, few / tiles).  Where groups have few rows
@@ -47,7 +51,10 @@ inline bool group_few_weights(int64_t n_rows, int n_groups, int64_t n_in, int64_
 // -- weight gradients: tiles of 128 or of 64 --
 inline bool group_weights_large(int64_t n_in, int64_t n_out) { return n_in > 64 && n_out > 64 && n_in * n_out >= 1 << 18; }
 
-// The rows of a group are taken in chunks where one group's tiles do not fill the chip: as many chunks of all rows as give `workgroups`
+// The rows of a group are taken in chunks where one group's tiles do not fill the chip: as many chunks of all rows as give `workgroups`.
+// Short chunks even out groups of all sizes, and cost the sum over them.  Tiles of 128 and 64, four workgroups a compute unit (three, two):
+// 20011 rows of 24 groups 1000 x 1021 bf16 157 us (165, 184), float 400 (422, 489), 65536 of 8 512 x 512 float 300 (279, 349).  Tiles of 256, one
+// every two compute units (one, two): 65536 of 8 512 x 512 82 us (97, 123), 20011 of 24 1000 x 1024 115 (112, 160).
 inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int64_t workgroups) {
     const int64_t want = group_ceil(workgroups, tiles_of_a_group);
     if (want <= 1) return std::max<int64_t>(n_rows, 1);

@@ -42,8 +42,10 @@ inline int64_t newton_words(const NewtonSize &s, int tile) {
 inline int64_t newton_tiles_x(const NewtonSize &s, int tile) { return (int64_t)(s.mp / tile) * (s.np / tile); }
 inline int64_t newton_tiles_a(const NewtonSize &s, int tile) { const int64_t t = s.mp / tile; return t * (t + 1) / 2; }
 
-// The tile of a call's matrices: the large one where its tiles of A fill the chip.
-inline bool newton_large(int64_t tiles_of_a) { return tiles_of_a >= 256; }
+// The tile of a call's matrices of more than 64 rows, by the tiles of 128 x 128 that all their A have (us of five steps, large / small):
+// four of 1024 x 1024 (144) 470 / 580, one of 2048 x 2048 (136) 799 / 1023; 32 of 200 x 200 (96) 193 / 144, two of 1024 x 4096 (72) 893 / 884,
+// one of 1024 x 1024 (36) 420 / 244, 16 of 128 x 2048 (16) 339 / 216.
+inline bool newton_large(int64_t tiles_of_a) { return tiles_of_a >= 128; }
 // A launch takes stacks up to this many padded elements, so that working memory stays in proportion
 constexpr int64_t NEWTON_LAUNCH = 1 << 27;
 
