@@ -298,13 +298,13 @@ def test_captured_calls(ctx, dtype):
         assert all(torch.equal(a, c) for a, c in zip(got, want)), k
 
 
-def test_another_stream(ctx):
+def test_other_streams(ctx):
     rng = np.random.default_rng(8)
     rows, groups, n_in, n_out = 3000, 4, 96, 80
     group = torch.from_numpy(_draw_groups(rng, rows, groups)).cuda()
     x, w = torch.randn((rows, n_in), device="cuda"), torch.randn((groups, n_in, n_out), device="cuda")
     res = []
-    for s in (torch.cuda.current_stream(), torch.cuda.Stream()):
+    for s in (torch.cuda.current_stream(), *[torch.cuda.Stream() for _ in range(4)]):      # (a stream for every hardware queue)
         s.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(s):
             ptr, order = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (groups + 1, rows))
@@ -314,7 +314,7 @@ def test_another_stream(ctx):
             ctx.gsplit_grouped_linear_bwd(x, ptr, order, w, y, dx, dw, db, ctx.gsplit_grouped_linear_work(x, w))
             torch.cuda.synchronize()
             res.append((ptr, order, y, dx, dw, db))
-    assert all(torch.equal(a, b) for a, b in zip(*res))
+    assert all(torch.equal(a, b) for r in res[1:] for a, b in zip(res[0], r))
 
 
 def test_more_than_32_bits_of_elements(ctx):

@@ -277,18 +277,18 @@ def test_captured_steps(ctx, shapes):
         assert all(torch.equal(a, b) for x, y in ((p, pe), (m, me), (o, oe)) for a, b in zip(x, y)), k
 
 
-def test_another_stream(ctx):
+def test_other_streams(ctx):
     from paper_2303_13775_amd import MatrixTensors
     shapes = [(3, 90, 200), (1, 500, 300)]
     mats, res = _matrices(shapes, 6), []
-    for s in (torch.cuda.current_stream(), torch.cuda.Stream()):
+    for s in (torch.cuda.current_stream(), *[torch.cuda.Stream() for _ in range(4)]):      # (a stream for every hardware queue)
         s.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(s):
             outs = [torch.zeros_like(g) for g in mats]
             ctx.gsplit_orthogonalize(MatrixTensors(mats, outs))
             torch.cuda.synchronize()
             res.append(outs)
-    assert all(torch.equal(a, b) for a, b in zip(*res))
+    assert all(torch.equal(a, b) for r in res[1:] for a, b in zip(res[0], r))
 
 
 def test_refusals(ctx):
