@@ -18,7 +18,6 @@ inline GroupRuns group_runs(int64_t n_rows, int n_groups, int64_t counters, int 
 }
 
 // -- the products: tiles of `rows` x `cols` --
-struct GroupTile { int rows, cols; };
 inline int64_t group_ceil(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // tiles of rows of all groups, at most: every group that has rows leaves one of its tiles short
 inline int64_t group_row_tiles(int64_t n_rows, int n_groups, int rows) { return n_rows / rows + std::min<int64_t>(n_groups, n_rows); }
@@ -62,3 +61,28 @@ inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int64_t wor
 }
 // slabs: the chunks of those groups that have more than one
 inline int64_t group_slabs(int64_t n_rows, int64_t chunk) { return n_rows > chunk ? 2 * (n_rows / chunk) : 0; }
+
+// Which kernel forms y or dx [n_rows x n] of a contraction of k, and which the weight gradients; granules: rows of whole 16 bytes
+enum GroupForm { GROUP_CORE, GROUP_FEW, GROUP_128, GROUP_64 };
+inline GroupForm group_rows_form(int64_t n_rows, int n_groups, int64_t k, int64_t n, bool is_float, bool transposed, bool granules, int n_cu) {
+    if (!is_float && granules && group_core_rows(n_rows, n_groups, k, n, n_cu)) return GROUP_CORE;
+    if (group_few_rows(n_rows, n_groups, n, is_float, transposed, n_cu)) return GROUP_FEW;
+    return group_row_tiles(n_rows, n_groups, 128) * group_ceil(n, 128) >= n_cu ? GROUP_128 : GROUP_64;
+}
+struct GroupWeights { GroupForm form; int tile; int64_t chunk, slabs; };
+inline GroupWeights group_weights_form(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, bool is_float, bool granules, int n_cu) {
+    GroupWeights f{};
+    f.form = !is_float && granules && group_core_weights(n_rows, n_groups, n_in, n_out, n_cu) ? GROUP_CORE
+             : group_few_weights(n_rows, n_groups, n_in, n_out, n_cu) ? GROUP_FEW : group_weights_large(n_in, n_out) ? GROUP_128 : GROUP_64;
+    f.tile = f.form == GROUP_CORE ? 256 : f.form == GROUP_FEW ? 32 : f.form == GROUP_128 ? 128 : 64;
+    f.chunk = f.form == GROUP_FEW ? std::max<int64_t>(n_rows, 1)
+                                  : group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.form == GROUP_CORE ? n_cu / 2 : 4 * n_cu);
+    f.slabs = group_slabs(n_rows, f.chunk);
+    return f;
+}
+// slabs that a call may need, whatever its addresses
+inline int64_t group_most_slabs(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, bool is_float, int n_cu) {
+    const bool granules = n_in % 8 == 0 && n_out % 8 == 0;
+    return std::max(group_weights_form(n_rows, n_groups, n_in, n_out, is_float, granules, n_cu).slabs,
+                    group_weights_form(n_rows, n_groups, n_in, n_out, is_float, false, n_cu).slabs);
+}

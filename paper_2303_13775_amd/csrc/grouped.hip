@@ -344,10 +344,12 @@ __device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G
     for (int base = 0;;) {
         const int n = __builtin_amdgcn_readlane(sum, 63);
         if (j < n) {
-            const int l = __builtin_ctzll(__ballot(sum > j));
+            const uint64_t past = __ballot(sum > j);
+            const int l = past ? __builtin_ctzll(past) : 0;
             const int c = j - (__builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(tiles, l));
             s.g = base + l;
             s.chunks = __builtin_amdgcn_readlane(tiles, l);
+            if (c < 0 || c >= s.chunks) return false;       // (offsets that make no sense may make sums that do not fit)
             s.first = __builtin_amdgcn_readlane(lo, l) + c * per;
             s.rows = min(per, __builtin_amdgcn_readlane(hi, l) - s.first);
             s.slab = slab + __builtin_amdgcn_readlane(slabs, l) - __builtin_amdgcn_readlane(own_slabs, l) + c;
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
         Spot s;
         if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
         const bool whole = s.chunks == 1;
-        if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
+        if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * BM, n0 = s.side % A.tiles_n * BN;
         const T *xs = (const T *)A.x, *dys = (const T *)A.dy;
         const auto x_row = [&](int k) { return xs + row_at(max(A.list.at(s.first + k), 0), A.ldx); };
@@ -600,7 +602,7 @@ __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
             slab += __builtin_amdgcn_readlane(sum, 63);
         }
     }
-    if (g < 0 || slab + chunks > A.slabs) return;
+    if (g < 0 || slab < 0 || (int64_t)slab + chunks > A.slabs) return;
     const float *part = A.slab + slab * each;
     float *const dw = A.dw + g * words, *const db = A.db ? A.db + (int64_t)g * A.N : nullptr;
     // four words a thread (the last ones, and those of rows that are no multiple of four, by themselves)
@@ -640,12 +642,6 @@ __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
 constexpr int64_t MOST_BLOCKS = 1 << 22;        // (a launch has less than 2^32 threads; workgroups go round)
 inline unsigned blocks(int64_t total) { return (unsigned)std::min<int64_t>((total + 7) / 8 * 8, MOST_BLOCKS); }
 
-template <class T, class TL, bool TRANSPOSED>
-void launch_rows(RowsArgs A, hipStream_t st) {
-    A.tiles_m = group_row_tiles(A.list.n, A.G, TL::BM);
-    A.tiles_n = (int32_t)group_ceil(A.N, TL::BN);
-    hipLaunchKernelGGL((k_grouped_rows<T, TL, TRANSPOSED>), dim3(blocks(A.tiles_m * A.tiles_n)), dim3(NT), 0, st, A);
-}
 // rows that start at multiples of 16 bytes, and are a whole number of them
 bool in_granules(std::initializer_list<const void *> p, std::initializer_list<int64_t> widths) {
     for (const void *x : p)
@@ -654,40 +650,31 @@ bool in_granules(std::initializer_list<const void *> p, std::initializer_list<in
         if (n % 8) return false;
     return true;
 }
-template <bool TRANSPOSED>
-void launch_rows(const gsplit_ctx *ctx, int32_t dtype, RowsArgs A, hipStream_t st) {
-    if (dtype == GSPLIT_BF16 && in_granules({A.a, A.w, A.c}, {A.K, A.N, A.lda, A.ldc}) && group_core_rows(A.list.n, A.G, A.K, A.N, ctx->n_cu)) {
-        A.tiles_m = group_row_tiles(A.list.n, A.G, CORE_TILE);
-        A.tiles_n = (int32_t)group_ceil(A.N, CORE_TILE);
-        hipLaunchKernelGGL(k_grouped_rows_core<TRANSPOSED>, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(CT), 0, st, A);
-        return;
-    }
-    if (group_few_rows(A.list.n, A.G, A.N, dtype == GSPLIT_F32, TRANSPOSED, ctx->n_cu)) {
-        A.tiles_m = group_row_tiles(A.list.n, A.G, 32);
-        A.tiles_n = (int32_t)group_ceil(A.N, 32);
-        const auto kernel = dtype == GSPLIT_F32 ? k_grouped_rows_few<float, TRANSPOSED> : k_grouped_rows_few<uint16_t, TRANSPOSED>;
-        hipLaunchKernelGGL(kernel, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(NT), 0, st, A);
-        return;
-    }
-    const bool large = group_row_tiles(A.list.n, A.G, 128) * group_ceil(A.N, 128) >= ctx->n_cu;
-    if (dtype == GSPLIT_F32) {
-        if (large) launch_rows<float, Tile<128, 128>, TRANSPOSED>(A, st);
-        else launch_rows<float, Tile<64, 64>, TRANSPOSED>(A, st);
-    } else {
-        if (large) launch_rows<uint16_t, Tile<128, 128>, TRANSPOSED>(A, st);
-        else launch_rows<uint16_t, Tile<64, 64>, TRANSPOSED>(A, st);
+template <class T, bool TRANSPOSED>
+void launch_rows(const gsplit_ctx *ctx, RowsArgs A, hipStream_t st) {
+    const auto launch = [&](auto kernel, int rows, int cols, int threads) {
+        A.tiles_m = group_row_tiles(A.list.n, A.G, rows);
+        A.tiles_n = (int32_t)group_ceil(A.N, cols);
+        hipLaunchKernelGGL(kernel, dim3(blocks(A.tiles_m * A.tiles_n)), dim3(threads), 0, st, A);
+    };
+    constexpr bool FLOAT = sizeof(T) == 4;
+    switch (group_rows_form(A.list.n, A.G, A.K, A.N, FLOAT, TRANSPOSED, !FLOAT && in_granules({A.a, A.w, A.c}, {A.K, A.N, A.lda, A.ldc}), ctx->n_cu)) {
+    case GROUP_CORE: return launch(k_grouped_rows_core<TRANSPOSED>, CORE_TILE, CORE_TILE, CT);
+    case GROUP_FEW: return launch(k_grouped_rows_few<T, TRANSPOSED>, 32, 32, NT);
+    case GROUP_128: return launch(k_grouped_rows<T, Tile<128, 128>, TRANSPOSED>, 128, 128, NT);
+    case GROUP_64: return launch(k_grouped_rows<T, Tile<64, 64>, TRANSPOSED>, 64, 64, NT);
     }
 }
-
-// How the weight gradients are formed
-struct WeightForm { bool core; int tile; int64_t chunk, slabs; };
-WeightForm weight_form(int n_cu, int64_t n_rows, int32_t n_groups, int32_t n_in, int32_t n_out, bool granules) {
-    WeightForm f;
-    f.core = granules && group_core_weights(n_rows, n_groups, n_in, n_out, n_cu);
-    f.tile = f.core ? CORE_TILE : group_few_weights(n_rows, n_groups, n_in, n_out, n_cu) ? 32 : group_weights_large(n_in, n_out) ? 128 : 64;
-    f.chunk = f.tile == 32 ? std::max<int64_t>(n_rows, 1) : group_chunk(n_rows, group_ceil(n_in, f.tile) * group_ceil(n_out, f.tile), f.core ? n_cu / 2 : 4 * n_cu);
-    f.slabs = group_slabs(n_rows, f.chunk);
-    return f;
+template <bool TRANSPOSED>
+void launch_rows(const gsplit_ctx *ctx, int32_t dtype, const RowsArgs &A, hipStream_t st) {
+    if (dtype == GSPLIT_F32) launch_rows<float, TRANSPOSED>(ctx, A, st);
+    else launch_rows<uint16_t, TRANSPOSED>(ctx, A, st);
+}
+template <class T>
+auto weights_kernel(GroupForm form) {
+    if constexpr (sizeof(T) == 2)
+        if (form == GROUP_CORE) return k_grouped_weights_core;
+    return form == GROUP_FEW ? k_grouped_weights_few<T> : form == GROUP_128 ? k_grouped_weights<T, Tile<128, 128>> : k_grouped_weights<T, Tile<64, 64>>;
 }
 
 }  // namespace
@@ -713,10 +700,7 @@ extern "C" int64_t gsplit_grouped_linear_work(gsplit_ctx *ctx, const gsplit_grou
     if (const char *e = op_check_grouped(c, n_rows)) {
         try { return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_work: ") + e); } catch (...) { return GSPLIT_ENOMEM; }
     }
-    // (of the form that needs more: which one it is depends on addresses too)
-    const bool granules = c->dtype == GSPLIT_BF16 && c->n_in % 8 == 0 && c->n_out % 8 == 0;
-    const int64_t slabs = std::max(weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out, granules).slabs,
-                                   weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out, false).slabs);
+    const int64_t slabs = group_most_slabs(n_rows, c->n_groups, c->n_in, c->n_out, c->dtype == GSPLIT_F32, ctx->n_cu);
     return slabs * ((int64_t)c->n_in + 1) * c->n_out * (int64_t)sizeof(float);
 }
 
@@ -729,10 +713,10 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
     return gs_call(ctx, st, [&] {
         const char *e = op_check_grouped_bwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_dy, dy_stride, d_dx, dx_stride, d_dw,
                                              d_dbias, d_work);
-        WeightForm f{};
+        GroupWeights f{};
         if (!e && d_dw) {
-            f = weight_form(ctx->n_cu, n_rows, c->n_groups, c->n_in, c->n_out,
-                            c->dtype == GSPLIT_BF16 && in_granules({d_x, d_dy, d_dw, d_dbias}, {c->n_in, c->n_out, x_stride, dy_stride}));
+            f = group_weights_form(n_rows, c->n_groups, c->n_in, c->n_out, c->dtype == GSPLIT_F32,
+                                   in_granules({d_x, d_dy, d_dw, d_dbias}, {c->n_in, c->n_out, x_stride, dy_stride}), ctx->n_cu);
             if (f.slabs && !d_work) e = "NULL d_work";
         }
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_bwd: ") + e);
@@ -749,11 +733,8 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
             const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));
             {
                 GsTimeScope ts(ctx, "grouped_dw", -1, st);
-                const auto kernel = f.core ? k_grouped_weights_core
-                                    : f.tile == 32 ? c->dtype == GSPLIT_F32 ? k_grouped_weights_few<float> : k_grouped_weights_few<uint16_t>
-                                    : c->dtype == GSPLIT_F32 ? f.tile == 128 ? k_grouped_weights<float, Tile<128, 128>> : k_grouped_weights<float, Tile<64, 64>>
-                                    : f.tile == 128 ? k_grouped_weights<uint16_t, Tile<128, 128>> : k_grouped_weights<uint16_t, Tile<64, 64>>;
-                hipLaunchKernelGGL(kernel, grid, dim3(f.core ? CT : NT), 0, st, A);
+                hipLaunchKernelGGL(c->dtype == GSPLIT_F32 ? weights_kernel<float>(f.form) : weights_kernel<uint16_t>(f.form), grid,
+                                   dim3(f.form == GROUP_CORE ? CT : NT), 0, st, A);
             }
             if (f.slabs) {
                 GsTimeScope ts(ctx, "grouped_dw_sum", -1, st);

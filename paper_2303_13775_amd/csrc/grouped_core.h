@@ -152,7 +152,7 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         Spot s;
         if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
         const bool whole = s.chunks == 1;
-        if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
+        if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * T, n0 = s.side % A.tiles_n * T;
         // a lane holds the number of a row of the next stage
         int next = 0;

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights_few(WeightArgs A) {
         Spot s;
         if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
         const bool whole = s.chunks == 1;
-        if (!whole && s.slab >= A.slabs) continue;          // (offsets that make no sense)
+        if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * 32, n0 = s.side % A.tiles_n * 32;
         const T *const x = (const T *)A.x + min(m0 + l32, A.K - 1), *const dy = (const T *)A.dy + min(n0 + l32, A.N - 1);
         const auto row = [&](int k) { return max(A.list.at(s.first + k), 0); };

@@ -146,18 +146,25 @@ def test_products(ctx, rows, groups, n_in, n_out, dtype, kw):
     _case(ctx, rows, groups, n_in, n_out, dtype, **kw)
 
 
-@pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows, groups, n_in, n_out, kw", [
+LARGE = [
     (9000, 3, 512, 512, dict(skew=1.0)), (20_011, 24, 300, 261, dict(skew=1.0, left_out=0.05, pad=7)), (3000, 1, 1000, 1021, dict(offset=3)),
-    (40_000, 2, 64, 16, dict(skew=2.0)), (2500, 9, 640, 520, dict(empty=(0, 4, 8))), (70_000, 300, 24, 40, dict(listed=False))])
+    (40_000, 2, 64, 16, dict(skew=2.0)), (2500, 9, 640, 520, dict(empty=(0, 4, 8))), (70_000, 300, 24, 40, dict(listed=False)),
+    (5000, 2, 100, 60, dict()), (6000, 512, 300, 129, dict(pad=3)), (250, 300, 96, 100, dict())]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows, groups, n_in, n_out, kw", LARGE)
 def test_large_products(ctx, rows, groups, n_in, n_out, kw, dtype):
     _case(ctx, rows, groups, n_in, n_out, dtype, **kw)
 
 
 # bfloat16 rows of whole granules, enough for the large tiles: edges of the rows, of the contraction, of the columns; groups of a few rows
-@pytest.mark.parametrize("rows, groups, n_in, n_out, kw", [
+LARGE_TILES = [
     (17_000, 5, 264, 520, dict(skew=1.0, left_out=0.1, pad=8, offset=8)), (33_000, 1, 128, 1000, dict(listed=False)), (20_000, 300, 512, 256, dict(skew=2.0)),
-    (35_000, 40, 136, 1288, dict(skew=1.0, pad=16, bias=False)), (16_500, 2, 1000, 504, dict(empty=(0,))), (40_000, 7, 392, 128, dict(left_out=0.5))])
+    (35_000, 40, 136, 1288, dict(skew=1.0, pad=16, bias=False)), (16_500, 2, 1000, 504, dict(empty=(0,))), (40_000, 7, 392, 136, dict(left_out=0.5)), (20_000, 3, 520, 128, dict(skew=2.0))]
+
+
+@pytest.mark.parametrize("rows, groups, n_in, n_out, kw", LARGE_TILES)
 def test_large_tiles(ctx, rows, groups, n_in, n_out, kw):
     _case(ctx, rows, groups, n_in, n_out, BF16, **kw)
 

@@ -30,6 +30,13 @@ extern "C" void runs(int64_t n, int32_t G, int64_t counters, int n_cu, int64_t *
 }
 extern "C" int64_t chunk(int64_t n, int64_t tiles, int n_cu) { return group_chunk(n, tiles, n_cu); }
 extern "C" int64_t slabs(int64_t n, int64_t chunk) { return group_slabs(n, chunk); }
+extern "C" int rows_form(int64_t n, int32_t G, int64_t k, int64_t w, int is_float, int transposed, int granules) {
+    return group_rows_form(n, G, k, w, is_float, transposed, granules, 256);
+}
+extern "C" void weights_form(int64_t n, int32_t G, int64_t k, int64_t w, int is_float, int granules, int64_t *out) {
+    const GroupWeights f = group_weights_form(n, G, k, w, is_float, granules, 256);
+    out[0] = f.form; out[1] = f.tile; out[2] = f.chunk; out[3] = f.slabs; out[4] = group_most_slabs(n, G, k, w, is_float, 256);
+}
 extern "C" int64_t row_tiles(int64_t n, int32_t G, int32_t rows) { return group_row_tiles(n, G, rows); }
 """
 
@@ -51,6 +58,8 @@ def _lib():
     L.fwd.argtypes = [cfg, vp, i64, i64, vp, vp, vp, vp, vp, i64]
     L.bwd.argtypes = [cfg, vp, i64, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp]
     L.runs.argtypes = [i64, i32, i64, C.c_int, C.POINTER(i64)]
+    L.rows_form.argtypes = [i64, i32, i64, i64, C.c_int, C.c_int, C.c_int]
+    L.weights_form.argtypes = [i64, i32, i64, i64, C.c_int, C.c_int, C.POINTER(i64)]
     for f, a in ((L.chunk, [i64, i64, C.c_int]), (L.slabs, [i64, i64]), (L.row_tiles, [i64, i32, i32])):
         f.argtypes, f.restype = a, i64
     return L
@@ -131,3 +140,44 @@ def test_chunks_and_slabs_cover_any_groups():
         assert sum(c > 1 for c in chunks) <= n // chunk
         for rows in (64, 128):
             assert sum(-(-s // rows) for s in sizes) <= _lib().row_tiles(n, G, rows)
+
+
+CORE, FEW, T128, T64 = range(4)
+
+
+def _forms(rows, groups, n_in, n_out, is_float, granules):
+    out = (C.c_int64 * 5)()
+    _lib().weights_form(rows, groups, n_in, n_out, is_float, granules, out)
+    f = _lib().rows_form
+    return f(rows, groups, n_in, n_out, is_float, 0, granules), f(rows, groups, n_out, n_in, is_float, 1, granules), list(out)
+
+
+def test_gpu_tests_reach_every_form():
+    import test_gpu_grouped as T
+    small = [(*shape, kw) for shape in T.SHAPES for kw in (dict(), dict(pad=1, offset=1), dict(pad=8))]
+    reached = {True: [set(), set(), set()], False: [set(), set(), set()]}
+    for cases, types in ((small + T.LARGE, (True, False)), (T.LARGE_TILES, (False,))):
+        for rows, groups, n_in, n_out, kw in cases:
+            for is_float in types:
+                granules = not is_float and all(x % 8 == 0 for x in (n_in, n_out, kw.get("pad", 0), kw.get("offset", 0)))
+                y, dx, w = _forms(rows, groups, n_in, n_out, is_float, granules)
+                reached[is_float][0].add(y)
+                reached[is_float][1].add(dx)
+                reached[is_float][2].add((w[0], w[3] > 0))
+    assert reached[True][:2] == [{FEW, T128, T64}] * 2 and reached[False][:2] == [{CORE, FEW, T128, T64}] * 2
+    assert reached[True][2] >= {(FEW, False), (T64, False), (T64, True), (T128, True)}
+    assert reached[False][2] >= {(FEW, False), (T64, False), (T64, True), (T128, True), (CORE, True)}
+
+
+def test_working_memory_serves_every_form():
+    import random
+    rng = random.Random(4)
+    for _ in range(3000):
+        n, G = rng.choice([0, 1, 300, 4096, 4097, 20_000, 10 ** 6]), rng.choice([1, 3, 64, 512])
+        k, w = (rng.choice([1, 8, 47, 64, 65, 128, 256, 1000, 2048, 5000]) for _ in range(2))
+        for is_float in (True, False):
+            for granules in (True, False):
+                if granules and (k % 8 or w % 8 or is_float):
+                    continue
+                form, tile, chunk, slabs, most = _forms(n, G, k, w, is_float, granules)[2]
+                assert slabs <= most and chunk >= 1 and tile == {CORE: 256, FEW: 32, T128: 128, T64: 64}[form]
