@@ -4,6 +4,12 @@
 // number of lanes in front of it in its own group, and one lane adds to a counter for all of them (as many atomics as rows would
 // meet at few addresses).  Small calls are one workgroup's, larger ones two launches: the counters of every workgroup's rows, and
 // the places, for which each workgroup adds up the counters of those in front of it.
+//
+// Latency bounds it: 8 MB are 1.6 us of a 5.05 TB/s copy, a million rows of 64 groups take 4.0 + 10.0 us, 1024 rows of 4 groups 3.7 in one
+// launch.  The groups of a wave's first 256 rows and their matches stay in registers over both of its passes, the counters come
+// eight loads at a time (one after the other, and rows read again: 14.4 us).  No faster: rows put in order in LDS so that threads
+// side by side write side by side (11.2), two workgroups a compute unit (5.2 + 15.8, twice the counters for everybody), one every
+// two (5.9 + 12.0), sixteen loads at a time (10.2).
 #include "group_rules.h"
 #include "gsplit_internal.h"
 #include "op_checks.h"
@@ -20,30 +26,42 @@ struct Rows {
     int32_t *ptr, *rows, *count;        // count [workgroups x G]
 };
 
-// the rows lo .. hi - 1 of a wave, 64 a round: f(first row of the round, group or -1, lanes of the same group)
-template <class F>
-__device__ __forceinline__ void rounds(const Rows &R, int64_t lo, int64_t hi, F &&f) {
+// DEEP rounds of 64 rows of a wave: every lane's group (-1: none) and the lanes of the same group
+constexpr int DEEP = 4;
+struct Rounds { int32_t g[DEEP]; uint64_t same[DEEP]; };
+__device__ __forceinline__ void load_rounds(const Rows &R, int64_t at, int64_t hi, Rounds &v) {
     const int lane = threadIdx.x & 63;
-    constexpr int DEEP = 4;
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) v.g[d] = -1;
+    if (at >= hi) return;                       // (nothing can be read where there are no rows)
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) {
+        const int64_t r = at + 64 * d + lane;
+        v.g[d] = R.group[min(r, R.n - 1)];
+        if (r >= hi || (uint32_t)v.g[d] >= (uint32_t)R.G) v.g[d] = -1;
+    }
+}
+__device__ __forceinline__ void match_rounds(const Rows &R, Rounds &v) {
+#pragma unroll
+    for (int d = 0; d < DEEP; ++d) v.same[d] = __ballot(v.g[d] >= 0);
+    for (int b = 0; b < R.bits; ++b)
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            const uint64_t set = __ballot(v.g[d] >> b & 1);
+            v.same[d] &= v.g[d] >> b & 1 ? set : ~set;
+        }
+}
+// the rows lo .. hi - 1 of a wave, of which the first rounds are there: f(first row of the round, group, lanes of the same group)
+template <class F>
+__device__ __forceinline__ void rounds(const Rows &R, int64_t lo, int64_t hi, const Rounds &first, F &&f) {
+    Rounds v = first;
     for (int64_t at = lo; at < hi; at += 64 * DEEP) {
-        int32_t g[DEEP];
-#pragma unroll
-        for (int d = 0; d < DEEP; ++d) {
-            const int64_t r = at + 64 * d + lane;
-            g[d] = R.group[min(r, R.n - 1)];
-            if (r >= hi || (uint32_t)g[d] >= (uint32_t)R.G) g[d] = -1;
+        if (at > lo) {
+            load_rounds(R, at, hi, v);
+            match_rounds(R, v);
         }
 #pragma unroll
-        for (int d = 0; d < DEEP; ++d) {
-            if (at + 64 * d >= hi) break;
-            uint64_t same = __ballot(g[d] >= 0);
-            for (int b = 0; b < R.bits; ++b) {
-                const bool bit = g[d] >> b & 1;
-                const uint64_t set = __ballot(bit);
-                same &= bit ? set : ~set;
-            }
-            f(at + 64 * d, g[d], same);
-        }
+        for (int d = 0; d < DEEP; ++d) f(at + 64 * d, v.g[d], v.same[d]);
     }
 }
 __device__ __forceinline__ int before_me(uint64_t same) {
@@ -57,11 +75,14 @@ __device__ __forceinline__ void run_of(const Rows &R, int64_t &lo, int64_t &hi) 
 
 __global__ __launch_bounds__(GT) void k_group_count(Rows R) {
     extern __shared__ int32_t s_count[];       // [G]
-    for (int g = threadIdx.x; g < R.G; g += GT) s_count[g] = 0;
-    __syncthreads();
     int64_t lo, hi;
     run_of(R, lo, hi);
-    rounds(R, lo, hi, [&](int64_t, int32_t g, uint64_t same) {
+    Rounds first;
+    load_rounds(R, lo, hi, first);
+    for (int g = threadIdx.x; g < R.G; g += GT) s_count[g] = 0;
+    __syncthreads();
+    match_rounds(R, first);
+    rounds(R, lo, hi, first, [&](int64_t, int32_t g, uint64_t same) {
         if (g >= 0 && before_me(same) == 0) atomicAdd(&s_count[g], __popcll(same));
     });
     __syncthreads();
@@ -90,16 +111,25 @@ __global__ __launch_bounds__(GT) void k_group_place(Rows R) {
     __shared__ int32_t s_wave[GROUP_WAVES];
     int32_t *s_next = lds, *s_part = lds + GROUP_WAVES * R.G;
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    int64_t lo, hi;
+    run_of(R, lo, hi);
+    Rounds first;
+    load_rounds(R, lo, hi, first);
     for (int i = t; i < GROUP_WAVES * R.G; i += GT) s_next[i] = 0;
     int32_t in_front = 0, all = 0;              // rows of group t in the workgroups in front; in all
     if (!WHOLE) {
         const int parts = GT / R.G;             // threads that share a group's counters
         const int g = t % R.G, part = t / R.G;
         if (part < parts)
-            for (int b = part; b < (int)gridDim.x; b += parts) {
-                const int32_t c = R.count[(int64_t)b * R.G + g];
-                all += c;
-                in_front += b < (int)blockIdx.x ? c : 0;
+            for (int b = part; b < (int)gridDim.x; b += 8 * parts) {
+                int32_t c[8];                   // (eight loads in flight)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) c[u] = R.count[(int64_t)min(b + u * parts, (int)gridDim.x - 1) * R.G + g];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    all += b + u * parts < (int)gridDim.x ? c[u] : 0;
+                    in_front += b + u * parts < (int)blockIdx.x ? c[u] : 0;
+                }
             }
         s_part[t] = in_front; s_part[GT + t] = all;
         __syncthreads();
@@ -107,10 +137,9 @@ __global__ __launch_bounds__(GT) void k_group_place(Rows R) {
         if (t < R.G)
             for (int p = 0; p < parts; ++p) { in_front += s_part[p * R.G + t]; all += s_part[GT + p * R.G + t]; }
     }
+    match_rounds(R, first);
     __syncthreads();
-    int64_t lo, hi;
-    run_of(R, lo, hi);
-    rounds(R, lo, hi, [&](int64_t, int32_t g, uint64_t same) {
+    rounds(R, lo, hi, first, [&](int64_t, int32_t g, uint64_t same) {
         if (g >= 0 && before_me(same) == 0) s_next[wave * R.G + g] += __popcll(same);
     });
     __syncthreads();
@@ -130,7 +159,7 @@ __global__ __launch_bounds__(GT) void k_group_place(Rows R) {
         }
     }
     __syncthreads();
-    rounds(R, lo, hi, [&](int64_t at, int32_t g, uint64_t same) {
+    rounds(R, lo, hi, first, [&](int64_t at, int32_t g, uint64_t same) {
         const int before = before_me(same);
         if (g >= 0) {
             const int32_t next = s_next[wave * R.G + g];
