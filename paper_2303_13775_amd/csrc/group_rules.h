@@ -52,13 +52,17 @@ inline bool group_weights_large(int64_t n_in, int64_t n_out) { return n_in > 64 
 
 // The rows of a group are taken in chunks where one group's tiles do not fill the chip: as many chunks of all rows as give `workgroups`.
 // Short chunks even out groups of all sizes, and cost the sum over them.  Tiles of 128 and 64, four workgroups a compute unit (three, two):
-// 20011 rows of 24 groups 1000 x 1021 bf16 157 us (165, 184), float 400 (422, 489), 65536 of 8 512 x 512 float 300 (279, 349).  Tiles of 256, one
+// 20011 rows of 24 groups 1000 x 1021 bf16 157 us (165, 184), float, before chunks went in pieces, 400 (422, 489), 65536 of 8 512 x 512 float 300 (279, 349).  Tiles of 256, one
 // every two compute units (one, two): 65536 of 8 512 x 512 82 us (97, 123), 20011 of 24 1000 x 1024 115 (112, 160).
 inline int64_t group_chunk(int64_t n_rows, int64_t tiles_of_a_group, int64_t workgroups) {
     const int64_t want = group_ceil(workgroups, tiles_of_a_group);
     if (want <= 1) return std::max<int64_t>(n_rows, 1);
     return std::max<int64_t>(256, group_ceil(group_ceil(n_rows, want), 64) * 64);
 }
+// Pieces of a chunk's tiles, which go to the XCDs in turn: more of them are dealt more evenly and share less in an XCD's L2 (whole chunks,
+// 2, 4, 8 pieces: 65536 rows of 64 groups 2048 x 2048 bf16 1360, 1010, 962, 1055 us; 20011 of 24 1000 x 1024 113, 102, 103, 105, float
+// 1000 x 1021 388, 365, 341, 353; 65536 of 8 512 x 512 float 294, 294, 260, 274).
+inline int group_pieces(int64_t tiles) { return tiles >= 16 ? 4 : 1; }
 // slabs: the chunks of those groups that have more than one
 inline int64_t group_slabs(int64_t n_rows, int64_t chunk) { return n_rows > chunk ? 2 * (n_rows / chunk) : 0; }
 

@@ -305,7 +305,7 @@ struct Sums {
 // inside 0 .. n_rows.
 struct Spot { int g, first, rows, chunks, slab, side; };
 template <bool EMPTY_TOO>
-__device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G, int n_rows, int per, int64_t block, int64_t across, Spot &s) {
+__device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G, int n_rows, int per, int64_t block, int64_t across, Spot &s, int pieces = 1) {
     const int lane = threadIdx.x & 63;
     int lo, hi, tiles, sum, own_slabs, slabs;
     const auto scan = [&](int base) __attribute__((always_inline)) {
@@ -330,11 +330,12 @@ __device__ __forceinline__ bool find_spot(const int32_t *__restrict__ ptr, int G
     // L2, an eighth of the tiles there are each (not of those there may be, or the last XCDs have less to do)
     int j, slab = 0;
     if (EMPTY_TOO && all >= 16) {
-        // (chunks of rows are of all lengths, and the long ones lie side by side: each in turn to another XCD)
-        const int q = (int)((block >> 3) / across);
-        j = q * 8 + (int)(block & 7);
-        s.side = (int)((block >> 3) - q * across);
-        if (j >= all) return false;
+        // (chunks of rows are of all lengths, and the long ones lie side by side: pieces of their tiles, each in turn to another XCD)
+        const int each = (int)((across + pieces - 1) / pieces), q = (int)((block >> 3) / each);
+        const int64_t piece = (int64_t)q * 8 + (block & 7);
+        j = (int)(piece / pieces);
+        s.side = (int)(piece - (int64_t)j * pieces) * each + (int)((block >> 3) - (int64_t)q * each);
+        if (j >= all || s.side >= across) return false;
     } else {
         const int64_t total = all * across, each = (total + 7) / 8, x = (block & 7) * each + (block >> 3);
         if (block >> 3 >= each || x >= total) return false;
@@ -470,7 +471,8 @@ struct WeightArgs {
     const int32_t *ptr;
     RowList list;
     int32_t per;                // rows of a chunk
-    int64_t items;              // chunks, at most (a multiple of 8)
+    int64_t room;               // workgroups that have a piece of a chunk's tiles, at most
+    int32_t pieces;
     int32_t tiles_m, tiles_n;
     float *dw, *db;
     float *slab;                // [slabs x (K + 1) x N]: the chunks' gradients of W, then of b
@@ -484,10 +486,10 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights(WeightArgs A) {
     __shared__ __attribute__((aligned(16))) uint4 s_a[P * BM * KG], s_b[P * BN * KG];
     __shared__ double s_sum[KG][BN];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
-    for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n;
+    for (int64_t block = blockIdx.x; block < A.room; block += gridDim.x) {
         Spot s;
-        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
+        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s, A.pieces)) continue;
         const bool whole = s.chunks == 1;
         if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * BM, n0 = s.side % A.tiles_n * BN;
@@ -727,10 +729,12 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
                                                       c->n_groups, d_group_ptr, list, 0, 0}, st);
         }
         if (d_dw) {
+            const int64_t tiles_m = group_ceil(c->n_in, f.tile), tiles_n = group_ceil(c->n_out, f.tile);
+            const int pieces = group_pieces(tiles_m * tiles_n);
+            const int64_t chunks = group_ceil(n_rows / f.chunk + c->n_groups, 8) * 8;          // (at most)
             WeightArgs A{d_x, d_dy, (uint32_t)x_stride, (uint32_t)dy_stride, c->n_in, c->n_out, c->n_groups, d_group_ptr, list, (int32_t)f.chunk,
-                         group_ceil(n_rows / f.chunk + c->n_groups, 8) * 8, (int32_t)group_ceil(c->n_in, f.tile), (int32_t)group_ceil(c->n_out, f.tile), d_dw, d_dbias,
-                         (float *)d_work, f.slabs};
-            const dim3 grid(blocks(A.items * A.tiles_m * A.tiles_n));
+                         chunks * pieces * group_ceil(tiles_m * tiles_n, pieces), pieces, (int32_t)tiles_m, (int32_t)tiles_n, d_dw, d_dbias, (float *)d_work, f.slabs};
+            const dim3 grid(blocks(A.room));
             {
                 GsTimeScope ts(ctx, "grouped_dw", -1, st);
                 hipLaunchKernelGGL(c->dtype == GSPLIT_F32 ? weights_kernel<float>(f.form) : weights_kernel<uint16_t>(f.form), grid,

@@ -147,10 +147,10 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
     constexpr int T = CORE_TILE;
     __shared__ __attribute__((aligned(16))) core_u32x4 lds[2][2 * CORE_HALF];
     const int lane = threadIdx.x & 63, wave = core_wave(), half = lane >> 5, l32 = lane & 31, wm = core_wm(), wn = core_wn();
-    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
-    for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n;
+    for (int64_t block = blockIdx.x; block < A.room; block += gridDim.x) {
         Spot s;
-        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
+        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s, A.pieces)) continue;
         const bool whole = s.chunks == 1;
         if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * T, n0 = s.side % A.tiles_n * T;

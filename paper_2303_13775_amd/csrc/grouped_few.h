@@ -141,10 +141,10 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_weights_few(WeightArgs A) {
     __shared__ float lds[4][16][64];
     __shared__ double s_sum[4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5, l32 = lane & 31;
-    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n, room = (A.items * tiles + 7) / 8 * 8;
-    for (int64_t block = blockIdx.x; block < room; block += gridDim.x) {
+    const int64_t tiles = (int64_t)A.tiles_m * A.tiles_n;
+    for (int64_t block = blockIdx.x; block < A.room; block += gridDim.x) {
         Spot s;
-        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s)) continue;
+        if (!find_spot<true>(A.ptr, A.G, A.list.n, A.per, block, tiles, s, A.pieces)) continue;
         const bool whole = s.chunks == 1;
         if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * 32, n0 = s.side % A.tiles_n * 32;

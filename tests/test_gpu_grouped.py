@@ -169,6 +169,13 @@ def test_large_tiles(ctx, rows, groups, n_in, n_out, kw):
     _case(ctx, rows, groups, n_in, n_out, BF16, **kw)
 
 
+# Weight gradients whose chunks are dealt in pieces: tiles that no piece divides (17 of 64, 25 of 64 and of 128, 18 of 256), groups of no rows among them
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows, groups, n_in, n_out", [(3000, 30, 17 * 64, 40), (2500, 20, 300, 310), (1500, 17, 600, 580), (9000, 40, 264, 9 * 256)])
+def test_chunks_in_pieces(ctx, rows, groups, n_in, n_out, dtype):
+    _case(ctx, rows, groups, n_in, n_out, dtype, skew=1.0, left_out=0.1, empty=(0, 9, groups - 1))
+
+
 @pytest.mark.parametrize("bad", [np.inf, np.nan])
 def test_large_tiles_keep_values_that_are_not_finite_where_they_belong(ctx, bad):
     rows, n_in, n_out = 17_000, 264, 520
