@@ -643,7 +643,7 @@ GSPLIT_API int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
  * 2.0315) do not converge but bring values from 0.01 on into 0.7 .. 1.2 within five steps; 1.875, -1.25, 0.375 converge.  A matrix
  * of zeros gives zeros (where |G| + eps is 0, X is 0); one with a value that is not finite gives NaN throughout.  d_in and d_out are
  * dense [count x rows x cols], each float or bfloat16; d_out may be d_in if their types are the same.  The
- * products' factors are held in two halves (24 bits) and summed in float; results of bfloat16 are rounded once.  The same bits on every call.
+ * products' factors are held in two halves (22 bits and a sign) and summed in float; results of bfloat16 are rounded once.  The same bits on every call.
  * Coefficients have to keep singular values from 0 to 1 below 2, and |a + b s^2 + c s^4| below 15, in every step.
  * d_work: 16-byte aligned working memory of gsplit_orthogonalize_work() bytes, which depends on the sizes alone; one call uses
  * it at a time.  What a call writes may overlap nothing else of it.  The HOST arrays are read during the call.  Asynchronous; may be captured at any time (the

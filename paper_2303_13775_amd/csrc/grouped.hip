@@ -6,9 +6,15 @@
 // memory with the contraction along its rows (`Along`: x and dy as rows, W of the input gradient) or across them (`Across`: W of the
 // forward product, x and dy of the weight gradient); there a thread fetches the same columns of eight rows and transposes them in
 // its registers.
-// Floats go through the bfloat16 matrix unit as three parts and six products (gemm_split.h); products of bfloat16 are exact there.
+// Floats go through the bfloat16 matrix unit as three parts and six products (split_parts.h); products of bfloat16 are exact there.
 // Sums are float.
 // The columns of the result run along the matrix unit's rows: a lane then holds four consecutive columns of one row.
+//
+// What bounds them.  Float: the six products and the splitting in front of them (60000 rows of 8 groups 512 x 512 233 us, matrix unit
+// busy for 39 %).  bfloat16 rows of whole granules have tiles of their own (grouped_core.h); at other addresses one tile's loads in
+// flight (20011 rows of 24 groups 1000 x 1021: dx 98 us, dW 146).  Few rows: latency (4096 x 256 x 172 of 16 groups 13.3; fewer, grouped_few.h).
+// Tiles of 128 x 128 where they fill the chip, else 64 x 64 (group_rules.h): a quarter of 128 x 128 is 64 registers of sums
+// a lane, and the most that leaves room for a tile in flight and two workgroups a compute unit.
 #include <algorithm>
 #include <type_traits>
 
