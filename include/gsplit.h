@@ -594,7 +594,7 @@ GSPLIT_API int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *con
  *
  * gsplit_group_rows sorts rows by their group: d_group [n_rows] int32; a row whose group lies outside
  * [0, n_groups) belongs to none.  d_group_ptr [n_groups + 1] receives where each group starts, d_rows [n_rows] the rows in that
- * order, those of a group ascending; d_rows behind d_group_ptr[n_groups] is left as it was.  n_rows < 2^31, n_groups at most
+ * order, those of a group ascending (d_rows may not be d_group); d_rows behind d_group_ptr[n_groups] is left as it was.  n_rows < 2^31, n_groups at most
  * GSPLIT_MAX_GROUPS.  EINVAL for NULL (d_group and d_rows may be NULL without rows) or misaligned pointers and sizes out of range.
  * Asynchronous; may be captured at any time; scratch memory as for the losses above. */
 #define GSPLIT_MAX_GROUPS 512

@@ -784,7 +784,7 @@ class Context:
         dev = self.device.index
         for t in (group, group_ptr, rows):
             assert t.dtype is torch.int32 and t.is_contiguous() and t.get_device() == dev
-        assert rows.numel() == group.numel()
+        assert rows.numel() == group.numel() and (group.numel() == 0 or rows.data_ptr() != group.data_ptr())
         rc = self.lib.gsplit_group_rows(self.h, group.data_ptr(), group.numel(), group_ptr.numel() - 1, group_ptr.data_ptr(),
                                         rows.data_ptr(), self._own_stream())
         if rc:
@@ -813,6 +813,7 @@ class Context:
         cfg, n, ptr, order = self._grouped(x, group_ptr, rows, w)
         xp, ldx = self._matrix(x, x, cfg.n_in)
         yp, ldy = self._matrix(y, x, cfg.n_out)
+        assert n == 0 or yp != xp           # (rows are written while others still read them)
         b, = self._vectors((bias,), cfg.n_groups * cfg.n_out)
         rc = self.lib.gsplit_grouped_linear_fwd(self.h, C.byref(cfg), xp, n, ldx, ptr, order, w.data_ptr(), b, yp, ldy, self._own_stream())
         if rc:
@@ -834,6 +835,7 @@ class Context:
         xp, ldx = self._matrix(x, x, cfg.n_in)
         dyp, lddy = self._matrix(dy, x, cfg.n_out)
         dxp, lddx = (None, 0) if dx is None else self._matrix(dx, x, cfg.n_in)
+        assert n == 0 or dxp not in (xp, dyp)
         dwp, = self._vectors((dw,), w.numel())
         dbp, = self._vectors((dbias,), cfg.n_groups * cfg.n_out)
         if dw is not None:

@@ -358,6 +358,18 @@ def test_more_than_32_bits_of_elements(ctx):
     assert int(torch.count_nonzero(y)) == 3 and y[0, 9] == 1 and y[1, 0] == 2 and y[1, -1] == 4
 
 
+def test_results_in_the_place_of_what_is_read(ctx):
+    x, w, dw = torch.ones((9, 6), device="cuda"), torch.ones((2, 6, 6), device="cuda"), torch.zeros((2, 6, 6), device="cuda")
+    dy, group, ptr = torch.ones((9, 6), device="cuda"), torch.zeros(9, dtype=torch.int32, device="cuda"), torch.tensor([0, 4, 9], dtype=torch.int32, device="cuda")
+    for call in (lambda: ctx.gsplit_group_rows(group, ptr, group), lambda: ctx.gsplit_grouped_linear_fwd(x, ptr, None, w, None, x),
+                 lambda: ctx.gsplit_grouped_linear_bwd(x, ptr, None, w, dy, x, dw, None), lambda: ctx.gsplit_grouped_linear_bwd(x, ptr, None, w, dy, dy, None, None)):
+        with pytest.raises(AssertionError):
+            call()
+    both = torch.ones((9, 12), device="cuda")           # columns of one buffer side by side are apart
+    ctx.gsplit_grouped_linear_fwd(both[:, :6], ptr, None, w, None, both[:, 6:])
+    assert bool((both[:, :6] == 1).all()) and bool((both[:, 6:] == 6).all())
+
+
 def test_refusals(ctx):
     from paper_2303_13775_amd import GsplitError
     i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")

@@ -183,6 +183,28 @@ def test_rank_one_and_repeated_rows(ctx):
     _close("rank", out, *_expected(g.double()))
 
 
+def test_a_matrix_of_more_than_32_bits_of_elements(ctx):
+    """A tall matrix with one value a column, no two in a row: every singular value is 1 / sqrt(columns), and a step is the polynomial of
+    one number.  A sum has one product that is not 0, so an element is off by the roundings of what is held: X, A (twice in its
+    square) and B, 2^-22 each, under 8 of them a step, which the
+    steps pass on with factors of at most 1 and, the last one (0.88 to 0.85), 1.61."""
+    from paper_2303_13775_amd import MatrixTensors
+    rows, cols = 60_001, 20_001
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    of = torch.randperm(rows, device="cuda", generator=gen)[:cols]
+    of[cols - 1] = torch.where((of == rows - 1).any(), of[cols - 1], rows - 1)
+    g = torch.zeros((rows, cols), device="cuda")
+    g[of, torch.arange(cols, device="cuda")] = 1e-3
+    out = torch.full_like(g, 7.0)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), eps=0.0)
+    s = 1 / math.sqrt(cols)
+    for _ in range(5):
+        s *= ABC[0] + s * s * (ABC[1] + s * s * ABC[2])
+    got = out[of, torch.arange(cols, device="cuda")].double()
+    assert float((got - s).abs().max()) <= 1.61 * 5 * 8 * 2.0**-22 * s
+    assert int(torch.count_nonzero(out)) == cols
+
+
 def _types(kind, n):
     return [F32] * n if kind == "f32" else [BF16] * n if kind == "bf16" else [(F32, BF16)[i % 2] for i in range(n)]
 
