@@ -68,12 +68,16 @@ inline int group_pieces(int64_t tiles) { return tiles >= 16 ? 4 : 1; }
 // slabs: the chunks of those groups that have more than one
 inline int64_t group_slabs(int64_t n_rows, int64_t chunk) { return n_rows > chunk ? 2 * (n_rows / chunk) : 0; }
 
-// Which kernel forms y or dx [n_rows x n] of a contraction of k, and which the weight gradients; granules: rows of whole 16 bytes
+// Which kernel forms y or dx [n_rows x n] of a contraction of k, and which the weight gradients; granules: rows of whole 16 bytes.  (The tiles
+// through registers fetch eight elements of a row at once.)
+// Tiles of 128 where they fill the chip and are not mostly empty columns (us forward, 128 / 64: 65536 rows of 8 groups float 100 x 64 37 / 20,
+// 256 x 100 56 / 51, 256 x 172 83 / 74, 100 x 256 57 / 56, 32768 of 16 512 x 300 102 / 108, 60000 of 8 512 x 511 228 / 289; bf16 100 x 64 15.5 / 11.0,
+// 256 x 172 31 / 28, 512 x 300 32 / 35, 512 x 511 78 / 102; dx of 256 x 100 float 49 / 56).
 enum GroupForm { GROUP_CORE, GROUP_FEW, GROUP_128, GROUP_64 };
 inline GroupForm group_rows_form(int64_t n_rows, int n_groups, int64_t k, int64_t n, bool is_float, bool transposed, bool granules, int n_cu) {
     if (!is_float && granules && group_core_rows(n_rows, n_groups, k, n, n_cu)) return GROUP_CORE;
-    if (group_few_rows(n_rows, n_groups, n, is_float, transposed, n_cu)) return GROUP_FEW;
-    return group_row_tiles(n_rows, n_groups, 128) * group_ceil(n, 128) >= n_cu ? GROUP_128 : GROUP_64;
+    if (k < 8 || group_few_rows(n_rows, n_groups, n, is_float, transposed, n_cu)) return GROUP_FEW;
+    return n > 192 && group_row_tiles(n_rows, n_groups, 128) * group_ceil(n, 128) >= n_cu ? GROUP_128 : GROUP_64;
 }
 struct GroupWeights { GroupForm form; int tile; int64_t chunk, slabs; };
 inline GroupWeights group_weights_form(int64_t n_rows, int n_groups, int64_t n_in, int64_t n_out, bool is_float, bool granules, int n_cu) {

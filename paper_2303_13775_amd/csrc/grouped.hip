@@ -83,36 +83,53 @@ struct Along {
 #pragma unroll
         for (int i = 0; i < N; ++i) p[i] = row(((int)threadIdx.x + i * NT) / KG);
     }
+    // No branch: where it meets the other way again, what is in flight would be waited for.  Past the row's end: its last eight (float: four)
+    // elements once more, from which `cut` takes what there is.
     __device__ __forceinline__ void load(int t) {
         const int g = threadIdx.x % KG, k0 = t * KT;
-        if (k0 + KT <= K) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (sizeof(T) == 4) {
-                    const u32x4 a = *(const u32x4_any *)(p[i] + k0 + 4 * g), b = *(const u32x4_any *)(p[i] + k0 + 16 + 4 * g);
+        for (int i = 0; i < N; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                const u32x4 a = *(const u32x4_any *)(p[i] + min(k0 + 4 * g, K - 4)), b = *(const u32x4_any *)(p[i] + min(k0 + 16 + 4 * g, K - 4));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) { r[i][j] = __uint_as_float(a[j]); r[i][4 + j] = __uint_as_float(b[j]); }
-                } else {
-                    const u32x4 a = *(const u32x4_any *)(p[i] + k0 + 8 * g);
-                    r[i] = make_uint4(a[0], a[1], a[2], a[3]);
-                }
+                for (int j = 0; j < 4; ++j) { r[i][j] = __uint_as_float(a[j]); r[i][4 + j] = __uint_as_float(b[j]); }
+            } else {
+                const u32x4 a = *(const u32x4_any *)(p[i] + min(k0 + 8 * g, K - 8));
+                r[i] = make_uint4(a[0], a[1], a[2], a[3]);
             }
-        } else {            // the last tile: element by element, zeros past the end
+        }
+    }
+    // zeros past the end of the contraction, in its tile t
+    __device__ __forceinline__ void cut(int t) {
+        if ((t + 1) * KT <= K) return;
+        const int g = threadIdx.x % KG, k0 = t * KT;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int h = 0; h < 8; h += 4) {
+                const int past = max(k0 + 4 * h + 4 * g - (K - 4), 0);         // elements in front of the first that is wanted
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int q = j; q < 4; ++q) v = q == j + past ? r[i][h + q] : v;
+                        r[i][h + j] = v;
+                    }
+            }
+        } else {
+            const int past = max(k0 + 8 * g - (K - 8), 0);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                T v[8];
+                const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+                uint32_t v[5] = {};
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = p[i][min(k0 + Kind<T>::k_of(g, j), K - 1)];
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (k0 + Kind<T>::k_of(g, j) >= K) v[j] = 0;
-                if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) r[i][j] = v[j];
-                } else {
-                    r[i] = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
-                                      v[6] | (uint32_t)v[7] << 16);
-                }
+                    for (int q = j; q < 4; ++q) v[j] = q == j + past / 2 ? w[q] : v[j];
+                const uint32_t by = past & 1 ? 16 : 0;
+                r[i] = make_uint4(__builtin_amdgcn_alignbit(v[1], v[0], by), __builtin_amdgcn_alignbit(v[2], v[1], by),
+                                  __builtin_amdgcn_alignbit(v[3], v[2], by), __builtin_amdgcn_alignbit(v[4], v[3], by));
             }
         }
     }
@@ -146,7 +163,7 @@ struct Across {
     // from row(j), the row of the granule's contraction index j.  (No branch around a single load: each would wait for the one before.)
     template <class Row>
     __device__ __forceinline__ void load(const Row &row) {
-        if (W > 1 && cols < W) {
+        if (ROWS == 64 && W > 1 && cols < W) {         // (tiles of 128 are for more than 64 columns)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const T *p = row(j);
@@ -445,7 +462,9 @@ __global__ __launch_bounds__(NT, 2) void k_grouped_rows(RowsArgs A) {
         const int KT = (A.K + Kind<T>::KT - 1) / Kind<T>::KT;
         load(0);
         for (int t = 0; t < KT; ++t) {
-            if constexpr (!TRANSPOSED) lb.cut(t, A.K);
+            la.cut(t);
+            if constexpr (TRANSPOSED) lb.cut(t);
+            else lb.cut(t, A.K);
             la.store(s_a);
             lb.store(s_b);
             __syncthreads();

@@ -176,6 +176,14 @@ def test_chunks_in_pieces(ctx, rows, groups, n_in, n_out, dtype):
     _case(ctx, rows, groups, n_in, n_out, dtype, skew=1.0, left_out=0.1, empty=(0, 9, groups - 1))
 
 
+# Contractions that end inside a granule, short of one, and rows whose last is the buffer's last: what lies past a row's end is its neighbour's
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows, groups", [(300, 2), (9000, 5), (40_000, 3)])
+@pytest.mark.parametrize("n_in, n_out", [(7, 9), (8, 200), (9, 17), (11, 15), (31, 33), (41, 71), (63, 65), (66, 201), (69, 130), (76, 8), (127, 257)])
+def test_contractions_that_end_anywhere(ctx, rows, groups, n_in, n_out, dtype):
+    _case(ctx, rows, groups, n_in, n_out, dtype, skew=0.5)
+
+
 @pytest.mark.parametrize("bad", [np.inf, np.nan])
 def test_large_tiles_keep_values_that_are_not_finite_where_they_belong(ctx, bad):
     rows, n_in, n_out = 17_000, 264, 520
