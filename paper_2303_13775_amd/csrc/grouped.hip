@@ -10,9 +10,9 @@
 // Sums are float.
 // The columns of the result run along the matrix unit's rows: a lane then holds four consecutive columns of one row.
 //
-// What bounds them.  Float: the six products and the splitting in front of them (60000 rows of 8 groups 512 x 512 233 us, matrix unit
-// busy for 39 %).  bfloat16 rows of whole granules have tiles of their own (grouped_core.h); at other addresses one tile's loads in
-// flight (20011 rows of 24 groups 1000 x 1021: dx 98 us, dW 146).  Few rows: latency (4096 x 256 x 172 of 16 groups 13.3; fewer, grouped_few.h).
+// What bounds them.  Float: the six products and the splitting in front of them (60000 rows of 8 groups 512 x 512 219 us, matrix unit
+// busy for 41 %).  bfloat16 rows of whole granules have tiles of their own (grouped_core.h); at other addresses one tile's loads in
+// flight (20011 rows of 24 groups 1000 x 1021: dx 95 us, dW 150).  Few rows: latency (4096 x 256 x 172 of 16 groups 12.8; fewer, grouped_few.h).
 // Tiles of 128 x 128 where they fill the chip, else 64 x 64 (group_rules.h): a quarter of 128 x 128 is 64 registers of sums
 // a lane, and the most that leaves room for a tile in flight and two workgroups a compute unit.
 #include <algorithm>
@@ -163,7 +163,9 @@ struct Across {
     // from row(j), the row of the granule's contraction index j.  (No branch around a single load: each would wait for the one before.)
     template <class Row>
     __device__ __forceinline__ void load(const Row &row) {
-        if (ROWS == 64 && W > 1 && cols < W) {         // (tiles of 128 are for more than 64 columns)
+        // (tiles of 128 are for more columns, but without this way the weight gradients' take 256 registers, not 239, and 166 us, not 159: 20011 rows of 24
+        // groups 1000 x 1021 bf16)
+        if ((ROWS == 64 || THREADS < NT) && W > 1 && cols < W) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const T *p = row(j);

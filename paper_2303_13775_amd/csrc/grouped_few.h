@@ -1,7 +1,7 @@
 // The grouped products of few rows (included by grouped.hip inside its anonymous namespace): latency is all of them, and a tile's loop of
 // fetch, barrier and multiplication is a chain of round trips to memory.  Here a workgroup forms 32 x 32 of the result; its four waves
 // take every fourth step of 16 of the contraction, four steps ahead and straight into registers, without a barrier, and their sums
-// meet in LDS, added in a fixed order.  33 rows of 8 groups 256 x 47 5.9 us (tiles of 64: 11.9), dW of 1024 rows of 4 groups 8.5 (13.4).
+// meet in LDS, added in a fixed order.  33 rows of 8 groups 256 x 47 5.9 us (tiles of 64: 11.9), dW of 1024 rows of 4 groups 7.8 (13.4).
 #pragma once
 
 constexpr int FEW_AHEAD = 4;
