@@ -181,3 +181,15 @@ def test_working_memory_serves_every_form():
                     continue
                 form, tile, chunk, slabs, most = _forms(n, G, k, w, is_float, granules)[2]
                 assert slabs <= most and chunk >= 1 and tile == {CORE: 256, FEW: 32, T128: 128, T64: 64}[form]
+
+
+def test_rows_shorter_than_a_fetch_take_the_form_that_reads_single_elements():
+    """The tiles through registers fetch eight elements of a row at once: none of them may get a shorter one."""
+    few = 1             # GROUP_FEW
+    for k in range(1, 8):
+        for n_rows in (1, 300, 70_000, 1 << 30):
+            for groups in (1, 16, 512):
+                for n in (1, 64, 200, 5000):
+                    for is_float in (0, 1):
+                        for transposed in (0, 1):
+                            assert _lib().rows_form(n_rows, groups, k, n, is_float, transposed, 0) == few
