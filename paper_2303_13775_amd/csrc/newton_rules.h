@@ -46,7 +46,7 @@ inline int64_t newton_tiles_a(const NewtonSize &s, int tile) { const int64_t t =
 // four of 1024 x 1024 (144) 470 / 580, one of 2048 x 2048 (136) 799 / 1023; 32 of 200 x 200 (96) 193 / 144, two of 1024 x 4096 (72) 893 / 884,
 // one of 1024 x 1024 (36) 420 / 244, 16 of 128 x 2048 (16) 339 / 216.
 inline bool newton_large(int64_t tiles_of_a) { return tiles_of_a >= 128; }
-// A launch takes stacks up to this many padded elements, so that working memory stays in proportion
+// A launch takes stacks up to this many padded elements, so that working memory stays in proportion; a matrix of more is one by itself
 constexpr int64_t NEWTON_LAUNCH = 1 << 27;
 
 // Matrices that one workgroup each takes through all steps (one launch).  By itself a small matrix is done sooner that way; in front of
@@ -85,7 +85,7 @@ void newton_groups(int64_t n_tensors, Size size, Group group) {
                 NewtonSize one = newton_size(1, s.rows, s.cols, tile);
                 const int64_t each = (int64_t)one.mp * one.np;
                 int64_t take = std::min<int64_t>(s.count - first, room / each);
-                if (n == NEWTON_STACKS || (take == 0 && n > 0)) {
+                if (n == NEWTON_STACKS || (take <= 0 && n > 0)) {           // (below 0: behind a matrix of more than a launch takes)
                     group(in, n, tile);
                     n = 0; room = NEWTON_LAUNCH;
                     continue;

@@ -166,3 +166,32 @@ def test_every_matrix_is_in_one_launch():
             assert (own[:, 4] * own[:, 5] * own[:, 6]).sum() <= 1 << 27 or (len(own) == 1 and own[0, 4] == 1)
         assert B.load_library().gsplit_orthogonalize_work(t, len(shapes)) == 16 * max([0] + [int(rows[rows[:, 0] == l, 7].sum()) for l in set(rows[:, 0])])
     assert tiles == {1, 64, 128}
+
+
+def test_a_matrix_above_a_launch_s_limit_is_one_by_itself():
+    """A matrix of more padded elements than a launch takes, in front of, between and behind smaller ones: those keep the limit."""
+    rng = random.Random(6)
+    out = (C.c_int64 * (8 * 4096))()
+    limit = 1 << 27
+    for k in range(60):
+        shapes = [(rng.choice([1, 5, 48]), rng.choice([100, 4096, 8192]), rng.choice([300, 4096, 8192])) for _ in range(rng.choice([1, 4, 30]))]
+        above = rng.choice([(1, 32000, 8192), (1, 16384, 16384), (1, 50304, 4096), (2, 65536, 65536)])
+        for at in {0: [0], 1: [len(shapes)]}.get(k % 3, [rng.randint(0, len(shapes)), 0]):
+            shapes.insert(at, above)
+        t = (B._MatrixTensor * len(shapes))(*[B._MatrixTensor(P, P + 64, c, r, q, 0, 0) for c, r, q in shapes])
+        n = _lib().groups(t, len(shapes), out, 4096)
+        assert n <= 4096
+        rows = np.array(out[:8 * n]).reshape(n, 8)
+        taken = {i: [] for i in range(len(shapes))}
+        for row in rows.tolist():
+            taken[row[2]] += range(row[3], row[3] + row[4])
+        assert all(taken[i] == list(range(c)) for i, (c, _, _) in enumerate(shapes))
+        words = []
+        for launch in range(int(rows[-1, 0]) + 1):
+            own = rows[rows[:, 0] == launch]
+            assert (own[:, 4] * own[:, 5] * own[:, 6]).sum() <= limit or (len(own) == 1 and own[0, 4] == 1), shapes
+            words.append(int(own[:, 7].sum()))
+        # no more working memory than the largest launch within the limit (A and B no larger than X; the sums a 256th) or the matrix above it needs
+        most = max([limit] + [row[5] * row[6] for row in rows.tolist()])
+        work = B.load_library().gsplit_orthogonalize_work(t, len(shapes))
+        assert work == 16 * max(words) and work <= 16 * (most + most // 256)
