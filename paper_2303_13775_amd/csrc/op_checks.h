@@ -173,11 +173,11 @@ inline bool op_newton_bounded(double a, double b, double c, int steps) {
         if (c != 0.0) {
             const double turn = -b / (2.0 * c), root = 9.0 * b * b - 20.0 * a * c;
             if (turn > 0.0 && turn < top * top) most = std::fmax(most, q(turn));
-            if (root >= 0.0)
-                for (const double sign : {-1.0, 1.0}) {
-                    const double x = (-3.0 * b + sign * std::sqrt(root)) / (10.0 * c);
+            if (root >= 0.0) {          // of 5 c x^2 + 3 b x + a: the sum that does not cancel gives either root
+                const double q0 = -0.5 * (3.0 * b + std::copysign(std::sqrt(root), b));
+                for (const double x : {q0 / (5.0 * c), a / q0})
                     if (x > 0.0 && x < top * top) next = std::fmax(next, std::fabs(p(std::sqrt(x))));
-                }
+            }
         } else if (b != 0.0 && -a / (3.0 * b) > 0.0 && -a / (3.0 * b) < top * top) {
             next = std::fmax(next, std::fabs(p(std::sqrt(-a / (3.0 * b)))));
         }

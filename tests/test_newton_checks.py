@@ -195,3 +195,22 @@ def test_a_matrix_above_a_launch_s_limit_is_one_by_itself():
         most = max([limit] + [row[5] * row[6] for row in rows.tolist()])
         work = B.load_library().gsplit_orthogonalize_work(t, len(shapes))
         assert work == 16 * max(words) and work <= 16 * (most + most // 256)
+
+
+def test_bounds_of_coefficients_with_a_last_one_near_zero():
+    """The largest value lies where the derivative is 0, also where the last coefficient all but drops out of its equation."""
+    rng = random.Random(7)
+    seen = {True: 0, False: 0}
+    for _ in range(600):
+        a, c = rng.uniform(0, 12), rng.choice([-1, 1]) * 10.0 ** rng.uniform(-320, -6)
+        b = -a * rng.uniform(0.5, 2.0)
+        s = np.linspace(0.0, 1.0, 20001)
+        nxt, most = np.abs(s * (a + b * s ** 2 + c * s ** 4)).max(), np.abs(a + b * s ** 2 + c * s ** 4).max()
+        if abs(nxt - 1.99) > 1e-3 and abs(most - 15.0) > 1e-3:
+            ok = bool(nxt <= 1.99 and most <= 15.0)
+            assert (_newton(abc=(a, b, c), steps=1) is None) == ok, (a, b, c, nxt, most)
+            seen[ok] += 1
+    assert min(seen.values()) > 50
+    for c in (1e-320, 1e-300, 1e-20, 1e-17, 1e-14, 1e-9):
+        for sign in (1, -1):
+            assert b"bounds" in _newton(abc=(8.0, -8.0, sign * c), steps=5) and _newton(abc=(1.5, -0.5, sign * c), steps=5) is None
