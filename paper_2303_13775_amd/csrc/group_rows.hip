@@ -67,6 +67,12 @@ __device__ __forceinline__ void rounds(const Rows &R, int64_t lo, int64_t hi, co
 __device__ __forceinline__ int before_me(uint64_t same) {
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
 }
+// Counters in LDS pass from lane to lane: what a round reads and writes stays between its neighbours' (LDS does a wave's instructions in
+// their order; the compiler is told to keep it)
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 __device__ __forceinline__ void run_of(const Rows &R, int64_t &lo, int64_t &hi) {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     lo = min((blockIdx.x * (int64_t)GROUP_WAVES + wave) * R.a_wave, R.n);
@@ -141,6 +147,7 @@ __global__ __launch_bounds__(GT) void k_group_place(Rows R) {
     __syncthreads();
     rounds(R, lo, hi, first, [&](int64_t, int32_t g, uint64_t same) {
         if (g >= 0 && before_me(same) == 0) s_next[wave * R.G + g] += __popcll(same);
+        settle();
     });
     __syncthreads();
     if (WHOLE && t < R.G)
@@ -161,11 +168,14 @@ __global__ __launch_bounds__(GT) void k_group_place(Rows R) {
     __syncthreads();
     rounds(R, lo, hi, first, [&](int64_t at, int32_t g, uint64_t same) {
         const int before = before_me(same);
+        int32_t next = 0;
         if (g >= 0) {
-            const int32_t next = s_next[wave * R.G + g];
+            next = s_next[wave * R.G + g];
             R.rows[next + before] = (int32_t)(at + (threadIdx.x & 63));
-            if (before == 0) s_next[wave * R.G + g] = next + __popcll(same);
         }
+        settle();
+        if (g >= 0 && before == 0) s_next[wave * R.G + g] = next + __popcll(same);
+        settle();
     });
 }
 

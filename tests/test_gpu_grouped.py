@@ -70,6 +70,22 @@ def test_rows_that_all_share_a_group_or_have_none(ctx):
         assert ptr.tolist() == [0] * 6 and bool((order == 88).all())
 
 
+@pytest.mark.parametrize("rows", [256, 1000, 4096, 4097, 90_001, 700_000])
+@pytest.mark.parametrize("groups", [1, 2, 3, 61, 512])
+def test_counters_that_pass_from_lane_to_lane(ctx, rows, groups):
+    """The lane that counts for a group is its first of 64 rows; here it is another one in every 64."""
+    i = np.arange(rows)
+    lane, turn = i % 64, i // 64
+    group = ((lane - 7 * turn) % 64 * groups // 64).astype(np.int32)            # a rotating pattern of runs
+    group[(lane == turn % 64) & (turn % 3 == 0)] = groups - 1                   # one row by itself
+    group[lane < turn % 5] = -1
+    ptr, order = _group(ctx, group, groups)
+    key = np.where(group >= 0, group, groups)
+    want = np.argsort(key, kind="stable")[:(group >= 0).sum()]
+    assert (ptr.cpu().numpy() == np.concatenate([[0], np.bincount(key, minlength=groups + 1)[:groups].cumsum()])).all()
+    assert (order.cpu().numpy()[:len(want)] == want).all() and bool((order[len(want):] == 88).all())
+
+
 def _tol(size, n):
     return 4 * (np.sqrt(n / 16 + 64) + 2) * U * size
 
