@@ -16,10 +16,11 @@ __device__ __forceinline__ int core_wave() { return __builtin_amdgcn_readfirstla
 
 // 64 lanes fetch 16 bytes each into 1 KB of LDS side by side.  (Not the compiler's built-in function: it has every transposed read of
 // LDS wait for all fetches on their way, whatever place they write, which left none of them in flight behind the matrix instructions.
-// Nothing here waits for a fetch but core_landed.)
+// Nothing here waits for a fetch but core_landed.  The place in LDS is an operand in m0, which the instruction reads one wait state after
+// it is set: the compiler sets it, and knows what else it keeps there.)
 __device__ __forceinline__ void core_fetch(const void *from, core_u32x4 *to) {
     const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(from) : "memory");
 }
 
 // Operand rows of 128 bytes a stage, eight granules of 16 each.  Granule p of row r of LDS holds granule p ^ (r / 2) % 8: sixteen rows of
