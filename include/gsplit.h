@@ -594,8 +594,9 @@ GSPLIT_API int gsplit_adamw_step(gsplit_ctx *ctx, const gsplit_adamw_config *con
  *
  * gsplit_group_rows sorts rows by their group: d_group [n_rows] int32; a row whose group lies outside
  * [0, n_groups) belongs to none.  d_group_ptr [n_groups + 1] receives where each group starts, d_rows [n_rows] the rows in that
- * order, those of a group ascending (d_rows may not be d_group); d_rows behind d_group_ptr[n_groups] is left as it was.  n_rows < 2^31, n_groups at most
- * GSPLIT_MAX_GROUPS.  EINVAL for NULL (d_group and d_rows may be NULL without rows) or misaligned pointers and sizes out of range.
+ * order, those of a group ascending; d_rows behind d_group_ptr[n_groups] is left as it was.  n_rows < 2^31, n_groups at most
+ * GSPLIT_MAX_GROUPS.  EINVAL for NULL (d_group and d_rows may be NULL without rows) or misaligned pointers, sizes out of range, and an
+ * output that overlaps another list.
  * Asynchronous; may be captured at any time; scratch memory as for the losses above. */
 #define GSPLIT_MAX_GROUPS 512
 
@@ -612,13 +613,13 @@ GSPLIT_API int gsplit_group_rows(gsplit_ctx *ctx, const int32_t *d_group, int64_
  * read nor written, the buffers' padding neither; a group without rows has the gradient 0.  Sums are float; float products go through
  * the bfloat16 matrix unit in six partial products (2^-24 of each product, infinities and NaN as in float arithmetic), those of
  * bfloat16 values are exact; y and dx are rounded once.  The sums are formed in a fixed order: the same bits on every call.
- * d_bias may be NULL (0).  d_dx, d_dw or d_dbias may be NULL: not asked for (d_dbias needs d_dw).  No output
- * may overlap anything.  Offsets that are not ascending or outside [0, n_rows] and rows outside it give wrong values, but no access
- * outside the buffers.
+ * d_bias may be NULL (0).  d_dx, d_dw or d_dbias may be NULL: not asked for (d_dbias needs d_dw).  No output, nor the
+ * working memory, may overlap another buffer of the call; columns of one buffer side by side do not.  Offsets that are not
+ * ascending or outside [0, n_rows] and rows outside it give wrong values, but no access outside the buffers.
  * d_work: 16-byte aligned working memory of gsplit_grouped_linear_work() bytes (NULL if that is 0, or without d_dw); one call
  * uses it at a time.  Asynchronous; may be captured at any time.
  * EINVAL for NULL or misaligned pointers, an unknown dtype, strides below their width or of 2^31 and more, n_groups above GSPLIT_MAX_GROUPS, widths
- * outside 1 .. 2^20, n_rows outside 0 .. 2^31 - 1, a backward call that asks for nothing. */
+ * outside 1 .. 2^20, n_rows outside 0 .. 2^31 - 1, a backward call that asks for nothing, an output that overlaps another buffer. */
 typedef struct {
     int32_t dtype;
     int32_t n_groups, n_in, n_out;

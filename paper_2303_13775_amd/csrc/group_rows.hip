@@ -186,7 +186,9 @@ extern "C" int gsplit_group_rows(gsplit_ctx *ctx, const int32_t *d_group, int64_
     if (!ctx) return GSPLIT_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     return gs_call(ctx, st, [&] {
-        if (const char *e = op_check_group_rows(d_group, n_rows, n_groups, d_group_ptr, d_rows))
+        const char *e = op_check_group_rows(d_group, n_rows, n_groups, d_group_ptr, d_rows);
+        if (!e) e = op_apart_group_rows(d_group, n_rows, n_groups, d_group_ptr, d_rows);
+        if (e)
             return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_group_rows: ") + e);
         const GroupRuns runs = group_runs(n_rows, n_groups, GS_ROW_PARTS * GS_ROW_PART_BYTES / 4, ctx->n_cu);
         int bits = 0;

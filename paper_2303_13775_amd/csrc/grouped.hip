@@ -714,7 +714,9 @@ extern "C" int gsplit_grouped_linear_fwd(gsplit_ctx *ctx, const gsplit_grouped_c
     if (!ctx) return GSPLIT_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     return gs_call(ctx, st, [&] {
-        if (const char *e = op_check_grouped_fwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_bias, d_y, y_stride))
+        const char *e = op_check_grouped_fwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_bias, d_y, y_stride);
+        if (!e) e = op_apart_grouped_fwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_bias, d_y, y_stride);
+        if (e)
             return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_fwd: ") + e);
         if (n_rows == 0) return (int)GSPLIT_OK;
         GsTimeScope ts(ctx, "grouped_fwd", -1, st);
@@ -748,6 +750,8 @@ extern "C" int gsplit_grouped_linear_bwd(gsplit_ctx *ctx, const gsplit_grouped_c
                                    in_granules({d_x, d_dy, d_dw, d_dbias}, {c->n_in, c->n_out, x_stride, dy_stride}), ctx->n_cu);
             if (f.slabs && !d_work) e = "NULL d_work";
         }
+        if (!e) e = op_apart_grouped_bwd(c, d_x, n_rows, x_stride, d_group_ptr, d_rows, d_w, d_dy, dy_stride, d_dx, dx_stride, d_dw, d_dbias,
+                                         d_work, f.slabs * ((int64_t)c->n_in + 1) * c->n_out * (int64_t)sizeof(float));
         if (e) return gs_fail(ctx, GSPLIT_EINVAL, std::string("gsplit_grouped_linear_bwd: ") + e);
         const RowList list{d_rows, (int32_t)n_rows};
         if (d_dx && n_rows > 0) {

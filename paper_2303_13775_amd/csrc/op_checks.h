@@ -2,9 +2,11 @@
 // (host programs include this header too).  Each returns what is wrong, or nullptr.
 #pragma once
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
+#include <numeric>
 
 #include "gsplit.h"
 
@@ -104,6 +106,53 @@ inline const char *op_check_adamw(const gsplit_adamw_config *c, const gsplit_ada
     return nullptr;
 }
 
+// Memory of a call: `rows` runs of `width` bytes, `stride` bytes from one to the next (at least `width`)
+struct OpArea {
+    const void *p;
+    int64_t rows, width, stride;
+    bool empty() const { return !p || rows <= 0 || width <= 0; }
+    int64_t first() const { return (int64_t)(uintptr_t)p; }
+    int64_t end() const {           // INT64_MAX: no memory reaches so far
+        const int64_t left = INT64_MAX - first(), more = rows - 1;
+        return left < width || (more && more > (left - width) / stride) ? INT64_MAX : first() + more * stride + width;
+    }
+};
+inline OpArea op_run(const void *p, int64_t bytes) { return {p, 1, bytes, bytes}; }
+inline OpArea op_matrix(const void *p, int64_t n_rows, int64_t width, int64_t stride, int size) { return {p, n_rows, width * size, stride * size}; }
+inline int64_t op_floor_div(int64_t a, int64_t b) { return a / b - (a % b != 0 && (a < 0) != (b < 0)); }
+
+// Whether two areas have a byte in common; columns of one buffer side by side have none.
+inline bool op_meet(const OpArea &a, const OpArea &b) {
+    if (a.empty() || b.empty() || a.first() >= b.end() || b.first() >= a.end() || a.end() == INT64_MAX || b.end() == INT64_MAX) return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    // rows i of a and j of b meet where low < j * b.stride - i * a.stride < high
+    const int64_t d = b.first() - a.first(), low = -b.width - d, high = a.width - d;
+    if (a.rows > 1 && b.rows > 1 && a.stride == b.stride) {
+        const int64_t k = std::max(op_floor_div(low, a.stride) + 1, 1 - a.rows);         // j - i
+        return k < b.rows && k * a.stride < high;
+    }
+    if (a.rows > 1 && b.rows > 1) {         // the difference is a multiple of what divides both strides
+        const int64_t g = std::gcd(a.stride, b.stride);
+        if ((op_floor_div(low, g) + 1) * g >= high) return false;
+    }
+    if (a.rows > b.rows) return op_meet(b, a);
+    // from the first row of a that ends behind b's start on: the first row of b that ends behind this one's start
+    for (int64_t i = std::max<int64_t>(op_floor_div(d - a.width, a.stride) + 1, 0); i < a.rows; ++i) {
+        const int64_t at = i * a.stride, j = std::max<int64_t>(op_floor_div(low + at, b.stride) + 1, 0);
+        if (j >= b.rows) return false;
+        if (j * b.stride - at < high) return true;
+    }
+    return false;
+}
+// The first `written` areas overlap no other one.
+inline const char *op_check_apart(std::initializer_list<OpArea> areas, int written) {
+    const OpArea *p = areas.begin();
+    for (int i = 0; i < written; ++i)
+        for (int j = i + 1; j < (int)areas.size(); ++j)
+            if (op_meet(p[i], p[j])) return "what is written overlaps another buffer";
+    return nullptr;
+}
+
 inline const char *op_check_group_rows(const int32_t *d_group, int64_t n_rows, int32_t n_groups, const int32_t *d_group_ptr,
                                        const int32_t *d_rows) {
     if (n_rows < 0 || n_rows > INT32_MAX) return "n_rows out of range";
@@ -160,6 +209,30 @@ inline const char *op_check_grouped_bwd(const gsplit_grouped_config *c, const vo
     if (d_dx && n_rows > 0 && !d_w) return "NULL buffer";
     return op_misaligned(d_w, size) || op_misaligned(d_dw, 4) || op_misaligned(d_dbias, 4) || op_misaligned(d_work, 16) ? "misaligned buffer"
                                                                                                                         : nullptr;
+}
+
+// (of arguments that are right by themselves)
+inline const char *op_apart_group_rows(const int32_t *d_group, int64_t n_rows, int32_t n_groups, const int32_t *d_group_ptr, const int32_t *d_rows) {
+    return op_check_apart({op_run(d_group_ptr, 4 * ((int64_t)n_groups + 1)), op_run(d_rows, 4 * n_rows), op_run(d_group, 4 * n_rows)}, 2);
+}
+inline const char *op_apart_grouped_fwd(const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                        const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const float *d_bias,
+                                        const void *d_y, int64_t y_stride) {
+    const int size = op_elem_size(c->dtype);
+    const int64_t b = (int64_t)c->n_groups * c->n_out;
+    return op_check_apart({op_matrix(d_y, n_rows, c->n_out, y_stride, size), op_matrix(d_x, n_rows, c->n_in, x_stride, size), op_run(d_w, b * c->n_in * size),
+                           op_run(d_bias, 4 * b), op_run(d_group_ptr, 4 * ((int64_t)c->n_groups + 1)), op_run(d_rows, 4 * n_rows)}, 1);
+}
+inline const char *op_apart_grouped_bwd(const gsplit_grouped_config *c, const void *d_x, int64_t n_rows, int64_t x_stride,
+                                        const int32_t *d_group_ptr, const int32_t *d_rows, const void *d_w, const void *d_dy,
+                                        int64_t dy_stride, const void *d_dx, int64_t dx_stride, const float *d_dw, const float *d_dbias,
+                                        const void *d_work, int64_t work_bytes) {
+    const int size = op_elem_size(c->dtype);
+    const int64_t b = (int64_t)c->n_groups * c->n_out;
+    return op_check_apart({op_matrix(d_dx, n_rows, c->n_in, dx_stride, size), op_run(d_dw, b * c->n_in * 4), op_run(d_dbias, 4 * b),
+                           op_run(d_dw ? d_work : nullptr, work_bytes), op_matrix(d_x, n_rows, c->n_in, x_stride, size),
+                           op_matrix(d_dy, n_rows, c->n_out, dy_stride, size), op_run(d_w, b * c->n_in * size),
+                           op_run(d_group_ptr, 4 * ((int64_t)c->n_groups + 1)), op_run(d_rows, 4 * n_rows)}, 4);
 }
 
 // Singular values s of [0, 1] under s -> |s (a + b s^2 + c s^4)|: the bounds of what the halves hold (newton.hip).

@@ -424,3 +424,37 @@ def test_refusals(ctx):
     assert ctx.gsplit_grouped_linear_work(big, wb).numel() > 0
     with pytest.raises(AssertionError):
         ctx.gsplit_grouped_linear_bwd(big, i32(2), None, wb, big.clone(), None, wb.clone(), None, torch.zeros(8, device="cuda"))
+
+
+def test_outputs_that_overlap_in_part(ctx):
+    from paper_2303_13775_amd import GsplitError
+    rows, n = 300, 8
+    buf, ptr = torch.ones((rows + 1, n), device="cuda"), torch.tensor([0, 100, rows], dtype=torch.int32, device="cuda")
+    w, ints = torch.ones((2, n, n), device="cuda"), torch.zeros(2 * rows + 2, dtype=torch.int32, device="cuda")
+    dy, dw, room = torch.ones((rows, n), device="cuda"), torch.zeros((4, n, n), device="cuda"), torch.zeros((5000, n), device="cuda")
+    assert ctx.gsplit_grouped_linear_work(dy, w).numel() <= room.numel()
+    parts = dw.view(-1)
+    calls = [lambda: ctx.gsplit_group_rows(ints[:rows], ptr, ints[rows - 1:2 * rows - 1]), lambda: ctx.gsplit_group_rows(ints[:rows], ints[rows:rows + 3], ints[rows + 2:2 * rows + 2]),
+             lambda: ctx.gsplit_grouped_linear_fwd(buf[:-1], ptr, None, w, None, buf[1:]),
+             lambda: ctx.gsplit_grouped_linear_bwd(buf[:-1], ptr, None, w, dy, buf[1:], None, None),
+             lambda: ctx.gsplit_grouped_linear_bwd(buf[:-1], ptr, None, w, dy, None, w, None, room),
+             lambda: ctx.gsplit_grouped_linear_bwd(buf[:-1], ptr, None, w, dy, None, dw[:2], parts[2 * n * n - 2:2 * n * n + 2 * n - 2].view(2, n), room),
+             lambda: ctx.gsplit_grouped_linear_bwd(buf[:-1], ptr, None, dw[1:3], dy, None, dw[:2], None, room)]
+    for k, call in enumerate(calls):
+        with pytest.raises(GsplitError) as e:
+            call()
+        assert e.value.code == -1 and "overlaps" in str(e.value), k
+    assert bool((buf == 1).all()) and bool((w == 1).all()) and not dw.any() and not ints.any()        # nothing was written
+    # several chunks of rows, whose gradients go through the working memory: not in the place of an output
+    big, wide = torch.ones((70_000, 64), device="cuda"), torch.ones((1, 64, 64), device="cuda")
+    one = torch.tensor([0, 70_000], dtype=torch.int32, device="cuda")
+    need = ctx.gsplit_grouped_linear_work(big, wide)
+    assert need.numel() > 64 * 64
+    with pytest.raises(GsplitError) as e:
+        ctx.gsplit_grouped_linear_bwd(big, one, None, wide, big, None, need[:64 * 64].view(1, 64, 64), None, need)
+    assert "overlaps" in str(e.value)
+    # what lies side by side is taken: columns of one buffer, neighbours in one allocation
+    both = torch.ones((rows, 2 * n), device="cuda")
+    ctx.gsplit_grouped_linear_fwd(both[:, n:], ptr, None, w, None, both[:, :n])
+    ctx.gsplit_grouped_linear_bwd(both[:, n:], ptr, None, w, dy, None, dw[:2], parts[2 * n * n:2 * n * n + 2 * n].view(2, n), room)
+    assert bool((both[:, :n] == n).all()) and dw[:2, 0, 0].tolist() == [100, 200] and parts[2 * n * n].item() == 100 and not dw[2:].view(-1)[2 * n:].any()
