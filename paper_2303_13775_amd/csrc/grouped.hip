@@ -655,10 +655,9 @@ __global__ __launch_bounds__(NT) void k_grouped_weights_sum(WeightArgs A) {
             store4(dw + 4 * x, sum, 4);
         } else {
             const int64_t i = quads * 4 + (x - quads);
-            float sum = 0.f;
-            for (int c = 0; c < chunks; ++c) sum += part[c * each + i];
-            if (i < words) dw[i] = sum;
-            else db[i - words] = sum;
+            double sum = 0.0;           // (a bias gradient's, as within most chunks; and the last words of dW)
+            for (int c = 0; c < chunks; ++c) sum += (double)part[c * each + i];
+            (i < words ? dw + i : db + (i - words))[0] = (float)sum;
         }
     }
 }

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 #pragma unroll
                 for (int b = 0; b < 2; ++b) f.q[b] = across_fragment<32>(now, base_q, h, 4 * b);
             };
-            if (bias)           // a column's sum is its product with ones
+            if (bias)           // a column's sum is its product with ones, in float over the chunk as dW is (the other forms' are double: here a lane has no column by itself)
                 core_contract<4, CoreFrag>(stages, lds, fetch, read, [&](const CoreFrag &f) __attribute__((always_inline)) {
                     sums.multiply(f);
 #pragma unroll

@@ -458,3 +458,18 @@ def test_outputs_that_overlap_in_part(ctx):
     ctx.gsplit_grouped_linear_fwd(both[:, n:], ptr, None, w, None, both[:, :n])
     ctx.gsplit_grouped_linear_bwd(both[:, n:], ptr, None, w, dy, None, dw[:2], parts[2 * n * n:2 * n * n + 2 * n].view(2, n), room)
     assert bool((both[:, :n] == n).all()) and dw[:2, 0, 0].tolist() == [100, 200] and parts[2 * n * n].item() == 100 and not dw[2:].view(-1)[2 * n:].any()
+
+
+@pytest.mark.parametrize("dtype, n_in, n_out", [(F32, 64, 64), (F32, 200, 301), (BF16, 64, 63), (BF16, 256, 256)])
+def test_bias_gradients_of_many_chunks(ctx, dtype, n_in, n_out):
+    """One large row, then ones too far apart to share a chunk: added to it one by one in float, each would be lost."""
+    rows, apart = 70_000, 1500
+    x, dy = torch.zeros((rows, n_in), dtype=dtype, device="cuda"), torch.zeros((rows, n_out), dtype=dtype, device="cuda")
+    dy[0], dy[apart::apart] = 2.0**24, 1.0
+    w, ptr = torch.zeros((1, n_in, n_out), dtype=dtype, device="cuda"), torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    dw, db = torch.full((1, n_in, n_out), 7.0, device="cuda"), torch.zeros((1, n_out), device="cuda")
+    work = ctx.gsplit_grouped_linear_work(x, w)
+    assert work.numel() > n_in * n_out                      # (there are chunks)
+    ctx.gsplit_grouped_linear_bwd(x, ptr, None, w, dy, None, dw, db, work)
+    want = np.float32(2.0**24 + (rows - 1) // apart)        # sums of whole numbers are exact in double: one rounding
+    assert bool((db == float(want)).all()) and want > 2.0**24 and not dw.any()
