@@ -205,6 +205,68 @@ def test_a_matrix_of_more_than_32_bits_of_elements(ctx):
     assert int(torch.count_nonzero(out)) == cols
 
 
+def _one_a_row_or_column(rows, cols, value):
+    """(matrix, places of its values): min(rows, cols) values, no two in a row or column, the last element of all among them."""
+    k, n = min(rows, cols), max(rows, cols)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    of = torch.randperm(n - 1, device="cuda", generator=gen)[:k]
+    of[k - 1] = n - 1
+    i = torch.arange(k, device="cuda")
+    at = of * cols + i if rows > cols else i * cols + of
+    g = torch.zeros((rows, cols), device="cuda")
+    g.view(-1)[at] = value
+    return g, at
+
+
+def _count(t):
+    return sum(int(torch.count_nonzero(t[i:i + 4096])) for i in range(0, len(t), 4096))
+
+
+@pytest.mark.parametrize("rows, cols", [(65_000, 33_100), (33_100, 65_000)])
+def test_a_matrix_past_2_to_the_31_elements(ctx, rows, cols):
+    """Element numbers that 31 bits do not hold: orthogonalised, and as gradient, momentum and parameter of an update from zeros.  Tolerance
+    as for the matrix above; of two steps, whose small values (0.0055, 0.019) pass on what a step rounds with factors of at most 1."""
+    from paper_2303_13775_amd import MatrixTensors, MuonTensors
+    assert rows * cols > 2**31
+    g, at = _one_a_row_or_column(rows, cols, 1e-3)
+    assert int(at.max()) == rows * cols - 1
+    s = 1 / math.sqrt(min(rows, cols))
+    for _ in range(2):
+        s *= ABC[0] + s * s * (ABC[1] + s * s * ABC[2])
+    off = 2 * 8 * 2.0**-22
+    out = torch.full_like(g, 7.0)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), steps=2, eps=0.0)
+    assert float((out.view(-1)[at].double() - s).abs().max()) <= off * s and _count(out) == len(at)
+    out.zero_()
+    mom = torch.zeros_like(g)
+    ctx.gsplit_muon_step(MuonTensors([out], [g], [mom]), lr=0.5, momentum=0.75, weight_decay=0.1, scaling="plain", steps=2, eps=0.0)
+    # (the momentum of one value is a float product, 1e-3 / 4; the update rounds once)
+    assert bool((mom.view(-1)[at] == g.view(-1)[at] * 0.25).all()) and _count(mom) == len(at)
+    assert float((out.view(-1)[at].double() + 0.5 * s).abs().max()) <= (off + U) * 0.5 * s and _count(out) == len(at)
+
+
+@pytest.mark.parametrize("count, rows, cols", [(530_000, 64, 64), (131_000, 65, 253), (1_100, 1400, 1408)])
+def test_matrices_that_lie_past_2_to_the_31_elements(ctx, count, rows, cols):
+    """A stack of zeros with a few matrices in front, around element 2^31 and at the end: those come out as by themselves, the rest zero."""
+    from paper_2303_13775_amd import MatrixTensors
+    assert count * rows * cols > 2**31
+    edge = 2**31 // (rows * cols)
+    at = [0, 1, edge - 1, edge, edge + 1, count - 1]
+    few, = [g.to(BF16) for g in _matrices([(len(at), rows, cols)], 77)]
+    g = torch.zeros((count, rows, cols), dtype=BF16, device="cuda")
+    g[at] = few
+    alone = torch.zeros_like(few)
+    ctx.gsplit_orthogonalize(MatrixTensors([few], [alone]), steps=2)
+    out = torch.full_like(g, 7.0)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), steps=2)
+    want, off = _expected(few.double(), steps=2)
+    for k, i in enumerate(at):
+        _close((count, k), out[i:i + 1], want[k:k + 1], off[k:k + 1], BF16)
+    out[at] = 0.0
+    assert bool(alone.any()) and _count(out) == 0
+    _close("alone", alone, want, off, BF16)
+
+
 def _types(kind, n):
     return [F32] * n if kind == "f32" else [BF16] * n if kind == "bf16" else [(F32, BF16)[i % 2] for i in range(n)]
 
