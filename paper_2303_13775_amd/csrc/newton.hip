@@ -177,6 +177,12 @@ __device__ __forceinline__ void put4(half *p, const float (&v)[4]) {
     *(halfx4 *)(p + 32) = lo;
 }
 
+// What a matrix is scaled by.  One of zeros stays one, also where an eps below 2^14 / the largest double is all of the norm; of a norm
+// that is not finite nothing is left
+__device__ __forceinline__ double newton_factor(double norm) {
+    return norm < INFINITY ? norm > 0.0 ? fmin((double)SCALE_X / norm, 1e300) : 0.0 : NAN;
+}
+
 // X = u / (|u| + eps): a workgroup a tile of 64 x 64 of the padded matrix
 template <bool MOMENTUM>
 __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double eps) {
@@ -226,8 +232,7 @@ __global__ __launch_bounds__(NT) void k_newton_start(Call C, Momentum M, double 
     if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
     __syncthreads();
     const double norm = sqrt((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) + eps;
-    // a matrix of zeros stays one; of a norm that is not finite nothing is left
-    const double factor = norm < INFINITY ? norm > 0.0 ? (double)SCALE_X / norm : 0.0 : NAN;
+    const double factor = newton_factor(norm);
     half *const out = (half *)C.x(s, i, 0);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -722,7 +727,7 @@ __global__ __launch_bounds__(ONE_NT) void k_newton_one(Call C, Momentum M, doubl
     sum = s_sum[0];
     for (int w = 1; w < ONE_NT / 64; ++w) sum += s_sum[w];
     const double norm = sqrt(sum) + eps;
-    const double factor = norm < INFINITY ? norm > 0.0 ? (double)SCALE_X / norm : 0.0 : NAN;
+    const double factor = newton_factor(norm);
     const auto place_x = [&](int r, int c, const float (&u)[4]) __attribute__((always_inline)) {
         float v[4];
 #pragma unroll

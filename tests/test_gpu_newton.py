@@ -173,6 +173,20 @@ def test_zeros_and_values_that_are_not_finite(ctx, rows, cols):
         assert torch.equal(out[0], alone[0]) and torch.equal(out[4], alone[4])
 
 
+@pytest.mark.parametrize("rows, cols", [(5, 9), (64, 300), (70, 90), (900, 65)])
+@pytest.mark.parametrize("eps", [0.0, 5e-324, 1e-310, 1e-300, 1e-45, 1e300])
+def test_zeros_with_any_eps(ctx, rows, cols, eps):
+    from paper_2303_13775_amd import MatrixTensors, MuonTensors
+    g, = _matrices([(3, rows, cols)], rows)
+    g[1] = 0.0
+    out = torch.full_like(g, 7.0)
+    ctx.gsplit_orthogonalize(MatrixTensors([g], [out]), eps=eps)
+    assert not out[1].any() and bool(out.isfinite().all()) and bool(out[0].any()) == (eps < 1.0)
+    p, m = torch.ones_like(g), torch.zeros_like(g)
+    ctx.gsplit_muon_step(MuonTensors([p], [g], [m]), eps=eps)
+    assert bool((p[1] == 1).all()) and bool(p.isfinite().all())
+
+
 def test_rank_one_and_repeated_rows(ctx):
     """Matrices whose singular values are mostly 0: their direction comes out, the rest stays at rounding times what the steps raise it by."""
     from paper_2303_13775_amd import MatrixTensors
