@@ -155,7 +155,7 @@ __global__ __launch_bounds__(CT) __attribute__((amdgpu_waves_per_eu(2, 2))) void
         const bool whole = s.chunks == 1;
         if (!whole && (uint64_t)s.slab >= (uint64_t)A.slabs) continue;          // (offsets that make no sense)
         const int m0 = s.side / A.tiles_n * T, n0 = s.side % A.tiles_n * T;
-        // a lane holds the number of a row of the next stage
+        // a lane holds the number of a row of the next stage (held inside the rows at once: the stage's fetches wait for the list's load)
         int next = 0;
         const auto look_up = [&](int t) __attribute__((always_inline)) {
             const int r = A.list.at(s.first + min(t * 64 + lane, s.rows - 1));
