@@ -113,7 +113,7 @@ struct OpArea {
     bool empty() const { return !p || rows <= 0 || width <= 0; }
     int64_t first() const { return (int64_t)(uintptr_t)p; }
     int64_t end() const {           // INT64_MAX: no memory reaches so far
-        const int64_t left = INT64_MAX - first(), more = rows - 1;
+        const int64_t left = first() < 0 ? 0 : INT64_MAX - first(), more = rows - 1;
         return left < width || (more && more > (left - width) / stride) ? INT64_MAX : first() + more * stride + width;
     }
 };

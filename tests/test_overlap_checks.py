@@ -79,6 +79,7 @@ def test_areas_of_any_size():
     assert not m(half, top, 2048, 4096, half + 2048, top, 1024, 8192)                   # every second row's other half
     assert not m(None, 5, 4, 4, None, 5, 4, 4) and not m(half, 0, 4, 4, half, 1, 4, 4)
     assert not m(half, top, 4, 2 ** 33, half + 8, top, 4, 2 ** 33 - 4)                  # (there is no such memory)
+    assert not m(2 ** 64 - 64, 4, 4, 8, 2 ** 64 - 64, 4, 4, 8) and not m(2 ** 63, 1, 4, 4, half, 3, 4, 4)
 
 
 GROUPS, N_IN, N_OUT, ROWS = 4, 8, 6, 10
